@@ -22,7 +22,7 @@ __all__ = [
     "lstm_dyn_create_cell", "lstm_dyn_check_cell_args", "CELL_LSTM", "CELL_GRU", "CELL_RNN",
     "lstm_dyn_forward_stop", "lstm_dyn_check_stop_args", "lstm_dyn_forward_train",
     "lstm_dyn_backward", "lstm_dyn_check_backward_args", "lstm_dyn_forward_noalloc",
-    "NOALLOC_SCRATCH_BYTES",
+    "NOALLOC_SCRATCH_BYTES", "GatedScan", "TokenEmbed", "AdamW", "BeamSearch",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -455,3 +455,6 @@ class LstmDyn:
 
     def __exit__(self, *exc):
         self.close()
+
+
+from .ops import AdamW, BeamSearch, GatedScan, TokenEmbed  # noqa: E402  (they use the names above)

@@ -10,6 +10,7 @@
 #include <rocblas/rocblas.h>
 
 #include "../../include/lstm_dyn.h"
+#include "../../include/lstm_dyn_ops.h"
 #include "launch.h"
 
 // rocBLAS serves the backward pass's plain GEMMs only.  It is loaded at the
@@ -248,6 +249,7 @@ extern "C" const char* lstm_dyn_strerror(int status) {
         case LSTM_DYN_ERR_TIMEOUT: return "a wait of a cooperative kernel exceeded its bound";
         case LSTM_DYN_ERR_TOO_LARGE:
             return "the workspace exceeds the allocation-free entry point's fixed scratch";
+        case LSTM_DYN_ERR_BAD_TOKENS: return "a token was outside [0, V) and taken as none";
         default: return "unknown status";
     }
 }

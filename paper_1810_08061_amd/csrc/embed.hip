@@ -1,0 +1,479 @@
+// embed.hip -- rows of a token table as the loop's input, and the gradient of
+// the table by sorted tokens.
+//
+//   x[b][t] = scale table[tok[b][t]] (t < L[b], else 0)
+//   d_table[v] = scale sum_{(b, t): tok = v} dx[b][t]
+//
+// The gradient: a stable radix sort of the places n = b T + t by token (places
+// past a length or with a bad token sort last, as token V), then sums over
+// pieces of R sorted places.  A token whose places lie inside one piece is
+// written at once; of the others each piece leaves a partial sum, joined
+// afterwards in the pieces' order.  No atomics on the sums, so the same sizes
+// give the same bits.  Rows of tokens that do not occur are found by a stamp
+// per token and written with zeros.
+#include "ops.h"
+
+namespace ldyn {
+namespace {
+
+constexpr int SORT_THREADS = 256, SORT_WAVES = 4, SORT_ITEMS = 8;
+constexpr int SORT_TILE = SORT_THREADS * SORT_ITEMS;
+constexpr int SORT_BITS = 9, SORT_BINS = 1 << SORT_BITS;
+
+struct EmbedParams {
+    const int32_t* tokens;
+    const int32_t* lengths;
+    int32_t* status;
+    uint32_t* epoch;   // bumped once per gradient
+    uint32_t* stamp;   // [V] the epoch of the last gradient that saw the token
+    uint32_t* hist;    // [blocks][bins]
+    float* part;       // [pieces][2][D]
+    int N, T, V, D;
+    float scale;
+};
+
+// The sort key of place n: its token, or V.
+__device__ inline uint32_t key_of(const EmbedParams& p, int n, bool report) {
+    const int b = n / p.T, t = n - b * p.T;
+    const int L = row_length(p.lengths, b, p.T, p.status, report && t == 0);
+    if (t >= L) return (uint32_t)p.V;
+    const int tok = p.tokens[n];
+    if ((unsigned)tok < (unsigned)p.V) return (uint32_t)tok;
+    if (report) atomicOr(p.status, STATUS_BAD_TOKENS);
+    return (uint32_t)p.V;
+}
+
+// --- lookup: one wave per row ---------------------------------------------------
+
+template <class E, int W>
+__global__ void __launch_bounds__(256)
+embed_forward_kernel(EmbedParams p, const E* __restrict__ table, E* __restrict__ x) {
+    const int lane = threadIdx.x & 63;
+    for (long n = blockIdx.x * 4L + (threadIdx.x >> 6); n < p.N; n += gridDim.x * 4L) {
+        const uint32_t v = (uint32_t)__builtin_amdgcn_readfirstlane((int)key_of(p, (int)n, lane == 0));
+        E* dst = x + n * p.D;
+        const E* src = table + (long)v * p.D;
+        for (int c = lane * W; c < p.D; c += 64 * W) {
+            float q[W];
+            if (v < (uint32_t)p.V) {
+                load_vec<E, W>(src + c, q);
+#pragma unroll
+                for (int i = 0; i < W; ++i) q[i] *= p.scale;
+            } else {
+#pragma unroll
+                for (int i = 0; i < W; ++i) q[i] = 0.0f;
+            }
+            store_vec<E, W>(dst + c, q);
+        }
+    }
+}
+
+// --- sort -------------------------------------------------------------------------
+
+struct SortPass {
+    const uint32_t* key_in;  // null in the first pass: key_of
+    const uint32_t* pos_in;
+    uint32_t* key_out;
+    uint32_t* pos_out;
+    int shift, bits, blocks;
+};
+
+__device__ inline uint32_t sort_key(const EmbedParams& p, const SortPass& s, int n, bool report) {
+    return s.key_in ? s.key_in[n] : key_of(p, n, report);
+}
+
+__global__ void __launch_bounds__(SORT_THREADS) sort_hist_kernel(EmbedParams p, SortPass s) {
+    __shared__ uint32_t cnt[SORT_BINS];
+    const int bins = 1 << s.bits;
+    for (int i = threadIdx.x; i < bins; i += SORT_THREADS) cnt[i] = 0;
+    __syncthreads();
+    const uint32_t now = *p.epoch + 1;
+#pragma unroll
+    for (int j = 0; j < SORT_ITEMS; ++j) {
+        const int n = blockIdx.x * SORT_TILE + j * SORT_THREADS + threadIdx.x;
+        if (n >= p.N) break;
+        const uint32_t k = sort_key(p, s, n, true);
+        if (!s.key_in && k < (uint32_t)p.V) p.stamp[k] = now;
+        atomicAdd(&cnt[(k >> s.shift) & (bins - 1)], 1u);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < bins; i += SORT_THREADS) p.hist[(long)blockIdx.x * bins + i] = cnt[i];
+}
+
+// Places of a block go behind those of smaller digits and of earlier blocks;
+// within the block in order (each wave holds a run of places and counts its
+// own digits, 64 places at a time).
+__global__ void __launch_bounds__(SORT_THREADS) sort_scatter_kernel(EmbedParams p, SortPass s) {
+    __shared__ uint32_t cnt[SORT_WAVES][SORT_BINS];
+    __shared__ uint32_t wsum[SORT_WAVES];
+    const int bins = 1 << s.bits, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    if (!s.key_in && blockIdx.x == 0 && threadIdx.x == 0) *p.epoch += 1;  // the stamps' reader comes later
+    for (int i = threadIdx.x; i < SORT_WAVES * SORT_BINS; i += SORT_THREADS) (&cnt[0][0])[i] = 0;
+    __syncthreads();
+
+    uint32_t key[SORT_ITEMS], rank[SORT_ITEMS];
+    const int first = blockIdx.x * SORT_TILE + w * 64 * SORT_ITEMS + lane;
+#pragma unroll
+    for (int j = 0; j < SORT_ITEMS; ++j) {
+        const int n = first + j * 64;
+        const bool on = n < p.N;
+        key[j] = on ? sort_key(p, s, n, false) : 0;
+        const uint32_t d = (key[j] >> s.shift) & (bins - 1);
+        unsigned long long peers = __ballot(on);
+        for (int bit = 0; bit < s.bits; ++bit) {
+            const unsigned long long m = __ballot((d >> bit) & 1);
+            peers &= (d >> bit) & 1 ? m : ~m;
+        }
+        const int before = __popcll(peers & ((1ull << lane) - 1));
+        uint32_t old = 0;
+        if (on && before == 0) old = atomicAdd(&cnt[w][d], (uint32_t)__popcll(peers));
+        old = __shfl(old, on ? __ffsll(peers) - 1 : lane);
+        rank[j] = old + before;
+    }
+    // the start of each digit: its total over all blocks, scanned; plus earlier blocks' counts
+    constexpr int PER = SORT_BINS / SORT_THREADS;
+    uint32_t total[PER], mine[PER], sum = 0;
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+        const int d = threadIdx.x * PER + q;
+        uint32_t t = 0, m = 0;
+        if (d < bins) {
+#pragma unroll 8
+            for (int b = 0; b < s.blocks; ++b) {
+                const uint32_t c = p.hist[(long)b * bins + d];
+                t += c;
+                m += b < (int)blockIdx.x ? c : 0;
+            }
+        }
+        total[q] = t;
+        mine[q] = m;
+        sum += t;
+    }
+    uint32_t incl = sum;
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t u = __shfl_up(incl, o);
+        if (lane >= o) incl += u;
+    }
+    if (lane == 63) wsum[w] = incl;
+    __syncthreads();
+    uint32_t run = incl - sum;
+    for (int i = 0; i < w; ++i) run += wsum[i];
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+        const int d = threadIdx.x * PER + q;
+        if (d < bins) {
+            uint32_t at = run + mine[q];
+            for (int i = 0; i < SORT_WAVES; ++i) {
+                const uint32_t c = cnt[i][d];
+                cnt[i][d] = at;
+                at += c;
+            }
+        }
+        run += total[q];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < SORT_ITEMS; ++j) {
+        const int n = first + j * 64;
+        if (n >= p.N) continue;
+        const uint32_t at = cnt[w][(key[j] >> s.shift) & (bins - 1)] + rank[j];
+        s.key_out[at] = key[j];
+        s.pos_out[at] = s.pos_in ? s.pos_in[n] : (uint32_t)n;
+    }
+}
+
+// --- sums over sorted places --------------------------------------------------------
+
+// Waves below `pieces * tiles`: piece w / tiles, columns of tile w % tiles (64 W
+// of them).  The waves after them write the zeros.
+template <class E, int W>
+__global__ void __launch_bounds__(256)
+embed_sum_kernel(EmbedParams p, const uint32_t* __restrict__ key, const uint32_t* __restrict__ pos,
+                 const E* __restrict__ dx, float* __restrict__ dt, int R, int pieces, int tiles) {
+    const int lane = threadIdx.x & 63;
+    const long w = blockIdx.x * 4L + (threadIdx.x >> 6);
+    const long sums = (long)pieces * tiles;
+    if (w >= sums) {
+        const uint32_t now = *p.epoch;
+        const long waves = gridDim.x * 4L - sums;
+        float zero[W] = {};
+        for (long v = w - sums; v < p.V; v += waves) {
+            if (p.stamp[v] == now) continue;
+            for (int c = lane * W; c < p.D; c += 64 * W) store_vec<float, W>(dt + v * p.D + c, zero);
+        }
+        return;
+    }
+    const int piece = (int)(w / tiles), c = (int)(w - (long)piece * tiles) * 64 * W + lane * W;
+    const int first = piece * R, n = min(R, p.N - first);
+    const bool on = c < p.D;
+    const uint32_t V = (uint32_t)p.V;
+    uint32_t k = V, q = 0;
+    if (lane < n) {
+        k = key[first + lane];
+        q = pos[first + lane];
+    }
+    const uint32_t before = piece > 0 ? key[first - 1] : V, after = first + n < p.N ? key[first + n] : V;
+    float acc[W] = {};
+    uint32_t cur = (uint32_t)__builtin_amdgcn_readlane((int)k, 0);
+    bool opened = before == cur;  // the token's places begin in an earlier piece
+
+    auto close = [&](bool goes_on) {
+        if (!on) return;
+        if (opened || goes_on) {
+            store_vec<float, W>(p.part + ((long)piece * 2 + (opened ? 0 : 1)) * p.D + c, acc);
+        } else {
+            float o[W];
+#pragma unroll
+            for (int i = 0; i < W; ++i) o[i] = acc[i] * p.scale;
+            store_vec<float, W>(dt + (long)cur * p.D + c, o);
+        }
+    };
+    constexpr int U = 8;  // rows in flight
+    for (int i0 = 0; i0 < n && cur != V; i0 += U) {
+        float row[U][W];
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const int i = min(i0 + j, n - 1);
+            const uint32_t r = (uint32_t)__builtin_amdgcn_readlane((int)q, i);
+            if (on) load_vec<E, W>(dx + (long)r * p.D + c, row[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            if (i0 + j >= n || cur == V) break;
+            const uint32_t kj = (uint32_t)__builtin_amdgcn_readlane((int)k, i0 + j);
+            if (kj != cur) {
+                close(false);
+                cur = kj;
+                opened = false;
+#pragma unroll
+                for (int i = 0; i < W; ++i) acc[i] = 0.0f;
+                if (cur == V) break;
+            }
+#pragma unroll
+            for (int i = 0; i < W; ++i) acc[i] += row[j][i];
+        }
+    }
+    if (cur != V) close(after == cur);
+}
+
+// The tokens whose places span pieces: one workgroup per piece in which such
+// a token begins and per column tile, its waves a run of the partial sums each.
+template <int W>
+__global__ void __launch_bounds__(256)
+embed_join_kernel(EmbedParams p, const uint32_t* __restrict__ key, float* __restrict__ dt, int R,
+                  int pieces) {
+    __shared__ float sum[4][64 * W];
+    const int piece = blockIdx.x, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int c = blockIdx.y * 64 * W + lane * W;
+    const int end = (piece + 1) * R;
+    const uint32_t v = end < p.N ? key[end] : (uint32_t)p.V;
+    if (v == (uint32_t)p.V || key[end - 1] != v) return;
+    if (piece > 0 && key[piece * R] == v && key[piece * R - 1] == v) return;  // begins earlier
+    // the last piece with a place of v: whole pieces 64 at a time
+    int last = piece + 1;
+    for (;;) {
+        const long at = (long)(last + lane + 1) * R;  // the place after piece last + lane
+        const unsigned long long goes = __ballot(at < p.N && key[min(at, (long)p.N - 1)] == v);
+        const int whole = goes == ~0ull ? 64 : __ffsll(~goes) - 1;
+        last += whole;
+        if (whole < 64) break;
+    }
+    const int parts = last - piece;  // in slot 0 of pieces piece + 1 .. last
+    const int per = (parts + 3) / 4, lo = min(parts, w * per), hi = min(parts, lo + per);
+    const bool on = c < p.D;
+    float acc[W] = {};
+    if (on) {
+        if (w == 0) load_vec<float, W>(p.part + ((long)piece * 2 + 1) * p.D + c, acc);
+#pragma unroll 8
+        for (int i = lo; i < hi; ++i) {
+            float q[W];
+            load_vec<float, W>(p.part + (long)(piece + 1 + i) * 2 * p.D + c, q);
+#pragma unroll
+            for (int j = 0; j < W; ++j) acc[j] += q[j];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < W; ++j) sum[w][lane * W + j] = acc[j];
+    __syncthreads();
+    if (w == 0 && on) {
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            float a = acc[j];
+            for (int i = 1; i < 4; ++i) a += sum[i][lane * W + j];
+            acc[j] = a * p.scale;
+        }
+        store_vec<float, W>(dt + (long)v * p.D + c, acc);
+    }
+}
+
+int check_embed_sizes(int B, int T, int V, int D, int dtype) {
+    if (B < 1 || T < 1 || V < 1 || D < 1 || !valid_dtype(dtype)) return LSTM_DYN_ERR_INVALID;
+    if ((long long)B * T >= 1LL << 30 || V >= 1 << 27 || D >= 1 << 21) return LSTM_DYN_ERR_UNSUPPORTED;
+    return LSTM_DYN_OK;
+}
+
+int check_embed_forward(int B, int T, int V, int D, int dtype, const int32_t* tokens,
+                        const int32_t* lengths, const void* table, const void* x) {
+    const long long e = dtype_bytes(dtype), N = (long long)B * T;
+    const Span s[] = {{tokens, 4 * N, 4, false}, {table, e * V * D, 16, false}, {x, e * N * D, 16, true},
+                      {lengths, 4LL * B, 4, false}};
+    return check_spans(s, lengths ? 4 : 3);
+}
+
+int check_embed_backward(int B, int T, int V, int D, const int32_t* tokens, const int32_t* lengths,
+                         const void* dx, int dx_dtype, const float* dt) {
+    if (!valid_dtype(dx_dtype)) return LSTM_DYN_ERR_INVALID;
+    const long long N = (long long)B * T;
+    const Span s[] = {{tokens, 4 * N, 4, false}, {dx, dtype_bytes(dx_dtype) * N * D, 16, false},
+                      {dt, 4LL * V * D, 16, true}, {lengths, 4LL * B, 4, false}};
+    return check_spans(s, lengths ? 4 : 3);
+}
+
+inline long long up256(long long n) { return (n + 255) / 256 * 256; }
+
+}  // namespace
+}  // namespace ldyn
+
+using namespace ldyn;
+
+struct lstm_dyn_embed : OpsHandle {
+    int B, T, V, D, dtype;
+    int N, passes, bits, blocks, R, pieces;
+    uint32_t *epoch, *stamp, *hist, *key[2], *pos[2];
+    float* part;
+};
+
+extern "C" int lstm_dyn_check_embed_args(int B, int T, int V, int D, int dtype,
+                                         const int32_t* tokens, const int32_t* lengths,
+                                         const void* table, const void* out_x, const void* dx,
+                                         int dx_dtype, const float* d_table) {
+    const int rc = check_embed_sizes(B, T, V, D, dtype);
+    if (rc != LSTM_DYN_OK) return rc;
+    if (!dx && !d_table) return check_embed_forward(B, T, V, D, dtype, tokens, lengths, table, out_x);
+    return check_embed_backward(B, T, V, D, tokens, lengths, dx, dx_dtype, d_table);
+}
+
+extern "C" int lstm_dyn_embed_create(lstm_dyn_embed_t** out, int B, int T, int V, int D, int dtype) {
+    if (!out) return LSTM_DYN_ERR_INVALID;
+    *out = nullptr;
+    int rc = check_embed_sizes(B, T, V, D, dtype);
+    if (rc != LSTM_DYN_OK) return rc;
+    lstm_dyn_embed* h = new (std::nothrow) lstm_dyn_embed();
+    if (!h) return LSTM_DYN_ERR_NOMEM;
+    h->B = B; h->T = T; h->V = V; h->D = D; h->dtype = dtype;
+    const long long N = (long long)B * T;
+    h->N = (int)N;
+    int bits = 1;
+    while ((1LL << bits) < (long long)V + 1) ++bits;
+    h->passes = (bits + SORT_BITS - 1) / SORT_BITS;
+    h->bits = (bits + h->passes - 1) / h->passes;
+    h->blocks = (int)((N + SORT_TILE - 1) / SORT_TILE);
+    h->R = 64;
+    h->pieces = (int)((N + h->R - 1) / h->R);
+    long long at = 256;
+    auto take = [&](long long n) {
+        const long long o = at;
+        at += up256(n);
+        return o;
+    };
+    const long long o_epoch = take(4), o_stamp = take(4LL * V), o_hist = take(4LL * h->blocks << h->bits);
+    long long o_key[2], o_pos[2];
+    for (int i = 0; i < 2; ++i) o_key[i] = take(4 * N), o_pos[i] = take(4 * N);
+    const long long o_part = take(8LL * h->pieces * D);
+    if ((rc = ops_init(h, at)) != LSTM_DYN_OK) {
+        delete h;
+        return rc;
+    }
+    auto u32 = [&](long long o) { return reinterpret_cast<uint32_t*>(h->block + o); };
+    h->epoch = u32(o_epoch); h->stamp = u32(o_stamp); h->hist = u32(o_hist);
+    for (int i = 0; i < 2; ++i) h->key[i] = u32(o_key[i]), h->pos[i] = u32(o_pos[i]);
+    h->part = reinterpret_cast<float*>(h->block + o_part);
+    *out = h;
+    return LSTM_DYN_OK;
+}
+
+static EmbedParams embed_params(const lstm_dyn_embed* h, const int32_t* tokens,
+                                const int32_t* lengths, float scale) {
+    return EmbedParams{tokens, lengths, h->status(), h->epoch, h->stamp, h->hist, h->part,
+                       h->N, h->T, h->V, h->D, scale};
+}
+
+extern "C" int lstm_dyn_embed_forward(lstm_dyn_embed_t* h, const int32_t* tokens,
+                                      const int32_t* lengths, const void* table, float scale,
+                                      void* out_x, void* stream) {
+    if (!h) return LSTM_DYN_ERR_INVALID;
+    int rc = check_embed_forward(h->B, h->T, h->V, h->D, h->dtype, tokens, lengths, table, out_x);
+    if (rc != LSTM_DYN_OK) return rc;
+    if ((rc = ops_begin(h, stream)) != LSTM_DYN_OK) return rc;
+    const EmbedParams p = embed_params(h, tokens, lengths, scale);
+    long grid = ((long)h->N + 3) / 4;
+    if (grid > 16L * h->num_cus) grid = 16L * h->num_cus;
+#define LDYN_EMB(E, W)                                                                              \
+    hipLaunchKernelGGL((embed_forward_kernel<E, W>), dim3((unsigned)grid), dim3(256), 0,            \
+                       h->last_stream, p, static_cast<const E*>(table), static_cast<E*>(out_x))
+    if (h->dtype == LSTM_DYN_BF16) {
+        if (h->D % 8 == 0) LDYN_EMB(__bf16, 8);
+        else if (h->D % 2 == 0) LDYN_EMB(__bf16, 2);
+        else LDYN_EMB(__bf16, 1);
+    } else {
+        if (h->D % 4 == 0) LDYN_EMB(float, 4);
+        else LDYN_EMB(float, 1);
+    }
+#undef LDYN_EMB
+    return ops_launched(h);
+}
+
+extern "C" int lstm_dyn_embed_backward(lstm_dyn_embed_t* h, const int32_t* tokens,
+                                       const int32_t* lengths, const void* dx, int dx_dtype,
+                                       float scale, float* d_table, void* stream) {
+    if (!h) return LSTM_DYN_ERR_INVALID;
+    int rc = check_embed_backward(h->B, h->T, h->V, h->D, tokens, lengths, dx, dx_dtype, d_table);
+    if (rc != LSTM_DYN_OK) return rc;
+    if ((rc = ops_begin(h, stream)) != LSTM_DYN_OK) return rc;
+    const EmbedParams p = embed_params(h, tokens, lengths, scale);
+    int in = 0;
+    for (int i = 0; i < h->passes; ++i, in ^= 1) {
+        const SortPass s{i ? h->key[in] : nullptr, i ? h->pos[in] : nullptr, h->key[in ^ 1],
+                         h->pos[in ^ 1], i * h->bits, h->bits, h->blocks};
+        hipLaunchKernelGGL(sort_hist_kernel, dim3(h->blocks), dim3(SORT_THREADS), 0, h->last_stream, p, s);
+        if ((rc = ops_launched(h)) != LSTM_DYN_OK) return rc;
+        hipLaunchKernelGGL(sort_scatter_kernel, dim3(h->blocks), dim3(SORT_THREADS), 0, h->last_stream, p, s);
+        if ((rc = ops_launched(h)) != LSTM_DYN_OK) return rc;
+    }
+    const int W = h->D % 4 ? 1 : 4;
+    const int tiles = (h->D + 64 * W - 1) / (64 * W);
+    const long zero_waves = h->V < 8L * h->num_cus ? h->V : 8L * h->num_cus;
+    const long waves = (long)h->pieces * tiles + zero_waves;
+    const unsigned grid = (unsigned)((waves + 3) / 4);
+#define LDYN_SUM(E, W)                                                                              \
+    hipLaunchKernelGGL((embed_sum_kernel<E, W>), dim3(grid), dim3(256), 0, h->last_stream, p,       \
+                       h->key[in], h->pos[in], static_cast<const E*>(dx), d_table, h->R, h->pieces, \
+                       tiles)
+    if (dx_dtype == LSTM_DYN_BF16) {
+        if (W == 4) LDYN_SUM(__bf16, 4);
+        else LDYN_SUM(__bf16, 1);
+    } else {
+        if (W == 4) LDYN_SUM(float, 4);
+        else LDYN_SUM(float, 1);
+    }
+#undef LDYN_SUM
+    if ((rc = ops_launched(h)) != LSTM_DYN_OK || h->pieces < 2) return rc;
+    if (W == 4)
+        hipLaunchKernelGGL((embed_join_kernel<4>), dim3(h->pieces - 1, tiles), dim3(256), 0,
+                           h->last_stream, p, h->key[in], d_table, h->R, h->pieces);
+    else
+        hipLaunchKernelGGL((embed_join_kernel<1>), dim3(h->pieces - 1, tiles), dim3(256), 0,
+                           h->last_stream, p, h->key[in], d_table, h->R, h->pieces);
+    return ops_launched(h);
+}
+
+extern "C" int lstm_dyn_embed_query(lstm_dyn_embed_t* h, int what, long long* value) {
+    return ops_query(h, what, value);
+}
+
+extern "C" int lstm_dyn_embed_destroy(lstm_dyn_embed_t* h) {
+    if (!h) return LSTM_DYN_OK;
+    const int rc = ops_free(h);
+    delete h;
+    return rc;
+}

@@ -1,0 +1,242 @@
+"""The gated scan against its definition in 64 bits: lengths of 0, 1 and T, odd widths, long time
+axes (several workgroups a row), one step, in-place state, padding that holds NaN, extreme gates,
+streams, graph replay; its gradients against the formula's and against differences."""
+import numpy as np
+import pytest
+
+import paper_1810_08061_amd as ld
+from paper_1810_08061_amd import ops
+from tests import ops_util as ou
+from tests.gpu_util import say
+
+pytestmark = pytest.mark.gpu
+
+
+def _inputs(B, T, H, dtype, seed, lengths=None, poison=True):
+    import torch
+    g = torch.Generator().manual_seed(seed)
+    et = torch.bfloat16 if dtype == "bf16" else torch.float32
+    z = torch.randn((B, T, 3 * H), generator=g)
+    z[..., :H] += 1.0
+    z, dy = z.to(et), torch.randn((B, T, H), generator=g).to(et)
+    h0, dh = torch.randn((B, H), generator=g), torch.randn((B, H), generator=g)
+    if lengths is None:
+        lengths = torch.randint(0, T + 1, (B,), generator=g)
+        lengths[0] = T
+        if B > 2:
+            lengths[1], lengths[2] = 0, 1
+    L = torch.as_tensor(lengths, dtype=torch.int32)
+    ref = ou.scan(z.double().numpy(), L.numpy(), h0.double().numpy(), dy.double().numpy(), dh.double().numpy())
+    if poison:
+        past = torch.arange(T)[None, :] >= L[:, None]
+        z[past], dy[past] = float("nan"), float("inf")
+    return [t.cuda() for t in (z, L, h0, dy, dh)], ref
+
+
+def _close(name, got, want, tol, rel):
+    got = got.double().cpu().numpy()
+    err = np.abs(got - want)
+    assert np.isfinite(got).all(), name
+    worst = (err - (tol + rel * np.abs(want))).max(initial=-1.0)
+    say(f"{name}: max error {err.max(initial=0):.3g}, bound {tol:.3g} + {rel:.3g} |y|")
+    assert worst <= 0, (name, worst)
+
+
+def _run_and_check(m, dev, ref, dtype, grads=True):
+    z, L, h0, dy, dh = dev
+    tol, rel = ou.scan_bounds(ref["info"], dtype == "bf16")
+    y, h = m.forward(z, L, h0)
+    _close("y", y, ref["y"], tol["y"], rel)
+    _close("h", h, ref["h"], tol["h"], 0)
+    if not grads:
+        return
+    y2, h2 = m.forward_train(z, L, h0)
+    assert (y2 == y).all() and (h2 == h).all()
+    d = m.backward(z, L, h0, dy, dh)
+    _close("dz", d["dz"], ref["dz"], tol["dz"], rel)
+    _close("dh0", d["dh0"], ref["dh0"], tol["dh0"], 0)
+    assert m.status() == ld.OK
+
+
+# T around the sizes at which a run, a workgroup's share and several workgroups begin and end
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,T,H", [
+    (1, 1, 1), (3, 1, 5), (4, 2, 64), (3, 15, 33), (3, 16, 130), (5, 17, 62), (3, 31, 256), (2, 33, 12),
+    (2, 127, 36), (4, 128, 20), (3, 129, 66), (3, 255, 8), (2, 256, 260), (3, 257, 7), (2, 511, 96),
+    (2, 513, 34), (1, 1025, 64), (3, 2050, 3), (1, 4097, 130), (9, 300, 48), (70, 20, 128), (2, 700, 1030)])
+def test_scan(B, T, H, dtype):
+    dev, ref = _inputs(B, T, H, dtype, 1000 * T + H + B)
+    with ld.GatedScan(B, H, T, dtype) as m:
+        _run_and_check(m, dev, ref, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lengths", [[0, 0, 0], [1, 0, 0], [600, 600, 600], [1, 599, 256], [16, 17, 512]])
+def test_lengths(lengths, dtype):
+    dev, ref = _inputs(3, 600, 40, dtype, sum(lengths), lengths)
+    with ld.GatedScan(3, 40, 600, dtype) as m:
+        _run_and_check(m, dev, ref, dtype)
+        y, h = m.forward(*dev[:3])
+        for b, L in enumerate(lengths):
+            assert (y[b, L:] == 0).all()
+            if L == 0:
+                assert (h[b] == dev[2][b]).all()      # the state comes back bit for bit
+
+
+def test_bad_lengths_are_clamped_and_reported():
+    dev, ref = _inputs(4, 50, 24, "f32", 5, [50, 0, 7, 50], poison=False)
+    z, L, h0, dy, dh = dev
+    with ld.GatedScan(4, 24, 50, "f32") as m:
+        y, h = m.forward(z, L, h0)
+        bad = L.clone()
+        bad[0], bad[1], bad[3] = 51, -3, 2 ** 31 - 1
+        assert m.status() == ld.OK
+        y2, h2 = m.forward_train(z, bad, h0)
+        assert m.status() == ld.ERR_BAD_LENGTHS and m.status() == ld.OK
+        assert (y == y2).all() and (h == h2).all()
+        d = m.backward(z, bad, h0, dy, dh)
+        assert m.status() == ld.ERR_BAD_LENGTHS
+        m.forward_train(z, L, h0)
+        d2 = m.backward(z, L, h0, dy, dh)
+        assert all((d[k] == d2[k]).all() for k in d)
+
+
+def test_extreme_gates():
+    """Gates at which the sigmoid is 0 or 1 to every bit: memories that last, and resets."""
+    import torch
+    B, T, H = 2, 700, 24
+    g = torch.Generator().manual_seed(3)
+    z = torch.randn((B, T, 3 * H), generator=g)
+    z[:, :, :8] = 40.0                                     # a = 1: h0 stays
+    z[:, :, 8:16] = torch.where(torch.rand((B, T, 8), generator=g) < 0.5, 200.0, -200.0)
+    z[:, ::3, 16:20] = -float("inf")                       # reset
+    z[:, ::5, 20:24] = float("inf")                        # kept
+    z[:, ::7, 2 * H:] = -float("inf")                      # closed output
+    h0, L = torch.randn((B, H), generator=g), torch.tensor([T, T - 1], dtype=torch.int32)
+    dy, dh = torch.randn((B, T, H), generator=g), torch.randn((B, H), generator=g)
+    ref = ou.scan(z.double().numpy(), L.numpy(), h0.double().numpy(), dy.double().numpy(), dh.double().numpy())
+    with ld.GatedScan(B, H, T, "f32") as m:
+        _run_and_check(m, [t.cuda() for t in (z, L, h0, dy, dh)], ref, "f32")
+
+
+def test_a_nan_stays_in_its_channel():
+    dev, ref = _inputs(2, 600, 16, "f32", 9, [600, 600])
+    z, L, h0 = dev[:3]
+    with ld.GatedScan(2, 16, 600, "f32") as m:
+        y0, h0_ = m.forward(z, L, h0)
+        z[0, 300, 3] = float("nan")                        # one forget gate
+        y, h = m.forward(z, L, h0)
+        assert y[0, 300:, 3].isnan().all() and h[0, 3].isnan()
+        y[0, 300:, 3], h[0, 3] = y0[0, 300:, 3], h0_[0, 3]
+        assert (y == y0).all() and (h == h0_).all()
+
+
+def test_without_the_states_gradient_and_in_place():
+    dev, _ = _inputs(3, 290, 20, "bf16", 11)
+    z, L, h0, dy, dh = dev
+    with ld.GatedScan(3, 20, 290, "bf16") as m:
+        m.forward_train(z, L, h0)
+        d = m.backward(z, L, h0, dy)
+        m.forward_train(z, L, h0)
+        d0 = m.backward(z, L, h0, dy, dh * 0)
+        assert all((d[k] == d0[k]).all() for k in d)
+        y, h = m.forward(z, L, h0)
+        state = h0.clone()
+        y2, h2 = m.forward(z, L, state, out_h=state)
+        assert h2 is state and (h2 == h).all() and (y2 == y).all()
+
+
+def test_backward_needs_a_forward_for_training():
+    dev, _ = _inputs(2, 9, 8, "f32", 2)
+    z, L, h0, dy, dh = dev
+    with ld.GatedScan(2, 8, 9, "f32") as m:
+        for prepare in (lambda: None, lambda: m.forward(z, L, h0),
+                        lambda: (m.forward_train(z, L, h0), m.backward(z, L, h0, dy, dh)),
+                        lambda: (m.forward_train(z, L, h0), m.forward(z, L, h0))):
+            prepare()
+            with pytest.raises(ld.LstmDynError) as e:
+                m.backward(z, L, h0, dy, dh)
+            assert e.value.code == ld.ERR_INVALID
+        with pytest.raises(ld.LstmDynError):
+            m.forward_train(z, L, h0, out_h=h0)
+        with pytest.raises(TypeError):
+            m.forward(z.bfloat16(), L, h0)
+        with pytest.raises(ValueError):
+            m.forward(z[:, :8], L, h0)
+        with pytest.raises(ValueError):
+            m.forward(z, L, h0.t().contiguous().t())
+        with pytest.raises(TypeError):
+            m.forward(z, L.long(), h0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("R,H", [(1, 1), (1, 512), (7, 33), (3, 64), (65, 18), (300, 20)])
+def test_step(R, H, dtype):
+    """One step is a sequence of length one, and a chain of them the whole sequence."""
+    import torch
+    dev, ref = _inputs(R, 3, H, dtype, R + H, [3] * R)
+    z, L, h0 = dev[:3]
+    tol, rel = ou.scan_bounds(ref["info"], dtype == "bf16")
+    with ld.GatedScan(R, H, 3, dtype) as m:
+        h, ys = h0.clone(), []
+        for t in range(3):
+            y, h2 = m.step(z[:, t].contiguous(), h, out_h=h if t else None)
+            h = h2
+            ys.append(y)
+        _close("y", torch.stack(ys, 1), ref["y"], tol["y"], rel)
+        _close("h", h, ref["h"], tol["h"], 0)
+
+
+def test_gradients_against_differences():
+    """Central differences of the loss through the kernels' own forward, along random directions."""
+    import torch
+    B, T, H = 3, 270, 10
+    dev, _ = _inputs(B, T, H, "f32", 21, [270, 130, 1], poison=False)
+    z, L, h0, dy, dh = dev
+    with ld.GatedScan(B, H, T, "f32") as m:
+        def loss(z, h0):
+            y, h = m.forward(z, L, h0)
+            return float((y.double() * dy.double()).sum() + (h.double() * dh.double()).sum())
+        m.forward_train(z, L, h0)
+        d = m.backward(z, L, h0, dy, dh)
+        g = torch.Generator(device="cuda").manual_seed(1)
+        eps = 2.0 ** -7
+        for _ in range(4):
+            vz, vh = (torch.empty_like(t).normal_(generator=g) for t in (z, h0))
+            want = float((d["dz"].double() * vz).sum() + (d["dh0"].double() * vh).sum())
+            got = (loss(z + eps * vz, h0 + eps * vh) - loss(z - eps * vz, h0 - eps * vh)) / (2 * eps)
+            # third derivatives: eps^2 of a loss of about 10^4 terms of size one; rounding: 1e-6 of it over eps
+            size = float(dy.abs().sum() + dh.abs().sum())
+            say(f"directional derivative {want:.6g}, by differences {got:.6g}")
+            assert abs(got - want) <= size * (eps ** 2 + 1e-6 / eps)
+
+
+def test_two_streams_and_graph_replay():
+    import torch
+    dev, _ = _inputs(4, 530, 72, "bf16", 31)
+    z, L, h0, dy, dh = dev
+    with ld.GatedScan(4, 72, 530, "bf16") as m, ld.GatedScan(4, 72, 530, "bf16") as m2:
+        y, h = m.forward_train(z, L, h0)
+        d = m.backward(z, L, h0, dy, dh)
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            y2, h2 = m2.forward_train(z, L, h0)
+            d2 = m2.backward(z, L, h0, dy, dh)
+        s.synchronize()
+        assert (y == y2).all() and (h == h2).all() and all((d[k] == d2[k]).all() for k in d)
+        zs = z.clone()
+        out = {"dz": torch.empty_like(z), "dh0": torch.empty_like(h0)}
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            yg, hg = m.forward_train(zs, L, h0)
+            m.backward(zs, L, h0, dy, dh, out=out)
+        for i in range(4):
+            zs.copy_(z * (1 - 0.1 * i))
+            graph.replay()
+            torch.cuda.synchronize()
+            ye, he = m2.forward_train(zs, L, h0)
+            de = m2.backward(zs, L, h0, dy, dh)
+            assert (yg == ye).all() and (hg == he).all() and all((out[k] == de[k]).all() for k in out), i
+            torch.cuda.synchronize()
+        assert m.status() == ld.OK
