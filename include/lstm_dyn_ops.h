@@ -60,7 +60,7 @@ enum {
  * where it is infinite step by step. */
 typedef struct lstm_dyn_scan lstm_dyn_scan_t;
 
-/* B, H, T_max >= 1, B * T_max < 2^31, H < 2^24. */
+/* B, H, T_max >= 1, B * T_max < 2^31, H < 2^18. */
 int lstm_dyn_scan_create(lstm_dyn_scan_t** out, int B, int H, int T_max, int dtype);
 
 int lstm_dyn_scan_forward(lstm_dyn_scan_t* h, const void* z, const int32_t* lengths,

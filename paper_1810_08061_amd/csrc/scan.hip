@@ -19,6 +19,11 @@ namespace {
 template <class E>
 constexpr int run_of() { return sizeof(E) == 2 ? 16 : 8; }
 
+// The largest workgroups.  The backward holds 160 registers a thread with bf16
+// data, so three waves a SIMD: workgroups of 256 (0.63 ms for 32 x 4096 x 2048;
+// of 512 it spills, 0.79 ms).
+constexpr int FWD_THREADS = 512, BWD_THREADS = 256;
+
 struct ScanParams {
     const void* z;
     const int32_t* lengths;
@@ -33,7 +38,7 @@ struct ScanParams {
     int32_t* status;
     int B, T, H;
     int tiles, segs;      // column tiles of a row; shares of its steps
-    unsigned* counters;   // [0] the next item, [1] items done, [2] launches done
+    unsigned long long* counters;  // [B tiles] shares taken, over all launches
     uint64_t* carry;      // [B][segs][H] {value, launch} a share passes on
     unsigned long long timeout_ticks;
 };
@@ -41,45 +46,78 @@ struct ScanParams {
 // 1 / (1 + e^x), which is 1 and 0 at the infinities.
 __device__ inline float logistic_neg(float x) { return rcp_f(1.0f + __expf(x)); }
 
-// V elements as they lie in memory.
+// V elements as they lie in memory, in 32-bit words.
 template <class E, int V>
-using raw_t = typename Vec<E, V>::type;
+struct Raw {
+    static constexpr int N = sizeof(E) * V <= 4 ? 1 : 2;
+    uint32_t w[N];
+
+    __device__ float operator[](int i) const {
+        if constexpr (sizeof(E) == 4) return __uint_as_float(w[i]);
+        else return __uint_as_float(i ? w[0] & 0xffff0000u : w[0] << 16);
+    }
+    // The compiler may not form anything of this before here (a bf16 pair widened early takes
+    // twice the registers).
+    __device__ void hold() {
+#pragma unroll
+        for (int i = 0; i < N; ++i) asm volatile("" : "+v"(w[i]));
+    }
+};
+
+// Memory at a scalar base and a lane's own offset of 32 bits.
 template <class E, int V>
-__device__ inline float elem(const raw_t<E, V>& x, int i) {
-    if constexpr (V == 1) return (float)x;
-    else return (float)x[i];
+__device__ inline Raw<E, V> load_raw(const E* base, unsigned off) {
+    const char* q = reinterpret_cast<const char*>(base) + off;
+    Raw<E, V> x;
+    if constexpr (sizeof(E) * V == 2) {
+        x.w[0] = *reinterpret_cast<const uint16_t*>(q);
+    } else if constexpr (sizeof(E) * V == 4) {
+        x.w[0] = *reinterpret_cast<const uint32_t*>(q);
+    } else {
+        const uint2 u = *reinterpret_cast<const uint2*>(q);
+        x.w[0] = u.x;
+        x.w[1] = u.y;
+    }
+    return x;
+}
+template <class E, int V>
+__device__ inline void store_at(E* base, unsigned off, const float* x) {
+    store_vec<E, V>(reinterpret_cast<E*>(reinterpret_cast<char*>(base) + off), x);
 }
 
-// Which share of which row and columns this workgroup takes.  Shares come in
-// the order of their dependence, by a counter, so that one whose turn it is only
-// ever waits for workgroups that have started: no residency is assumed.
+// Which share of which row and columns this workgroup takes.  The shares of one
+// row and tile are a chain, in the order of their dependence.  A workgroup's
+// number names its chain; which share, the chain's counter: a workgroup then
+// only ever waits for one that has started, whatever order they are started
+// in.  Every launch takes each chain's shares once, so the counter also numbers
+// the launches, and nothing is cleared between them.  (One counter for all
+// chains: an atomic on one address takes 40 ns, 0.33 ms for 4096 shares.)
 struct Item {
     int b, tile, seg;
+    unsigned launch;
 };
-__device__ inline Item take_item(const ScanParams& p, bool last_first, unsigned* lds) {
-    unsigned n = blockIdx.x;
-    if (p.segs > 1) {
-        if (threadIdx.x == 0) *lds = atomicAdd(p.counters, 1u);
-        __syncthreads();
-        n = *lds;
-    }
-    const unsigned per = (unsigned)p.B * p.tiles, seg = n / per, rest = n - seg * per;
+constexpr int COUNTER_WORDS = 8;  // a counter per 64 bytes
+__device__ inline Item take_item(const ScanParams& p, bool last_first, unsigned (*lds)[2]) {
+    const unsigned chains = (unsigned)p.B * p.tiles;
     Item it;
-    it.b = (int)(rest / p.tiles);
-    it.tile = (int)(rest - (unsigned)it.b * p.tiles);
+    unsigned chain = blockIdx.x, seg = 0;
+    it.launch = 0;
+    if (p.segs > 1) {
+        chain = blockIdx.x % chains;
+        if (threadIdx.x == 0) {
+            const unsigned long long n = atomicAdd(p.counters + (long)chain * COUNTER_WORDS, 1ull);
+            const unsigned long long l = n >> 32 ? n / (unsigned)p.segs : (unsigned)n / (unsigned)p.segs;
+            (*lds)[0] = (unsigned)(n - l * (unsigned)p.segs);
+            (*lds)[1] = (unsigned)l + 1;
+        }
+        __syncthreads();
+        seg = (unsigned)__builtin_amdgcn_readfirstlane((int)(*lds)[0]);  // scalar addresses
+        it.launch = (unsigned)__builtin_amdgcn_readfirstlane((int)(*lds)[1]);
+    }
+    it.b = (int)(chain / p.tiles);
+    it.tile = (int)(chain - (unsigned)it.b * p.tiles);
     it.seg = last_first ? p.segs - 1 - (int)seg : (int)seg;
     return it;
-}
-
-// The last workgroup to end makes the counters ready for the next launch.
-__device__ inline void end_item(const ScanParams& p) {
-    if (p.segs > 1 && threadIdx.x == 0) {
-        if (atomicAdd(p.counters + 1, 1u) == gridDim.x - 1) {
-            __hip_atomic_store(p.counters, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            __hip_atomic_store(p.counters + 1, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            __hip_atomic_fetch_add(p.counters + 2, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
-    }
 }
 
 // A value and the launch it belongs to in one word: no flag beside it, and
@@ -189,198 +227,179 @@ __device__ inline void join_runs(float* A, float* S, float* total_A, float* tota
     }
 }
 
+// What a workgroup's threads know of their place.
 template <class E, int V, int NT, int CL>
-__global__ void __launch_bounds__(NT) scan_forward_kernel(ScanParams p) {
-    constexpr int R = run_of<E>(), G = NT / CL, NW = NT / 64;
-    __shared__ unsigned turn;
-    __shared__ float maps[NW][2][CL * V];
-    __shared__ float start[CL * V];
-    const Item it = take_item(p, false, &turn);
-    const int H = p.H, T = p.T, cl = threadIdx.x % CL, g = threadIdx.x / CL;
-    const int ch = (it.tile * CL + cl) * V;
-    const bool on = ch < H;
-    const int c = on ? ch : 0;
-    const int L = row_length(p.lengths, it.b, T, p.status, it.tile == 0 && it.seg == 0 && threadIdx.x == 0);
-    const int t0 = (it.seg * G + g) * R, first = it.seg * G * R;
-    E* y = static_cast<E*>(p.y) + ((long)it.b * T + t0) * H + c;
-    const unsigned launch = p.segs > 1 ? p.counters[2] + 1 : 0;
-    const long row = (long)it.b * H + c;
+struct Place {
+    static constexpr int R = run_of<E>(), G = NT / CL;
+    int b, seg, cl, g, c, t0, first, L;
+    unsigned launch;
+    bool on, full;
+    unsigned zoff, yoff;  // bytes from the share's first step to this thread's
 
-    if (first >= L && !(first == 0)) {  // a share past the row's end
-        float zero[V] = {};
-        if (on)
-            for (int r = 0; r < R && t0 + r < T; ++r) store_vec<E, V>(y + (long)r * H, zero);
-        end_item(p);
-        return;
+    __device__ Place(const ScanParams& p, const Item& it)
+        : b(it.b), seg(it.seg), cl(threadIdx.x % CL), g(threadIdx.x / CL), launch(it.launch) {
+        const int ch = (it.tile * CL + cl) * V;
+        on = ch < p.H;
+        c = on ? ch : 0;
+        first = seg * G * R;
+        t0 = first + g * R;
+        L = row_length(p.lengths, b, p.T, p.status, it.tile == 0 && seg == 0 && threadIdx.x == 0);
+        full = first + G * R <= L;
+        zoff = ((unsigned)(g * R * 3) * p.H + c) * sizeof(E);
+        yoff = ((unsigned)(g * R) * p.H + c) * sizeof(E);
     }
+    __device__ long step0(const ScanParams& p) const { return (long)b * p.T + first; }
+};
+
+// The steps of a share.  WHOLE: all of them are valid, so loads and selects
+// depend on nothing; written out apart, because where the two ways would meet
+// the compiler waits for every load.
+template <bool WHOLE, class E, int V, int NT, int CL>
+__device__ inline void forward_share(const ScanParams& p, const Place<E, V, NT, CL>& at,
+                                     float (*maps)[2][CL * V], float* start) {
+    constexpr int R = run_of<E>(), G = NT / CL;
+    const int H = p.H, L = at.L, t0 = at.t0;
+    const unsigned launch = at.launch;
+    const long row = (long)at.b * H + at.c;
+    const E* z = static_cast<const E*>(p.z) + at.step0(p) * 3 * H;
+    E* y = static_cast<E*>(p.y) + at.step0(p) * H;
     float k[R][V], A[V], S[V];
-    raw_t<E, V> v[R], o[R];
-    const bool full = first + G * R <= L;
-    if (L > 0) {
-        // steps past the end read the last valid one, and are left out below
-        const E* z = static_cast<const E*>(p.z) + (long)it.b * T * 3 * H + c;
-        raw_t<E, V> f[R];
+    Raw<E, V> f[R], v[R], o[R];
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const E* q = z + (long)min(t0 + r, L - 1) * 3 * H;
-            f[r] = *reinterpret_cast<const raw_t<E, V>*>(q);
-            v[r] = *reinterpret_cast<const raw_t<E, V>*>(q + H);
+    for (int r = 0; r < R; ++r) {
+        if (!WHOLE) f[r] = v[r] = Raw<E, V>{};
+        if (WHOLE || t0 + r < L) {
+            f[r] = load_raw<E, V>(z + (long)r * 3 * H, at.zoff);
+            v[r] = load_raw<E, V>(z + (long)r * 3 * H + H, at.zoff);
         }
+    }
 #pragma unroll
-        for (int r = 0; r < R; ++r)
-            o[r] = *reinterpret_cast<const raw_t<E, V>*>(z + (long)min(t0 + r, L - 1) * 3 * H + 2 * H);
+    for (int r = 0; r < R; ++r) {
+        if (!WHOLE) o[r] = Raw<E, V>{};
+        if (WHOLE || t0 + r < L) o[r] = load_raw<E, V>(z + (long)r * 3 * H + 2 * H, at.zoff);
+    }
 #pragma unroll
-        for (int i = 0; i < V; ++i) A[i] = 1.0f, S[i] = 0.0f;
-        auto maps_of = [&](auto whole) {
+    for (int i = 0; i < V; ++i) A[i] = 1.0f, S[i] = 0.0f;
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
+    for (int r = 0; r < R; ++r) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    k[r][i] = logistic_neg(elem<E, V>(f[r], i));
-                    const float s = fmaf(k[r][i], elem<E, V>(v[r], i) - S[i], S[i]);
-                    const float a = fmaf(-k[r][i], A[i], A[i]);
-                    if (whole.value || t0 + r < L) S[i] = s, A[i] = a;
-                }
-            }
-        };
-        if (full) maps_of(std::true_type{});
-        else maps_of(std::false_type{});
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i) A[i] = 1.0f, S[i] = 0.0f;
+        for (int i = 0; i < V; ++i) {
+            k[r][i] = logistic_neg(f[r][i]);
+            const float s = fmaf(k[r][i], v[r][i] - S[i], S[i]);
+            const float a = fmaf(-k[r][i], A[i], A[i]);
+            if (WHOLE || t0 + r < L) S[i] = s, A[i] = a;
+        }
     }
     float tA[V], tS[V], h[V] = {};
     join_runs<V, NT, CL, false>(A, S, tA, tS, maps);
-    if (threadIdx.x < CL) {
-        uint64_t* w = p.carry + ((long)it.b * p.segs + it.seg) * H + c;
-        if (it.seg == 0) {
+    if (threadIdx.x < CL && at.on) {
+        uint64_t* w = p.carry + ((long)at.b * p.segs + at.seg) * H + at.c;
+        if (at.seg == 0) {
 #pragma unroll
             for (int i = 0; i < V; ++i) h[i] = p.h0[row + i];
-        } else if (on) {
+        } else {
             await<V>(p, w - H, h, launch);
         }
         float e[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            start[cl * V + i] = h[i];
-            e[i] = fmaf(tA[i], h[i], tS[i]);
-            if (L == 0) e[i] = h[i];
+            start[at.cl * V + i] = h[i];
+            e[i] = L == 0 ? h[i] : fmaf(tA[i], h[i], tS[i]);
         }
-        if (on) {
-            if (first + G * R < L) {
-                publish<V>(w, e, launch);
-            } else {
+        if (at.first + G * R < L) {
+            publish<V>(w, e, launch);
+        } else {
 #pragma unroll
-                for (int i = 0; i < V; ++i) p.out_h[row + i] = e[i];
-            }
+            for (int i = 0; i < V; ++i) p.out_h[row + i] = e[i];
         }
     }
     __syncthreads();
+    if (!at.on) return;
 #pragma unroll
-    for (int i = 0; i < V; ++i) h[i] = fmaf(A[i], start[cl * V + i], S[i]);
-    if (on) {
-        if (p.kept && t0 < L) {
-            float* kp = p.kept + ((long)it.b * ((T + R - 1) / R) + t0 / R) * H + c;
+    for (int r = 0; r < R; ++r) v[r].hold(), o[r].hold();
 #pragma unroll
-            for (int i = 0; i < V; ++i) kp[i] = h[i];
-        }
-        auto steps = [&](auto whole) {
+    for (int i = 0; i < V; ++i) h[i] = fmaf(A[i], start[at.cl * V + i], S[i]);
+    if (p.kept && t0 < L) {
+        float* kp = p.kept + ((long)at.b * ((p.T + R - 1) / R) + t0 / R) * H + at.c;
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                float out[V];
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    h[i] = fmaf(k[r][i], elem<E, V>(v[r], i) - h[i], h[i]);
-                    out[i] = logistic_neg(-elem<E, V>(o[r], i)) * h[i];
-                    if (!whole.value && t0 + r >= L) out[i] = 0.0f;
-                }
-                if (whole.value || t0 + r < T) store_vec<E, V>(y + (long)r * H, out);
-            }
-        };
-        if (full) {
-            steps(std::true_type{});
-        } else if (L > 0) {
-            steps(std::false_type{});
-        } else {
-            float zero[V] = {};
-            for (int r = 0; r < R && t0 + r < T; ++r) store_vec<E, V>(y + (long)r * H, zero);
-        }
+        for (int i = 0; i < V; ++i) kp[i] = h[i];
     }
-    end_item(p);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        float out[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            h[i] = fmaf(k[r][i], v[r][i] - h[i], h[i]);
+            out[i] = logistic_neg(-o[r][i]) * h[i];
+            if (!WHOLE && t0 + r >= L) out[i] = 0.0f;
+        }
+        if (WHOLE || t0 + r < p.T) store_at<E, V>(y + (long)r * H, at.yoff, out);
+    }
 }
 
 template <class E, int V, int NT, int CL>
-__global__ void __launch_bounds__(NT) scan_backward_kernel(ScanParams p) {
-    constexpr int R = run_of<E>(), G = NT / CL, NW = NT / 64;
-    __shared__ unsigned turn;
+__global__ void __launch_bounds__(NT, 4) scan_forward_kernel(ScanParams p) {
+    constexpr int R = run_of<E>(), NW = NT / 64;
+    __shared__ unsigned turn[1][2];
     __shared__ float maps[NW][2][CL * V];
     __shared__ float start[CL * V];
-    const Item it = take_item(p, true, &turn);
-    const int H = p.H, T = p.T, cl = threadIdx.x % CL, g = threadIdx.x / CL;
-    const int ch = (it.tile * CL + cl) * V;
-    const bool on = ch < H;
-    const int c = on ? ch : 0;
-    const int L = row_length(p.lengths, it.b, T, p.status, it.tile == 0 && it.seg == 0 && threadIdx.x == 0);
-    const int t0 = (it.seg * G + g) * R, first = it.seg * G * R;
-    E* dz = static_cast<E*>(p.dz) + ((long)it.b * T + t0) * 3 * H + c;
-    const unsigned launch = p.segs > 1 ? p.counters[2] + 1 : 0;
-    const long row = (long)it.b * H + c;
-
-    if (first >= L) {  // a share past the row's end
+    const Place<E, V, NT, CL> at(p, take_item(p, false, turn));
+    if (at.full) {
+        forward_share<true, E, V, NT, CL>(p, at, maps, start);
+    } else if (at.first < at.L || at.first == 0) {
+        forward_share<false, E, V, NT, CL>(p, at, maps, start);
+    } else if (at.on) {  // past the row's end
+        E* y = static_cast<E*>(p.y) + at.step0(p) * p.H;
         float zero[V] = {};
-        if (on) {
-            for (int r = 0; r < R && t0 + r < T; ++r)
-#pragma unroll
-                for (int j = 0; j < 3; ++j) store_vec<E, V>(dz + ((long)r * 3 + j) * H, zero);
-            if (L == 0 && first == 0 && g == 0) {
-#pragma unroll
-                for (int i = 0; i < V; ++i) p.dh0[row + i] = p.d_out_h ? p.d_out_h[row + i] : 0.0f;
-            }
-        }
-        end_item(p);
-        return;
+        for (int r = 0; r < R && at.t0 + r < p.T; ++r) store_at<E, V>(y + (long)r * p.H, at.yoff, zero);
     }
-    const bool full = first + G * R <= L;
+}
+
+template <bool WHOLE, class E, int V, int NT, int CL>
+__device__ inline void backward_share(const ScanParams& p, const Place<E, V, NT, CL>& at,
+                                      float (*maps)[2][CL * V], float* start) {
+    constexpr int R = run_of<E>(), G = NT / CL;
+    const int H = p.H, L = at.L, t0 = at.t0;
+    const unsigned launch = at.launch;
+    const long row = (long)at.b * H + at.c;
+    const E* z = static_cast<const E*>(p.z) + at.step0(p) * 3 * H;
+    const E* dy = static_cast<const E*>(p.dy) + at.step0(p) * H;
+    E* dz = static_cast<E*>(p.dz) + at.step0(p) * 3 * H;
     // per step: the gate's complement, s dy, and dzf's factor of g
-    float k[R][V], q[R][V], f[R][V], A[V], S[V];
-    {
-        const E* z = static_cast<const E*>(p.z) + (long)it.b * T * 3 * H + c;
-        const E* dy = static_cast<const E*>(p.dy) + (long)it.b * T * H + c;
-        raw_t<E, V> zf[R], zv[R], zo[R], zd[R];
-        float h[V];
-        const float* kp = p.kept + ((long)it.b * ((T + R - 1) / R) + min(t0, L - 1) / R) * H + c;
+    float k[R][V], q[R][V], f[R][V], A[V], S[V], h[V] = {};
+    Raw<E, V> zf[R], zv[R], zo[R], zd[R];
+    if (WHOLE || t0 < L) {
+        const float* kp = p.kept + ((long)at.b * ((p.T + R - 1) / R) + t0 / R) * H + at.c;
 #pragma unroll
         for (int i = 0; i < V; ++i) h[i] = kp[i];
+    }
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const long t = min(t0 + r, L - 1);
-            zf[r] = *reinterpret_cast<const raw_t<E, V>*>(z + t * 3 * H);
-            zv[r] = *reinterpret_cast<const raw_t<E, V>*>(z + t * 3 * H + H);
-            zo[r] = *reinterpret_cast<const raw_t<E, V>*>(z + t * 3 * H + 2 * H);
-            zd[r] = *reinterpret_cast<const raw_t<E, V>*>(dy + t * H);
+    for (int r = 0; r < R; ++r) {
+        if (!WHOLE) zf[r] = zv[r] = zo[r] = zd[r] = Raw<E, V>{};
+        if (WHOLE || t0 + r < L) {
+            zf[r] = load_raw<E, V>(z + (long)r * 3 * H, at.zoff);
+            zv[r] = load_raw<E, V>(z + (long)r * 3 * H + H, at.zoff);
+            zo[r] = load_raw<E, V>(z + (long)r * 3 * H + 2 * H, at.zoff);
+            zd[r] = load_raw<E, V>(dy + (long)r * H, at.yoff);
         }
-        auto again = [&](auto whole) {
+    }
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                float out[V];
-                const bool valid = whole.value || t0 + r < L;
+    for (int r = 0; r < R; ++r) {
+        float out[V];
+        const bool valid = WHOLE || t0 + r < L;
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float kk = logistic_neg(elem<E, V>(zf[r], i));
-                    const float s = logistic_neg(-elem<E, V>(zo[r], i));
-                    const float qq = s * elem<E, V>(zd[r], i);
-                    const float diff = elem<E, V>(zv[r], i) - h[i];
-                    h[i] = fmaf(kk, diff, h[i]);
-                    out[i] = valid ? qq * h[i] * (1.0f - s) : 0.0f;
-                    k[r][i] = valid ? kk : 0.0f;
-                    q[r][i] = valid ? qq : 0.0f;
-                    f[r][i] = -diff * kk * (1.0f - kk);
-                }
-                if (on && (whole.value || t0 + r < T)) store_vec<E, V>(dz + ((long)r * 3 + 2) * H, out);
-            }
-        };
-        if (full) again(std::true_type{});
-        else again(std::false_type{});
+        for (int i = 0; i < V; ++i) {
+            const float kk = logistic_neg(zf[r][i]);
+            const float s = logistic_neg(-zo[r][i]);
+            const float qq = s * zd[r][i];
+            const float diff = zv[r][i] - h[i];
+            h[i] = fmaf(kk, diff, h[i]);
+            out[i] = valid ? qq * h[i] * (1.0f - s) : 0.0f;
+            k[r][i] = valid ? kk : 0.0f;
+            q[r][i] = valid ? qq : 0.0f;
+            f[r][i] = -diff * kk * (1.0f - kk);
+        }
+        if (at.on && (WHOLE || t0 + r < p.T)) store_at<E, V>(dz + ((long)r * 3 + 2) * H, at.zoff, out);
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) A[i] = 1.0f, S[i] = 0.0f;
@@ -395,55 +414,72 @@ __global__ void __launch_bounds__(NT) scan_backward_kernel(ScanParams p) {
     }
     float tA[V], tS[V], e[V] = {};
     join_runs<V, NT, CL, true>(A, S, tA, tS, maps);
-    if (threadIdx.x < CL) {
-        uint64_t* w = p.carry + ((long)it.b * p.segs + it.seg) * H + c;
-        if (first + G * R >= L) {
+    if (threadIdx.x < CL && at.on) {
+        uint64_t* w = p.carry + ((long)at.b * p.segs + at.seg) * H + at.c;
+        if (at.first + G * R >= L) {
 #pragma unroll
             for (int i = 0; i < V; ++i) e[i] = p.d_out_h ? p.d_out_h[row + i] : 0.0f;
-        } else if (on) {
+        } else {
             await<V>(p, w + H, e, launch);
         }
         float x[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            start[cl * V + i] = e[i];
+            start[at.cl * V + i] = e[i];
             x[i] = fmaf(tA[i], e[i], tS[i]);
         }
-        if (on) {
-            if (it.seg > 0) {
-                publish<V>(w, x, launch);
-            } else {
+        if (at.seg > 0) {
+            publish<V>(w, x, launch);
+        } else {
 #pragma unroll
-                for (int i = 0; i < V; ++i) p.dh0[row + i] = x[i];
-            }
+            for (int i = 0; i < V; ++i) p.dh0[row + i] = x[i];
         }
     }
     __syncthreads();
+    if (!at.on) return;
 #pragma unroll
-    for (int i = 0; i < V; ++i) e[i] = fmaf(A[i], start[cl * V + i], S[i]);
-    if (on) {
-        auto steps = [&](auto whole) {
+    for (int i = 0; i < V; ++i) e[i] = fmaf(A[i], start[at.cl * V + i], S[i]);
 #pragma unroll
-            for (int r = R - 1; r >= 0; --r) {
-                float df[V], dv[V];
-                const bool valid = whole.value || t0 + r < L;
+    for (int r = R - 1; r >= 0; --r) {
+        float df[V], dv[V];
+        const bool valid = WHOLE || t0 + r < L;
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float gr = q[r][i] + e[i];
-                    df[i] = valid ? gr * f[r][i] : 0.0f;
-                    dv[i] = valid ? gr * k[r][i] : 0.0f;
-                    e[i] = valid ? fmaf(-k[r][i], gr, gr) : e[i];
-                }
-                if (whole.value || t0 + r < T) {
-                    store_vec<E, V>(dz + (long)r * 3 * H, df);
-                    store_vec<E, V>(dz + ((long)r * 3 + 1) * H, dv);
-                }
-            }
-        };
-        if (full) steps(std::true_type{});
-        else steps(std::false_type{});
+        for (int i = 0; i < V; ++i) {
+            const float gr = q[r][i] + e[i];
+            df[i] = valid ? gr * f[r][i] : 0.0f;
+            dv[i] = valid ? gr * k[r][i] : 0.0f;
+            e[i] = valid ? fmaf(-k[r][i], gr, gr) : e[i];
+        }
+        if (WHOLE || t0 + r < p.T) {
+            store_at<E, V>(dz + (long)r * 3 * H, at.zoff, df);
+            store_at<E, V>(dz + ((long)r * 3 + 1) * H, at.zoff, dv);
+        }
     }
-    end_item(p);
+}
+
+template <class E, int V, int NT, int CL>
+__global__ void __launch_bounds__(NT, sizeof(E) == 2 && V == 2 ? 3 : 4) scan_backward_kernel(ScanParams p) {
+    constexpr int R = run_of<E>(), NW = NT / 64;
+    __shared__ unsigned turn[1][2];
+    __shared__ float maps[NW][2][CL * V];
+    __shared__ float start[CL * V];
+    const Place<E, V, NT, CL> at(p, take_item(p, true, turn));
+    if (at.full) {
+        backward_share<true, E, V, NT, CL>(p, at, maps, start);
+    } else if (at.first < at.L) {
+        backward_share<false, E, V, NT, CL>(p, at, maps, start);
+    } else if (at.on) {  // past the row's end
+        E* dz = static_cast<E*>(p.dz) + at.step0(p) * 3 * p.H;
+        float zero[V] = {};
+        for (int r = 0; r < R && at.t0 + r < p.T; ++r)
+#pragma unroll
+            for (int j = 0; j < 3; ++j) store_at<E, V>(dz + ((long)r * 3 + j) * p.H, at.zoff, zero);
+        if (at.L == 0 && at.t0 == 0) {
+            const long row = (long)at.b * p.H + at.c;
+#pragma unroll
+            for (int i = 0; i < V; ++i) p.dh0[row + i] = p.d_out_h ? p.d_out_h[row + i] : 0.0f;
+        }
+    }
 }
 
 // One step of each row: elementwise, V channels per thread.
@@ -474,7 +510,7 @@ scan_step_kernel(const E* z, const float* h, float* out_h, E* y, int rows, int H
 
 int check_scan_sizes(int B, int H, int T, int dtype) {
     if (B < 1 || H < 1 || T < 1 || !valid_dtype(dtype)) return LSTM_DYN_ERR_INVALID;
-    if ((long long)B * T > 0x7fffffffLL || H >= 1 << 24) return LSTM_DYN_ERR_UNSUPPORTED;
+    if ((long long)B * T > 0x7fffffffLL || H >= 1 << 18) return LSTM_DYN_ERR_UNSUPPORTED;
     return LSTM_DYN_OK;
 }
 
@@ -501,39 +537,48 @@ int check_scan_backward(int B, int H, int T, int dtype, const void* z, const int
 
 using namespace ldyn;
 
+struct Shape {
+    int threads, lanes;  // of a workgroup; of those along the channels
+    int segs, tiles;
+};
+
 struct lstm_dyn_scan : OpsHandle {
     int B, H, T, dtype;
-    int vec, threads, lanes;  // channels per thread, threads of a workgroup, lanes along the channels
-    int run, segs, tiles;
-    uint64_t* carry = nullptr;
+    int run, vec;  // steps and channels of a thread
+    Shape fwd, bwd;
+    char* chains[2];  // forward's and backward's counters, then their carries
     float* kept = nullptr;  // made by the first forward for training
     bool has_kept = false;
 };
 
-// The workgroup's shape.
-static void scan_shape(lstm_dyn_scan* h) {
-    h->run = h->dtype == LSTM_DYN_BF16 ? run_of<__bf16>() : run_of<float>();
-    h->vec = h->H % 2 ? 1 : 2;
-    h->lanes = 64;
-    h->threads = 64;
-    while (h->threads < 512 && h->threads / 64 * h->run < h->T) h->threads *= 2;
-    if (h->threads == 512 && 8 * h->run < h->T) h->lanes = 32;  // the longer share: fewer shares in a row's chain
-    const int steps = h->threads / h->lanes * h->run;
-    h->segs = (h->T + steps - 1) / steps;
-    h->tiles = (h->H + h->lanes * h->vec - 1) / (h->lanes * h->vec);
+// The smallest workgroup that holds all steps, up to `most` threads.
+static Shape scan_shape(const lstm_dyn_scan* h, int most) {
+    Shape w{64, 64, 0, 0};
+    while (w.threads < most && w.threads / 64 * h->run < h->T) w.threads *= 2;
+    if (w.threads == most && most / 64 * h->run < h->T) w.lanes = 32;  // the longer share: fewer in a row's chain
+    const int steps = w.threads / w.lanes * h->run;
+    w.segs = (h->T + steps - 1) / steps;
+    w.tiles = (h->H + w.lanes * h->vec - 1) / (w.lanes * h->vec);
+    return w;
 }
 
 template <class E, int V>
 static void scan_launch(const lstm_dyn_scan* h, const ScanParams& p, bool back) {
-    const dim3 grid((unsigned)((long)h->B * h->tiles * h->segs)), block((unsigned)h->threads);
-#define LDYN_SCAN(NT, CL) (back ? scan_backward_kernel<E, V, NT, CL> : scan_forward_kernel<E, V, NT, CL>)
-    auto* k = h->lanes == 32       ? LDYN_SCAN(512, 32)
-              : h->threads == 64  ? LDYN_SCAN(64, 64)
-              : h->threads == 128 ? LDYN_SCAN(128, 64)
-              : h->threads == 256 ? LDYN_SCAN(256, 64)
-                                  : LDYN_SCAN(512, 64);
-    hipLaunchKernelGGL(k, grid, block, 0, h->last_stream, p);
-#undef LDYN_SCAN
+    const Shape& w = back ? h->bwd : h->fwd;
+    void (*k)(ScanParams);
+    if (back)
+        k = w.lanes == 32       ? scan_backward_kernel<E, V, BWD_THREADS, 32>
+            : w.threads == 64  ? scan_backward_kernel<E, V, 64, 64>
+            : w.threads == 128 ? scan_backward_kernel<E, V, 128, 64>
+                               : scan_backward_kernel<E, V, 256, 64>;
+    else
+        k = w.lanes == 32       ? scan_forward_kernel<E, V, FWD_THREADS, 32>
+            : w.threads == 64  ? scan_forward_kernel<E, V, 64, 64>
+            : w.threads == 128 ? scan_forward_kernel<E, V, 128, 64>
+            : w.threads == 256 ? scan_forward_kernel<E, V, 256, 64>
+                               : scan_forward_kernel<E, V, 512, 64>;
+    hipLaunchKernelGGL(k, dim3((unsigned)((long)h->B * w.tiles * w.segs)), dim3((unsigned)w.threads), 0,
+                       h->last_stream, p);
 }
 
 static int scan_run(lstm_dyn_scan* h, const ScanParams& p, bool back) {
@@ -547,8 +592,8 @@ static int scan_run(lstm_dyn_scan* h, const ScanParams& p, bool back) {
     return ops_launched(h);
 }
 
-static ScanParams scan_params(const lstm_dyn_scan* h, const void* z, const int32_t* lengths,
-                              const float* h0) {
+static ScanParams scan_params(const lstm_dyn_scan* h, const Shape& w, const void* z,
+                              const int32_t* lengths, const float* h0) {
     ScanParams p{};
     p.z = z;
     p.lengths = lengths;
@@ -557,10 +602,11 @@ static ScanParams scan_params(const lstm_dyn_scan* h, const void* z, const int32
     p.B = h->B;
     p.T = h->T;
     p.H = h->H;
-    p.tiles = h->tiles;
-    p.segs = h->segs;
-    p.counters = reinterpret_cast<unsigned*>(h->block + 64);
-    p.carry = h->carry;
+    p.tiles = w.tiles;
+    p.segs = w.segs;
+    char* c = h->chains[&w == &h->bwd];
+    p.counters = reinterpret_cast<unsigned long long*>(c);
+    p.carry = reinterpret_cast<uint64_t*>(c + 8LL * COUNTER_WORDS * h->B * w.tiles);
     p.timeout_ticks = (unsigned long long)(5.0 * 1e3 * (double)h->wclk_khz);
     return p;
 }
@@ -583,13 +629,19 @@ extern "C" int lstm_dyn_scan_create(lstm_dyn_scan_t** out, int B, int H, int T, 
     lstm_dyn_scan* h = new (std::nothrow) lstm_dyn_scan();
     if (!h) return LSTM_DYN_ERR_NOMEM;
     h->B = B; h->H = H; h->T = T; h->dtype = dtype;
-    scan_shape(h);
-    const long long carry = h->segs > 1 ? 8LL * B * h->segs * H : 0;
-    if ((rc = ops_init(h, 256 + carry)) != LSTM_DYN_OK) {
+    h->run = dtype == LSTM_DYN_BF16 ? run_of<__bf16>() : run_of<float>();
+    h->vec = H % 2 ? 1 : 2;
+    h->fwd = scan_shape(h, FWD_THREADS);
+    h->bwd = scan_shape(h, BWD_THREADS);
+    auto bytes = [&](const Shape& w) {
+        return w.segs > 1 ? 8LL * COUNTER_WORDS * B * w.tiles + 8LL * B * w.segs * H : 0;
+    };
+    if ((rc = ops_init(h, 256 + bytes(h->fwd) + bytes(h->bwd))) != LSTM_DYN_OK) {
         delete h;
         return rc;
     }
-    h->carry = reinterpret_cast<uint64_t*>(h->block + 256);
+    h->chains[0] = h->block + 256;
+    h->chains[1] = h->chains[0] + bytes(h->fwd);
     *out = h;
     return LSTM_DYN_OK;
 }
@@ -612,7 +664,7 @@ static int scan_forward_impl(lstm_dyn_scan* h, const void* z, const int32_t* len
         h->kept = static_cast<float*>(p);
         h->bytes += n;
     }
-    ScanParams p = scan_params(h, z, lengths, h0);
+    ScanParams p = scan_params(h, h->fwd, z, lengths, h0);
     p.out_h = out_h;
     p.y = out_y;
     p.kept = train ? h->kept : nullptr;
@@ -640,7 +692,7 @@ extern "C" int lstm_dyn_scan_backward(lstm_dyn_scan_t* h, const void* z, const i
     if (!h->has_kept) return LSTM_DYN_ERR_INVALID;  // no forward for training before it
     if ((rc = ops_begin(h, stream)) != LSTM_DYN_OK) return rc;
     h->has_kept = false;
-    ScanParams p = scan_params(h, z, lengths, h0);
+    ScanParams p = scan_params(h, h->bwd, z, lengths, h0);
     p.kept = h->kept;
     p.dy = dy;
     p.d_out_h = d_out_h;
