@@ -187,7 +187,8 @@ int lstm_dyn_check_adamw_args(const lstm_dyn_adamw_tensor_t* tensors, int count,
  * and for a finished beam the one candidate (k, end) = scores[k], all others -inf.
  * A NaN logit counts as -inf; a candidate that is not a number is -inf (a beam whose logits
  * are all -inf has no other).  The K largest candidates are taken, equal ones by the
- * lowest k V + j (within a beam by the logits themselves), in that order:
+ * lowest k V + j, in that order (within a beam the K largest logits are its
+ * candidates, so two that differ only before rounding are not told apart wrongly):
  *     out_scores[k'], out_parent[k'] = k, out_token[k'] = j,
  *     out_finished[k'] = finished[k] or j = end,
  * and every state's rows follow their parents, dst[b][k'] = src[b][out_parent[k']].
@@ -206,7 +207,7 @@ typedef struct {
     long long row_bytes; /* >= 1 */
 } lstm_dyn_beam_state_t;
 
-/* B, V >= 1, 1 <= K <= 32, B * K < 2^24, V < 2^27. */
+/* B, V >= 1, 1 <= K <= 32, B * K < 2^22, V < 2^27. */
 int lstm_dyn_beam_create(lstm_dyn_beam_t** out, int B, int K, int V, int dtype);
 int lstm_dyn_beam_step(lstm_dyn_beam_t* h, const void* logits, const float* scores,
                        const uint8_t* finished, int end, float* out_scores, int32_t* out_parent,

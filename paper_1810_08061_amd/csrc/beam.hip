@@ -7,15 +7,22 @@
 // an order-preserving form above the complement of its index: keys are
 // distinct, and the larger key is the earlier candidate.
 //
-// The simple form: one workgroup per beam takes the largest key below the
-// last one K times over; one per sequence ranks its K K candidates; one per
-// row and state copies.
+// One launch reads the logits once: a workgroup holds a slice of a beam in
+// registers, sums its exps and finds its K best keys:
+//   the K-th largest of 64 lanes' own maxima, found bit by bit with ballots, is
+//   a bound that K keys reach; of the four waves' bounds the largest is taken;
+//   what reaches it (at most K lanes of a wave hold such a key, since keys
+//   are distinct; about 4 K keys in fact) is gathered in LDS and ranked by counting.
+// The last workgroup of a sequence to end joins the slices: the beams'
+// log-sum-exps, then the K best of the slices' keys in the same way.
 #include "ops.h"
 
 namespace ldyn {
 namespace {
 
-constexpr int THREADS = 256, WAVES = THREADS / 64;
+constexpr long long FUSED_STATE_BYTES = 64 << 10;
+
+constexpr int THREADS = 256, WAVES = THREADS / 64, ARRIVED_WORDS = 16;
 
 __device__ inline uint32_t ordered(float x) {
     const uint32_t u = __float_as_uint(x + 0.0f);  // -0 and 0 are equal
@@ -37,9 +44,10 @@ struct BeamParams {
     int32_t* out_parent;
     int32_t* out_token;
     uint8_t* out_finished;
-    uint64_t* best;  // [B K][K] each beam's best keys, in order
-    float* lse;      // [B K]
-    int B, K, V, end;
+    uint64_t* best;    // [B K][slices][K] each slice's best keys, in order; 0 past the last
+    uint64_t* sums;    // [B K][slices] {m, s}
+    unsigned* arrived; // [B] workgroups of the sequence that have ended, 64 bytes apart
+    int B, K, V, end, slices;
 };
 
 // m, s of exp(x - m): joined with those of another part.
@@ -49,92 +57,98 @@ __device__ inline void join_sum(float& m, float& s, float m2, float s2) {
     m = t;
 }
 
-template <class E>
-__global__ void __launch_bounds__(THREADS) beam_rows_simple(BeamParams p) {
-    __shared__ float wm[WAVES], wsum[WAVES];
-    __shared__ uint64_t wk[WAVES];
-    const int row = blockIdx.x, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const E* x = static_cast<const E*>(p.logits) + (long)row * p.V;
-    float m = -__builtin_inff(), s = 0.0f;
-    for (int j = threadIdx.x; j < p.V; j += THREADS) {
-        const float q = (float)x[j];
-        if (q == q && q > -__builtin_inff()) join_sum(m, s, q, 1.0f);
-    }
-    for (int o = 32; o > 0; o >>= 1) {
-        const float m2 = __shfl_xor(m, o), s2 = __shfl_xor(s, o);
-        join_sum(m, s, m2, s2);
-    }
-    if (lane == 0) wm[w] = m, wsum[w] = s;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int i = 1; i < WAVES; ++i) join_sum(m, s, wm[i], wsum[i]);
-        p.lse[row] = m + __logf(s);
-    }
-    uint64_t last = ~0ull;
-    for (int k = 0; k < p.K; ++k) {
-        uint64_t best = 0;
-        for (int j = threadIdx.x; j < p.V; j += THREADS) {
-            const uint64_t q = key_of((float)x[j], (uint32_t)j);
-            if (q < last && q > best) best = q;
+// A bound that the keys of exactly K lanes reach (0 if fewer than K lanes have a
+// key), from the high words alone where they tell K lanes apart; else from
+// low(), the lanes' low words.
+template <class Low>
+__device__ inline uint64_t wave_bound(uint32_t high, int K, Low low) {
+    uint64_t alive = __ballot(high != 0);
+    int need = K;
+    if (__popcll(alive) < K) return 0;
+    uint32_t hi = 0, lo = 0;
+    for (int bit = 31; bit >= 0; --bit) {
+        if (__popcll(alive) == need) return (uint64_t)hi << 32;
+        const uint64_t m = __ballot((high >> bit) & 1) & alive;
+        const int c = __popcll(m);
+        if (c >= need) {
+            alive = m;
+            hi |= 1u << bit;
+        } else {
+            need -= c;
+            alive &= ~m;
         }
-        for (int o = 32; o > 0; o >>= 1) {
-            const uint64_t q = __shfl_xor((unsigned long long)best, o);
-            best = q > best ? q : best;
-        }
-        __syncthreads();
-        if (lane == 0) wk[w] = best;
-        __syncthreads();
-        for (int i = 0; i < WAVES; ++i) best = wk[i] > best ? wk[i] : best;
-        last = best;
-        if (threadIdx.x == 0) p.best[(long)row * p.K + k] = best;  // 0: fewer than K tokens
-        if (best == 0) last = 0;
     }
+    if (__popcll(alive) == need) return (uint64_t)hi << 32;
+    const uint32_t word = low();
+    for (int bit = 31; bit >= 0; --bit) {
+        if (__popcll(alive) == need) break;
+        const uint64_t m = __ballot((word >> bit) & 1) & alive;
+        const int c = __popcll(m);
+        if (c >= need) {
+            alive = m;
+            lo |= 1u << bit;
+        } else {
+            need -= c;
+            alive &= ~m;
+        }
+    }
+    return (uint64_t)hi << 32 | lo;
 }
 
+struct Shared {
+    uint64_t bound[WAVES];
+    uint64_t best[LSTM_DYN_BEAM_MAX_K];  // the K largest keys so far, in order; 0: none
+    float m[WAVES], s[WAVES];
+    float lse[LSTM_DYN_BEAM_MAX_K];
+    int parent[LSTM_DYN_BEAM_MAX_K];
+    unsigned n;
+    int last;
+};
+
+__device__ inline void gather(uint64_t key, uint64_t* cand, unsigned cap, Shared* sh) {
+    const unsigned at = atomicAdd(&sh->n, 1u);
+    if (at < cap) cand[at] = key;
+}
+
+// The K best of the gathered keys and of sh->best, into sh->best.  Called by
+// the whole workgroup after the gathering.
+__device__ inline void rank_keys(uint64_t* cand, unsigned cap, int K, Shared* sh) {
+    if (threadIdx.x < (unsigned)K && sh->best[threadIdx.x]) gather(sh->best[threadIdx.x], cand, cap, sh);
+    __syncthreads();
+    const unsigned n = min(sh->n, cap);
+    if (threadIdx.x < (unsigned)K) sh->best[threadIdx.x] = 0;
+    __syncthreads();
+    for (unsigned i = threadIdx.x; i < n; i += THREADS) {
+        const uint64_t q = cand[i];
+        int rank = 0;
+        for (unsigned j = 0; j < n; ++j) rank += cand[j] > q;
+        if (rank < K) sh->best[rank] = q;
+    }
+    if (threadIdx.x == 0) sh->n = 0;
+    __syncthreads();
+}
+
+// Sixteen bytes of logits.
+template <class E>
+struct Quad {
+    static constexpr int N = 16 / (int)sizeof(E);
+    uint32_t w[4];
+
+    __device__ float operator[](int i) const {
+        if constexpr (sizeof(E) == 4) return __uint_as_float(w[i]);
+        else return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
+    }
+    __device__ void set_nan(int i) {
+        if constexpr (sizeof(E) == 4) w[i] = 0x7fc00000u;
+        else w[i >> 1] = i & 1 ? (w[i >> 1] & 0xffffu) | 0x7fc00000u : (w[i >> 1] & 0xffff0000u) | 0x7fc0u;
+    }
+};
+
 // The k-th entry of a beam whose only candidate is `end` (or none): that one,
-// then the other tokens in order.  Returns the token, or V past the last one.
+// then the other tokens in order.
 __device__ inline int plain_token(int k, int end, int V) {
     if ((unsigned)end >= (unsigned)V) return k;
     return k == 0 ? end : (k <= end ? k - 1 : k);
-}
-
-__global__ void __launch_bounds__(THREADS) beam_select_simple(BeamParams p) {
-    __shared__ uint64_t key[LSTM_DYN_BEAM_MAX_K * LSTM_DYN_BEAM_MAX_K];
-    __shared__ int token[LSTM_DYN_BEAM_MAX_K * LSTM_DYN_BEAM_MAX_K];
-    const int b = blockIdx.x, K = p.K, KK = K * K;
-    for (int i = threadIdx.x; i < KK; i += THREADS) {
-        const int k = i / K, r = i - k * K, row = b * K + k;
-        const float score = p.scores[row], lse = p.lse[row];
-        const bool done = p.finished[row] != 0;
-        const bool dead = !(score > -__builtin_inff()) || !(lse < __builtin_inff());
-        float c = -__builtin_inff();
-        int t;
-        if (done || dead) {
-            t = plain_token(r, done && !dead ? p.end : -1, p.V);
-            if (done && !dead && r == 0 && t == p.end) c = score;
-        } else {
-            const uint64_t q = p.best[(long)row * K + r];
-            t = q ? (int)~(uint32_t)q : p.V;
-            c = score + (unordered((uint32_t)(q >> 32)) - lse);
-        }
-        token[i] = t;
-        // nothing is taken past a beam's last token
-        key[i] = t < p.V ? key_of(c, (uint32_t)i) : 0;
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < KK; i += THREADS) {
-        const uint64_t q = key[i];
-        if (!q) continue;
-        int rank = 0;
-        for (int j = 0; j < KK; ++j) rank += key[j] > q;
-        if (rank < K) {
-            const int k = i / K, o = b * K + rank;
-            p.out_scores[o] = unordered((uint32_t)(q >> 32));
-            p.out_parent[o] = k;
-            p.out_token[o] = token[i];
-            p.out_finished[o] = p.finished[b * K + k] != 0 || token[i] == p.end;
-        }
-    }
 }
 
 struct States {
@@ -142,7 +156,223 @@ struct States {
     char* dst[LSTM_DYN_BEAM_MAX_STATES];
     long long bytes[LSTM_DYN_BEAM_MAX_STATES];
     int unit[LSTM_DYN_BEAM_MAX_STATES];  // 16, 4 or 1 bytes at once
+    int n;                               // how many the selection's launch reorders itself
 };
+
+template <class U>
+__device__ inline void copy_rows(const char* src, char* dst, unsigned row_units, int K, const int* parent) {
+    for (unsigned i = threadIdx.x; i < K * row_units; i += THREADS) {
+        const unsigned k = i / row_units, u = i - k * row_units;
+        reinterpret_cast<U*>(dst)[i] = reinterpret_cast<const U*>(src)[parent[k] * row_units + u];
+    }
+}
+
+// Joins the slices of sequence b; its last workgroup does this.
+__device__ void join_slices(const BeamParams& p, const States& st, int b, uint64_t* cand, unsigned cap,
+                            Shared* sh) {
+    constexpr int HOLD = 8;  // keys a thread holds at once
+    const int K = p.K, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const float ninf = -__builtin_inff();
+    if (threadIdx.x < (unsigned)K) {
+        const int row = b * K + threadIdx.x;
+        float m = ninf, s = 0.0f;
+        for (int i = 0; i < p.slices; ++i) {
+            const uint64_t q = __hip_atomic_load(p.sums + (long)row * p.slices + i, __ATOMIC_RELAXED,
+                                                 __HIP_MEMORY_SCOPE_AGENT);
+            join_sum(m, s, __uint_as_float((uint32_t)(q >> 32)), __uint_as_float((uint32_t)q));
+        }
+        const float lse = m + logf(s);
+        const bool live = p.scores[row] > ninf && lse < __builtin_inff();
+        // a beam that is not live, or whose logits are all -inf, has no number among its candidates
+        sh->lse[threadIdx.x] = live || p.finished[row] ? lse : __builtin_nanf("");
+        sh->best[threadIdx.x] = 0;
+    }
+    __syncthreads();
+    const unsigned per = (unsigned)p.slices * K, total = per * K;
+    for (unsigned base = 0; base < total; base += THREADS * HOLD) {
+        uint64_t key[HOLD], top = 0;
+#pragma unroll
+        for (int i = 0; i < HOLD; ++i) {
+            const unsigned at = base + i * THREADS + threadIdx.x;
+            key[i] = 0;
+            if (at >= total) continue;
+            const unsigned k = at / per, r = at - k * per;
+            const int row = b * K + (int)k;
+            const bool done = p.finished[row] != 0;
+            const float score = p.scores[row], lse = sh->lse[k];
+            if (done || lse != lse) {
+                const int end = done && score > ninf ? p.end : -1;
+                const int t = r < (unsigned)K ? plain_token((int)r, end, p.V) : p.V;
+                if (t < p.V) key[i] = key_of(t == end ? score : ninf, k * (unsigned)p.V + (unsigned)t);
+            } else {
+                const uint64_t q = __hip_atomic_load(p.best + (long)row * per + r, __ATOMIC_RELAXED,
+                                                     __HIP_MEMORY_SCOPE_AGENT);
+                if (q) key[i] = key_of(score + (unordered((uint32_t)(q >> 32)) - lse), k * (unsigned)p.V + ~(uint32_t)q);
+            }
+            top = key[i] > top ? key[i] : top;
+        }
+        const uint64_t bound = wave_bound((uint32_t)(top >> 32), K, [&] { return (uint32_t)top; });
+        if (lane == 0) sh->bound[w] = bound;
+        __syncthreads();
+        uint64_t least = 1;
+        for (int i = 0; i < WAVES; ++i) least = sh->bound[i] > least ? sh->bound[i] : least;
+#pragma unroll
+        for (int i = 0; i < HOLD; ++i)
+            if (key[i] >= least) gather(key[i], cand, cap, sh);
+        rank_keys(cand, cap, K, sh);
+    }
+    if (threadIdx.x < (unsigned)K) {
+        const uint64_t q = sh->best[threadIdx.x];
+        const uint32_t flat = ~(uint32_t)q;
+        const int k = (int)(flat / (unsigned)p.V), t = (int)(flat - (unsigned)k * (unsigned)p.V);
+        const int o = b * K + threadIdx.x;
+        p.out_scores[o] = unordered((uint32_t)(q >> 32));
+        p.out_parent[o] = k;
+        p.out_token[o] = t;
+        p.out_finished[o] = p.finished[b * K + k] != 0 || t == p.end;
+        sh->parent[threadIdx.x] = k;
+    }
+    if (!st.n) return;
+    __syncthreads();
+    for (int q = 0; q < st.n; ++q) {
+        const char* src = st.src[q] + (long)b * K * st.bytes[q];
+        char* dst = st.dst[q] + (long)b * K * st.bytes[q];
+        const unsigned units = (unsigned)(st.bytes[q] / st.unit[q]);
+        if (st.unit[q] == 16) copy_rows<uint4>(src, dst, units, K, sh->parent);
+        else if (st.unit[q] == 4) copy_rows<uint32_t>(src, dst, units, K, sh->parent);
+        else copy_rows<uint8_t>(src, dst, units, K, sh->parent);
+    }
+}
+
+// N: sixteen-byte loads a thread holds at once.
+template <class E, int N>
+__global__ void __launch_bounds__(THREADS) beam_kernel(BeamParams p, States st, unsigned cap) {
+    extern __shared__ uint64_t cand[];
+    __shared__ Shared sh;
+    constexpr int Q = Quad<E>::N;
+    const float ninf = -__builtin_inff();
+    const int K = p.K, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int row = (int)(blockIdx.x / (unsigned)p.slices), slice = (int)(blockIdx.x - (unsigned)row * p.slices);
+    const int b = row / K;
+    if (threadIdx.x < (unsigned)K) sh.best[threadIdx.x] = 0;
+    if (threadIdx.x == 0) sh.n = 0;
+    float m = ninf, s = 0.0f;  // of this wave
+    if (!p.finished[row] && p.scores[row] > ninf) {
+        // the quads of the buffer that hold the row's tokens; token j is element off + j of them
+        const long first = (long)row * p.V, whole = ((long)p.B * K * p.V) / Q;
+        const long quad0 = first / Q;
+        const int off = (int)(first - quad0 * Q);
+        const int quads = (int)(((long)off + p.V + Q - 1) / Q);
+        const int per = (quads + p.slices - 1) / p.slices;
+        const int end = min(quads, (slice + 1) * per);
+        const Quad<E>* x = static_cast<const Quad<E>*>(p.logits) + quad0;
+        const bool ragged = p.V % Q != 0;
+        for (int from = slice * per; from < end; from += THREADS * N) {
+            Quad<E> v[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int at = from + i * THREADS + threadIdx.x;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[i].w[j] = sizeof(E) == 4 ? 0x7fc00000u : 0x7fc07fc0u;
+                if (at < end && quad0 + at < whole) {
+                    const uint4 u = *reinterpret_cast<const uint4*>(x + at);
+                    v[i].w[0] = u.x;
+                    v[i].w[1] = u.y;
+                    v[i].w[2] = u.z;
+                    v[i].w[3] = u.w;
+                } else if (at < end) {  // the buffer ends inside this one
+                    const E* e = static_cast<const E*>(p.logits) + (quad0 + at) * Q;
+                    const int n = (int)((long)p.B * K * p.V - (quad0 + at) * Q);
+#pragma unroll
+                    for (int j = 0; j < Q - 1; ++j) {
+                        if (j >= n) continue;
+                        if constexpr (sizeof(E) == 4) v[i].w[j] = __float_as_uint(e[j]);
+                        else v[i].w[j >> 1] = j & 1 ? (v[i].w[j >> 1] & 0xffffu) | (uint32_t)reinterpret_cast<const uint16_t*>(e)[j] << 16
+                                                    : (v[i].w[j >> 1] & 0xffff0000u) | reinterpret_cast<const uint16_t*>(e)[j];
+                    }
+                }
+                if (ragged && at < end && (at == 0 || at == quads - 1)) {  // other rows' tokens
+#pragma unroll
+                    for (int j = 0; j < Q; ++j) {
+                        const int t = at * Q + j - off;
+                        if (t < 0 || t >= p.V) v[i].set_nan(j);
+                    }
+                }
+            }
+            // a NaN is passed over by the maximum, and adds nothing to the sum
+            float top = ninf;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int j = 0; j < Q; ++j) top = fmaxf(top, v[i][j]);
+            float wm = top;
+            for (int o = 32; o > 0; o >>= 1) wm = fmaxf(wm, __shfl_xor(wm, o));
+            if (wm > ninf) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+#pragma unroll
+                    for (int j = 0; j < Q; ++j) sum += __expf(fmaxf(v[i][j], ninf) - wm);
+                for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+                join_sum(m, s, wm, sum);
+            }
+            const int mine = from + (int)threadIdx.x;  // this thread's first quad
+            auto token = [&](int i, int j) { return (mine + i * THREADS) * Q + j - off; };
+            const uint64_t bound = wave_bound(mine < end ? ordered(top) : 0u, K, [&] {
+                uint32_t t = 0;  // the first token that has the maximum
+#pragma unroll
+                for (int i = N - 1; i >= 0; --i)
+#pragma unroll
+                    for (int j = Q - 1; j >= 0; --j) {
+                        const int q = token(i, j);
+                        const bool in = mine + i * THREADS < end && q >= 0 && q < p.V;
+                        if (in && fmaxf(v[i][j], ninf) == top) t = (uint32_t)q;
+                    }
+                return ~t;
+            });
+            if (lane == 0) sh.bound[w] = bound;
+            __syncthreads();
+            uint64_t least = 1;
+            for (int i = 0; i < WAVES; ++i) least = sh.bound[i] > least ? sh.bound[i] : least;
+            const float low = unordered((uint32_t)(least >> 32));
+            const bool all = (uint32_t)(least >> 32) <= ordered(ninf);  // -inf reaches it, or anything
+            if (mine < end && (all || top >= low)) {
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+#pragma unroll
+                    for (int j = 0; j < Q; ++j) {
+                        if (!all && !(v[i][j] >= low)) continue;
+                        const int q = token(i, j);
+                        const uint64_t key = key_of(v[i][j], (uint32_t)q);
+                        if (mine + i * THREADS < end && q >= 0 && q < p.V && key >= least) gather(key, cand, cap, &sh);
+                    }
+            }
+            rank_keys(cand, cap, K, &sh);
+        }
+    }
+    if (lane == 0) sh.m[w] = m, sh.s[w] = s;
+    __syncthreads();
+    // Written past the caches of this XCD, and counted once they are there.
+    if (threadIdx.x < (unsigned)K)
+        __hip_atomic_store(p.best + ((long)row * p.slices + slice) * K + threadIdx.x, sh.best[threadIdx.x],
+                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (threadIdx.x == 64) {
+        for (int i = 0; i < WAVES; ++i)
+            if (i != w) join_sum(m, s, sh.m[i], sh.s[i]);
+        __hip_atomic_store(p.sums + (long)row * p.slices + slice, (uint64_t)__float_as_uint(m) << 32 | __float_as_uint(s),
+                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        unsigned* count = p.arrived + (long)b * ARRIVED_WORDS;
+        const unsigned all = (unsigned)(K * p.slices);
+        sh.last = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == all - 1;
+        if (sh.last) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // for the next launch
+    }
+    __syncthreads();
+    if (sh.last) join_slices(p, st, b, cand, cap, &sh);
+}
 
 template <class U>
 __device__ inline void copy_row(const char* src, char* dst, long long bytes) {
@@ -164,7 +394,7 @@ __global__ void __launch_bounds__(THREADS) beam_reorder_kernel(BeamParams p, Sta
 
 int check_beam_sizes(int B, int K, int V, int dtype) {
     if (B < 1 || K < 1 || V < 1 || !valid_dtype(dtype)) return LSTM_DYN_ERR_INVALID;
-    if (K > LSTM_DYN_BEAM_MAX_K || (long long)B * K >= 1 << 24 || V >= 1 << 27) return LSTM_DYN_ERR_UNSUPPORTED;
+    if (K > LSTM_DYN_BEAM_MAX_K || (long long)B * K >= 1 << 22 || V >= 1 << 27) return LSTM_DYN_ERR_UNSUPPORTED;
     return LSTM_DYN_OK;
 }
 
@@ -194,9 +424,40 @@ using namespace ldyn;
 
 struct lstm_dyn_beam : OpsHandle {
     int B, K, V, dtype;
-    uint64_t* best;
-    float* lse;
+    int hold, slices;  // sixteen-byte loads a thread holds; slices of a beam
+    unsigned cap;      // keys a workgroup gathers at most
+    uint64_t *best, *sums;
+    unsigned* arrived;
 };
+
+// How a beam's logits are cut: as many loads a thread as the LDS for their
+// keys allows (32 KB), fewer where that would leave fewer than four
+// workgroups a CU; and no more slices than can be joined in a few rounds (a
+// workgroup takes its slice in pieces then).
+static void beam_shape(lstm_dyn_beam* h, int num_cus) {
+    const int quad = 16 / dtype_bytes(h->dtype);
+    const long quads = ((long)h->V + quad - 1) / quad + (h->V % quad ? 1 : 0), rows = (long)h->B * h->K;
+    auto slices = [&](int n) { return (quads + THREADS * n - 1) / (THREADS * n); };
+    int n = 8;
+    while (n > 1 && (WAVES * h->K * n * quad * 8 > 32768 || rows * slices(n) < 4L * num_cus)) n /= 2;
+    long most = 2048 / (h->K * h->K);
+    if (most < 8) most = 8;
+    h->hold = n;
+    h->slices = (int)(slices(n) < most ? slices(n) : most);
+    // a lane's keys for K lanes of each wave, the best so far; in the join eight a lane
+    const int lane = n * quad > 8 ? n * quad : 8;
+    h->cap = (unsigned)(WAVES * h->K * lane + h->K);
+}
+
+template <class E>
+static void beam_launch(const lstm_dyn_beam* h, const BeamParams& p, const States& st) {
+    auto* k = h->hold == 8   ? beam_kernel<E, 8>
+              : h->hold == 4 ? beam_kernel<E, 4>
+              : h->hold == 2 ? beam_kernel<E, 2>
+                             : beam_kernel<E, 1>;
+    hipLaunchKernelGGL(k, dim3((unsigned)(h->B * h->K) * (unsigned)h->slices), dim3(THREADS), 8 * h->cap,
+                       h->last_stream, p, st, h->cap);
+}
 
 extern "C" int lstm_dyn_check_beam_args(int B, int K, int V, int dtype, const void* logits,
                                         const float* scores, const uint8_t* finished,
@@ -215,13 +476,22 @@ extern "C" int lstm_dyn_beam_create(lstm_dyn_beam_t** out, int B, int K, int V, 
     lstm_dyn_beam* h = new (std::nothrow) lstm_dyn_beam();
     if (!h) return LSTM_DYN_ERR_NOMEM;
     h->B = B; h->K = K; h->V = V; h->dtype = dtype;
-    const long long nb = 8LL * B * K * K;
-    if ((rc = ops_init(h, 256 + nb + 4LL * B * K)) != LSTM_DYN_OK) {
+    int dev = 0, cus = 0;
+    if (hipGetDevice(&dev) != hipSuccess ||
+        hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) {
+        (void)hipGetLastError();
+        delete h;
+        return LSTM_DYN_ERR_HIP;
+    }
+    beam_shape(h, cus);
+    const long long na = 4LL * ARRIVED_WORDS * B, ns = 8LL * B * K * h->slices;
+    if ((rc = ops_init(h, 256 + na + ns + ns * K)) != LSTM_DYN_OK) {
         delete h;
         return rc;
     }
-    h->best = reinterpret_cast<uint64_t*>(h->block + 256);
-    h->lse = reinterpret_cast<float*>(h->block + 256 + nb);
+    h->arrived = reinterpret_cast<unsigned*>(h->block + 256);
+    h->sums = reinterpret_cast<uint64_t*>(h->block + 256 + na);
+    h->best = h->sums + (long)B * K * h->slices;
     *out = h;
     return LSTM_DYN_OK;
 }
@@ -236,25 +506,25 @@ extern "C" int lstm_dyn_beam_step(lstm_dyn_beam_t* h, const void* logits, const 
     if (rc != LSTM_DYN_OK) return rc;
     if ((rc = ops_begin(h, stream)) != LSTM_DYN_OK) return rc;
     const BeamParams p{logits, scores, finished, out_scores, out_parent, out_token, out_finished,
-                       h->best, h->lse, h->B, h->K, h->V, end};
-    const unsigned rows = (unsigned)(h->B * h->K);
-    if (h->dtype == LSTM_DYN_BF16)
-        hipLaunchKernelGGL((beam_rows_simple<__bf16>), dim3(rows), dim3(THREADS), 0, h->last_stream, p);
-    else
-        hipLaunchKernelGGL((beam_rows_simple<float>), dim3(rows), dim3(THREADS), 0, h->last_stream, p);
-    if ((rc = ops_launched(h)) != LSTM_DYN_OK) return rc;
-    hipLaunchKernelGGL(beam_select_simple, dim3((unsigned)h->B), dim3(THREADS), 0, h->last_stream, p);
-    if ((rc = ops_launched(h)) != LSTM_DYN_OK || !n_states) return rc;
+                       h->best, h->sums, h->arrived, h->B, h->K, h->V, end, h->slices};
     States s{};
+    long long bytes = 0;
     for (int i = 0; i < n_states; ++i) {
         s.src[i] = static_cast<const char*>(states[i].src);
         s.dst[i] = static_cast<char*>(states[i].dst);
         s.bytes[i] = states[i].row_bytes;
+        bytes += states[i].row_bytes;
         const uintptr_t a = reinterpret_cast<uintptr_t>(s.src[i]) | reinterpret_cast<uintptr_t>(s.dst[i]) |
                             (uintptr_t)s.bytes[i];
         s.unit[i] = a % 16 == 0 ? 16 : a % 4 == 0 ? 4 : 1;
     }
-    hipLaunchKernelGGL(beam_reorder_kernel, dim3(rows, (unsigned)n_states), dim3(THREADS), 0,
+    // up to this much of a sequence's states its last workgroup copies itself
+    const bool own = bytes * h->K <= FUSED_STATE_BYTES;
+    if (own) s.n = n_states;
+    if (h->dtype == LSTM_DYN_BF16) beam_launch<__bf16>(h, p, s);
+    else beam_launch<float>(h, p, s);
+    if ((rc = ops_launched(h)) != LSTM_DYN_OK || own) return rc;
+    hipLaunchKernelGGL(beam_reorder_kernel, dim3((unsigned)(h->B * h->K), (unsigned)n_states), dim3(THREADS), 0,
                        h->last_stream, p, s);
     return ops_launched(h);
 }
