@@ -23,6 +23,7 @@ namespace {
 constexpr long long FUSED_STATE_BYTES = 64 << 10;
 
 constexpr int THREADS = 256, WAVES = THREADS / 64, ARRIVED_WORDS = 16;
+constexpr int GATHER = 512;  // keys ranked at once
 
 __device__ inline uint32_t ordered(float x) {
     const uint32_t u = __float_as_uint(x + 0.0f);  // -0 and 0 are equal
@@ -57,74 +58,91 @@ __device__ inline void join_sum(float& m, float& s, float m2, float s2) {
     m = t;
 }
 
-// A bound that the keys of exactly K lanes reach (0 if fewer than K lanes have a
-// key), from the high words alone where they tell K lanes apart; else from
-// low(), the lanes' low words.
-template <class Low>
-__device__ inline uint64_t wave_bound(uint32_t high, int K, Low low) {
+// Over the wave, in every lane (row shifts, then broadcasts of rows' last lanes).
+template <int CTRL>
+__device__ inline float dpp(float old, float x) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(old), __float_as_int(x), CTRL, 0xf, 0xf, false));
+}
+__device__ inline float lane63(float x) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63)); }
+__device__ inline float wave_max(float x) {
+    const float ninf = -__builtin_inff();
+    x = fmaxf(x, dpp<0x111>(ninf, x));
+    x = fmaxf(x, dpp<0x112>(ninf, x));
+    x = fmaxf(x, dpp<0x114>(ninf, x));
+    x = fmaxf(x, dpp<0x118>(ninf, x));
+    x = fmaxf(x, dpp<0x142>(ninf, x));
+    x = fmaxf(x, dpp<0x143>(ninf, x));
+    return lane63(x);
+}
+__device__ inline float wave_sum(float x) {
+    x += dpp<0x111>(0.0f, x);
+    x += dpp<0x112>(0.0f, x);
+    x += dpp<0x114>(0.0f, x);
+    x += dpp<0x118>(0.0f, x);
+    x += dpp<0x142>(0.0f, x);
+    x += dpp<0x143>(0.0f, x);
+    return lane63(x);
+}
+
+// A bound that the keys of at least K lanes reach (0 if fewer have a key): the
+// K-th largest, bit by bit from the top (LAST: below it all bits are the
+// same), ended as soon as the bits so far tell exactly K lanes apart.  From the
+// high words alone, where equal ones may let more than K lanes reach it; with
+// `exact` also from low(), the lanes' low words.
+template <int LAST, class Low>
+__device__ inline uint64_t wave_bound(uint32_t high, int K, bool exact, Low low) {
     uint64_t alive = __ballot(high != 0);
-    int need = K;
     if (__popcll(alive) < K) return 0;
-    uint32_t hi = 0, lo = 0;
-    for (int bit = 31; bit >= 0; --bit) {
-        if (__popcll(alive) == need) return (uint64_t)hi << 32;
-        const uint64_t m = __ballot((high >> bit) & 1) & alive;
-        const int c = __popcll(m);
-        if (c >= need) {
-            alive = m;
-            hi |= 1u << bit;
-        } else {
-            need -= c;
-            alive &= ~m;
+    int need = K;
+    auto narrow = [&](uint32_t word, int last) {
+        uint32_t bits = 0;
+        for (int bit = 31; bit >= last && __popcll(alive) != need; --bit) {
+            const uint64_t m = __ballot((word >> bit) & 1) & alive;
+            const int c = __popcll(m);
+            if (c >= need) {
+                alive = m;
+                bits |= 1u << bit;
+            } else {
+                need -= c;
+                alive &= ~m;
+            }
         }
-    }
-    if (__popcll(alive) == need) return (uint64_t)hi << 32;
-    const uint32_t word = low();
-    for (int bit = 31; bit >= 0; --bit) {
-        if (__popcll(alive) == need) break;
-        const uint64_t m = __ballot((word >> bit) & 1) & alive;
-        const int c = __popcll(m);
-        if (c >= need) {
-            alive = m;
-            lo |= 1u << bit;
-        } else {
-            need -= c;
-            alive &= ~m;
-        }
-    }
-    return (uint64_t)hi << 32 | lo;
+        return bits;
+    };
+    const uint64_t hi = (uint64_t)narrow(high, LAST) << 32;
+    if (!exact || __popcll(alive) == need) return hi;
+    return hi | narrow(low(), 0);
 }
 
 struct Shared {
     uint64_t bound[WAVES];
     uint64_t best[LSTM_DYN_BEAM_MAX_K];  // the K largest keys so far, in order; 0: none
+    uint64_t cand[GATHER + LSTM_DYN_BEAM_MAX_K];
     float m[WAVES], s[WAVES];
     float lse[LSTM_DYN_BEAM_MAX_K];
     int parent[LSTM_DYN_BEAM_MAX_K];
-    unsigned n;
+    unsigned n, quads;
     int last;
 };
 
-__device__ inline void gather(uint64_t key, uint64_t* cand, unsigned cap, Shared* sh) {
-    const unsigned at = atomicAdd(&sh->n, 1u);
-    if (at < cap) cand[at] = key;
-}
+__device__ inline void gather(uint64_t key, Shared* sh) { sh->cand[atomicAdd(&sh->n, 1u)] = key; }
 
-// The K best of the gathered keys and of sh->best, into sh->best.  Called by
-// the whole workgroup after the gathering.
-__device__ inline void rank_keys(uint64_t* cand, unsigned cap, int K, Shared* sh) {
-    if (threadIdx.x < (unsigned)K && sh->best[threadIdx.x]) gather(sh->best[threadIdx.x], cand, cap, sh);
+// The K best of the gathered keys (at most GATHER) and of sh->best, into sh->best.
+// Called by the whole workgroup after the gathering.
+__device__ inline void rank_keys(int K, Shared* sh) {
+    if (threadIdx.x < (unsigned)K && sh->best[threadIdx.x]) gather(sh->best[threadIdx.x], sh);
     __syncthreads();
-    const unsigned n = min(sh->n, cap);
+    const unsigned n = sh->n;
     if (threadIdx.x < (unsigned)K) sh->best[threadIdx.x] = 0;
     __syncthreads();
     for (unsigned i = threadIdx.x; i < n; i += THREADS) {
-        const uint64_t q = cand[i];
+        const uint64_t q = sh->cand[i];
         int rank = 0;
-        for (unsigned j = 0; j < n; ++j) rank += cand[j] > q;
+#pragma unroll 4
+        for (unsigned j = 0; j < n; ++j) rank += sh->cand[j] > q;
         if (rank < K) sh->best[rank] = q;
     }
-    if (threadIdx.x == 0) sh->n = 0;
+    if (threadIdx.x == 0) sh->n = sh->quads = 0;
     __syncthreads();
 }
 
@@ -143,6 +161,16 @@ struct Quad {
         else w[i >> 1] = i & 1 ? (w[i >> 1] & 0xffffu) | 0x7fc00000u : (w[i >> 1] & 0xffff0000u) | 0x7fc0u;
     }
 };
+
+// The compiler may not keep what it formed of these before here (bf16 pairs
+// widened once and kept take twice their registers).
+template <class E, int N>
+__device__ inline void hold(Quad<E>* v) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(v[i].w[j]));
+}
 
 // The k-th entry of a beam whose only candidate is `end` (or none): that one,
 // then the other tokens in order.
@@ -168,9 +196,8 @@ __device__ inline void copy_rows(const char* src, char* dst, unsigned row_units,
 }
 
 // Joins the slices of sequence b; its last workgroup does this.
-__device__ void join_slices(const BeamParams& p, const States& st, int b, uint64_t* cand, unsigned cap,
-                            Shared* sh) {
-    constexpr int HOLD = 8;  // keys a thread holds at once
+__device__ void join_slices(const BeamParams& p, const States& st, int b, Shared* sh) {
+    constexpr int HOLD = GATHER / THREADS;  // keys a thread holds at once
     const int K = p.K, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const float ninf = -__builtin_inff();
     if (threadIdx.x < (unsigned)K) {
@@ -190,7 +217,7 @@ __device__ void join_slices(const BeamParams& p, const States& st, int b, uint64
     __syncthreads();
     const unsigned per = (unsigned)p.slices * K, total = per * K;
     for (unsigned base = 0; base < total; base += THREADS * HOLD) {
-        uint64_t key[HOLD], top = 0;
+        uint64_t key[HOLD];
 #pragma unroll
         for (int i = 0; i < HOLD; ++i) {
             const unsigned at = base + i * THREADS + threadIdx.x;
@@ -209,17 +236,20 @@ __device__ void join_slices(const BeamParams& p, const States& st, int b, uint64
                                                      __HIP_MEMORY_SCOPE_AGENT);
                 if (q) key[i] = key_of(score + (unordered((uint32_t)(q >> 32)) - lse), k * (unsigned)p.V + ~(uint32_t)q);
             }
-            top = key[i] > top ? key[i] : top;
         }
-        const uint64_t bound = wave_bound((uint32_t)(top >> 32), K, [&] { return (uint32_t)top; });
+        // no worse than the K-th so far, and than what K lanes of a wave have
+        uint64_t top = key[0];
+#pragma unroll
+        for (int i = 1; i < HOLD; ++i) top = key[i] > top ? key[i] : top;
+        const uint64_t bound = wave_bound<0>((uint32_t)(top >> 32), K, false, [] { return 0u; });
         if (lane == 0) sh->bound[w] = bound;
         __syncthreads();
-        uint64_t least = 1;
+        uint64_t least = sh->best[K - 1] | 1;
         for (int i = 0; i < WAVES; ++i) least = sh->bound[i] > least ? sh->bound[i] : least;
 #pragma unroll
         for (int i = 0; i < HOLD; ++i)
-            if (key[i] >= least) gather(key[i], cand, cap, sh);
-        rank_keys(cand, cap, K, sh);
+            if (key[i] >= least) gather(key[i], sh);
+        rank_keys(K, sh);
     }
     if (threadIdx.x < (unsigned)K) {
         const uint64_t q = sh->best[threadIdx.x];
@@ -244,18 +274,34 @@ __device__ void join_slices(const BeamParams& p, const States& st, int b, uint64
     }
 }
 
+// A lane's largest key.  Read again, element by element: only rows with more
+// equal logits than a workgroup can put aside come here.
+template <class E, int N>
+__device__ __attribute__((noinline)) uint64_t largest_key(const E* row, int mine, int end, int off, int V) {
+    uint64_t top = 0;
+#pragma unroll 1
+    for (int i = 0; i < N * Quad<E>::N; ++i) {
+        const int quad = mine + i / Quad<E>::N * THREADS, t = quad * Quad<E>::N + i % Quad<E>::N - off;
+        if (quad >= end || t < 0 || t >= V) continue;
+        const uint64_t key = key_of((float)row[t], (uint32_t)t);
+        top = key > top ? key : top;
+    }
+    return top;
+}
+
 // N: sixteen-byte loads a thread holds at once.
 template <class E, int N>
-__global__ void __launch_bounds__(THREADS) beam_kernel(BeamParams p, States st, unsigned cap) {
-    extern __shared__ uint64_t cand[];
+__global__ void __launch_bounds__(THREADS) beam_kernel(BeamParams p, States st, unsigned room) {
+    extern __shared__ uint4 held[];  // `room` quads, then their numbers
     __shared__ Shared sh;
+    int* number = reinterpret_cast<int*>(held + room);
     constexpr int Q = Quad<E>::N;
     const float ninf = -__builtin_inff();
     const int K = p.K, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int row = (int)(blockIdx.x / (unsigned)p.slices), slice = (int)(blockIdx.x - (unsigned)row * p.slices);
     const int b = row / K;
     if (threadIdx.x < (unsigned)K) sh.best[threadIdx.x] = 0;
-    if (threadIdx.x == 0) sh.n = 0;
+    if (threadIdx.x == 0) sh.n = sh.quads = 0;
     float m = ninf, s = 0.0f;  // of this wave
     if (!p.finished[row] && p.scores[row] > ninf) {
         // the quads of the buffer that hold the row's tokens; token j is element off + j of them
@@ -299,55 +345,87 @@ __global__ void __launch_bounds__(THREADS) beam_kernel(BeamParams p, States st, 
                     }
                 }
             }
-            // a NaN is passed over by the maximum, and adds nothing to the sum
-            float top = ninf;
+            // a NaN is passed over by the maximum
+            float most[N], top = ninf;
 #pragma unroll
-            for (int i = 0; i < N; ++i)
+            for (int i = 0; i < N; ++i) {
+                most[i] = ninf;
 #pragma unroll
-                for (int j = 0; j < Q; ++j) top = fmaxf(top, v[i][j]);
-            float wm = top;
-            for (int o = 32; o > 0; o >>= 1) wm = fmaxf(wm, __shfl_xor(wm, o));
+                for (int j = 0; j < Q; ++j) most[i] = fmaxf(most[i], v[i][j]);
+                top = fmaxf(top, most[i]);
+            }
+            const float wm = wave_max(top);
+            hold<E, N>(v);
             if (wm > ninf) {
+                // exp(x - wm) as 2^(x log2 e - c), c = wm log2 e: c's rounding is common to all terms
+                const float log2e = 1.44269504f, c = wm * log2e;
                 float sum = 0.0f;
 #pragma unroll
                 for (int i = 0; i < N; ++i)
 #pragma unroll
-                    for (int j = 0; j < Q; ++j) sum += __expf(fmaxf(v[i][j], ninf) - wm);
-                for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-                join_sum(m, s, wm, sum);
+                    for (int j = 0; j < Q; ++j) sum += __builtin_amdgcn_exp2f(fmaf(v[i][j], log2e, -c));
+                sum = wave_sum(sum);
+                if (sum != sum) {  // NaN logits add nothing
+                    hold<E, N>(v);
+                    sum = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < N; ++i)
+#pragma unroll
+                        for (int j = 0; j < Q; ++j) sum += __builtin_amdgcn_exp2f(fmaf(fmaxf(v[i][j], ninf), log2e, -c));
+                    sum = wave_sum(sum);
+                }
+                join_sum(m, s, wm, sum * __builtin_amdgcn_exp2f(c - wm * log2e));
             }
             const int mine = from + (int)threadIdx.x;  // this thread's first quad
-            auto token = [&](int i, int j) { return (mine + i * THREADS) * Q + j - off; };
-            const uint64_t bound = wave_bound(mine < end ? ordered(top) : 0u, K, [&] {
-                uint32_t t = 0;  // the first token that has the maximum
+            // Quads that hold a key as large as the bound go to LDS.  First by the maxima
+            // alone; where equal logits make those too many, by the tokens too, which leaves
+            // at most K lanes of a wave.
+            bool exact = false;
+            uint64_t least;
+            for (;;) {
+                const uint64_t own = exact ? largest_key<E, N>(static_cast<const E*>(p.logits) + first, mine, end, off, p.V)
+                                           : (uint64_t)(mine < end ? ordered(top) : 0u) << 32;
+                const uint64_t bound = exact ? wave_bound<0>((uint32_t)(own >> 32), K, true, [&] { return (uint32_t)own; })
+                                             : wave_bound<sizeof(E) == 2 ? 16 : 0>((uint32_t)(own >> 32), K, false, [] { return 0u; });
+                if (lane == 0) sh.bound[w] = bound;
+                __syncthreads();
+                least = sh.best[K - 1] | 1;
+                for (int i = 0; i < WAVES; ++i) least = sh.bound[i] > least ? sh.bound[i] : least;
+                const uint32_t low = (uint32_t)(least >> 32);
+                // a lane whose own largest key does not reach the bound holds none that does
+                const bool in = exact ? own >= least : (uint32_t)(own >> 32) >= low && mine < end;
+                if (in) {
 #pragma unroll
-                for (int i = N - 1; i >= 0; --i)
-#pragma unroll
-                    for (int j = Q - 1; j >= 0; --j) {
-                        const int q = token(i, j);
-                        const bool in = mine + i * THREADS < end && q >= 0 && q < p.V;
-                        if (in && fmaxf(v[i][j], ninf) == top) t = (uint32_t)q;
-                    }
-                return ~t;
-            });
-            if (lane == 0) sh.bound[w] = bound;
-            __syncthreads();
-            uint64_t least = 1;
-            for (int i = 0; i < WAVES; ++i) least = sh.bound[i] > least ? sh.bound[i] : least;
-            const float low = unordered((uint32_t)(least >> 32));
-            const bool all = (uint32_t)(least >> 32) <= ordered(ninf);  // -inf reaches it, or anything
-            if (mine < end && (all || top >= low)) {
-#pragma unroll
-                for (int i = 0; i < N; ++i)
-#pragma unroll
-                    for (int j = 0; j < Q; ++j) {
-                        if (!all && !(v[i][j] >= low)) continue;
-                        const int q = token(i, j);
-                        const uint64_t key = key_of(v[i][j], (uint32_t)q);
-                        if (mine + i * THREADS < end && q >= 0 && q < p.V && key >= least) gather(key, cand, cap, &sh);
-                    }
+                    for (int i = 0; i < N; ++i)
+                        if (mine + i * THREADS < end && ordered(most[i]) >= low) {
+                            const unsigned at = atomicAdd(&sh.quads, 1u);
+                            if (at < room) {
+                                held[at] = uint4{v[i].w[0], v[i].w[1], v[i].w[2], v[i].w[3]};
+                                number[at] = mine + i * THREADS;
+                            }
+                        }
+                }
+                __syncthreads();
+                if (sh.quads <= room || exact) break;
+                exact = true;
+                __syncthreads();
+                if (threadIdx.x == 0) sh.quads = 0;
+                __syncthreads();
             }
-            rank_keys(cand, cap, K, &sh);
+            // their keys, GATHER at a time
+            const unsigned elems = min(sh.quads, room) * Q;
+            for (unsigned base = 0; base < elems; base += GATHER) {
+                least = sh.best[K - 1] > least ? sh.best[K - 1] : least;
+                for (unsigned at = base + threadIdx.x; at < min(elems, base + GATHER); at += THREADS) {
+                    const unsigned q = at / Q, j = at % Q;
+                    const float x = sizeof(E) == 4 ? reinterpret_cast<const float*>(held)[at]
+                                                   : __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(held)[at] << 16);
+                    const int t = number[q] * Q + (int)j - off;
+                    const uint64_t key = key_of(x, (uint32_t)t);
+                    if (t >= 0 && t < p.V && key >= least) gather(key, &sh);
+                }
+                rank_keys(K, &sh);
+            }
         }
     }
     if (lane == 0) sh.m[w] = m, sh.s[w] = s;
@@ -371,7 +449,7 @@ __global__ void __launch_bounds__(THREADS) beam_kernel(BeamParams p, States st, 
         if (sh.last) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // for the next launch
     }
     __syncthreads();
-    if (sh.last) join_slices(p, st, b, cand, cap, &sh);
+    if (sh.last) join_slices(p, st, b, &sh);
 }
 
 template <class U>
@@ -425,28 +503,25 @@ using namespace ldyn;
 struct lstm_dyn_beam : OpsHandle {
     int B, K, V, dtype;
     int hold, slices;  // sixteen-byte loads a thread holds; slices of a beam
-    unsigned cap;      // keys a workgroup gathers at most
+    unsigned room;     // quads a workgroup puts aside at most
     uint64_t *best, *sums;
     unsigned* arrived;
 };
 
-// How a beam's logits are cut: as many loads a thread as the LDS for their
-// keys allows (32 KB), fewer where that would leave fewer than four
-// workgroups a CU; and no more slices than can be joined in a few rounds (a
+// How a beam's logits are cut: eight loads a thread, fewer where that would
+// leave fewer than four workgroups a CU; and no more slices than can be joined in a few rounds (a
 // workgroup takes its slice in pieces then).
 static void beam_shape(lstm_dyn_beam* h, int num_cus) {
     const int quad = 16 / dtype_bytes(h->dtype);
     const long quads = ((long)h->V + quad - 1) / quad + (h->V % quad ? 1 : 0), rows = (long)h->B * h->K;
     auto slices = [&](int n) { return (quads + THREADS * n - 1) / (THREADS * n); };
     int n = 8;
-    while (n > 1 && (WAVES * h->K * n * quad * 8 > 32768 || rows * slices(n) < 4L * num_cus)) n /= 2;
+    while (n > 1 && rows * slices(n) < 4L * num_cus) n /= 2;
     long most = 2048 / (h->K * h->K);
     if (most < 8) most = 8;
     h->hold = n;
     h->slices = (int)(slices(n) < most ? slices(n) : most);
-    // a lane's keys for K lanes of each wave, the best so far; in the join eight a lane
-    const int lane = n * quad > 8 ? n * quad : 8;
-    h->cap = (unsigned)(WAVES * h->K * lane + h->K);
+    h->room = (unsigned)(WAVES * h->K * n);  // all quads of K lanes of each wave
 }
 
 template <class E>
@@ -455,8 +530,8 @@ static void beam_launch(const lstm_dyn_beam* h, const BeamParams& p, const State
               : h->hold == 4 ? beam_kernel<E, 4>
               : h->hold == 2 ? beam_kernel<E, 2>
                              : beam_kernel<E, 1>;
-    hipLaunchKernelGGL(k, dim3((unsigned)(h->B * h->K) * (unsigned)h->slices), dim3(THREADS), 8 * h->cap,
-                       h->last_stream, p, st, h->cap);
+    hipLaunchKernelGGL(k, dim3((unsigned)(h->B * h->K) * (unsigned)h->slices), dim3(THREADS), 20 * h->room,
+                       h->last_stream, p, st, h->room);
 }
 
 extern "C" int lstm_dyn_check_beam_args(int B, int K, int V, int dtype, const void* logits,
