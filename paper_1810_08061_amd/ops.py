@@ -65,7 +65,7 @@ def _lib():
 # --- C ABI mirrors ----------------------------------------------------------
 
 def _call(name, *args):
-    rc = getattr(_lib(), name)(*args)
+    rc = getattr(_ready or _lib(), name)(*args)
     if rc != OK:
         raise LstmDynError(rc, name)
 
@@ -192,29 +192,42 @@ def lstm_dyn_check_beam_args(*args) -> int:
 
 # --- torch convenience wrappers ---------------------------------------------
 
+_torch = None
+
+
+def _t():
+    """torch, imported at the first handle: importing this module does not need it."""
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
 def _check(name, t, dtype, shape):
-    import torch
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+    try:
+        if t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous():
+            return
+    except AttributeError:
+        pass
+    if not isinstance(t, _t().Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a device tensor")
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
+    raise ValueError(f"{name} must be contiguous")
 
 
 def _stream(stream, device):
     if stream is None:
-        import torch
-        stream = torch.cuda.current_stream(device)
+        return _t().cuda.current_stream(device).cuda_stream
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
 def _dtype(dtype):
-    import torch
     code = _DTYPES[dtype] if isinstance(dtype, str) else int(dtype)
-    return code, (torch.bfloat16 if code == BF16 else torch.float32)
+    return code, (_t().bfloat16 if code == BF16 else _t().float32)
 
 
 class _Handle:
@@ -259,7 +272,7 @@ class GatedScan(_Handle):
         self.handle = lstm_dyn_scan_create(B, H, T_max, self.dtype)
 
     def _forward(self, call, z, lengths, h0, out_h, out_y, stream):
-        import torch
+        torch = _torch
         B, T, H = self.B, self.T, self.H
         _check("z", z, self._et, (B, T, 3 * H))
         _check("lengths", lengths, torch.int32, (B,))
@@ -291,7 +304,7 @@ class GatedScan(_Handle):
         [B, T_max, 3H] (the handle's dtype) and dh0 float32 [B, H].  dy in the
         handle's dtype; d_out_h float32 [B, H] or None.  out: a dict with those
         keys holding caller-owned tensors."""
-        import torch
+        torch = _torch
         B, T, H = self.B, self.T, self.H
         _check("z", z, self._et, (B, T, 3 * H))
         _check("lengths", lengths, torch.int32, (B,))
@@ -314,7 +327,7 @@ class GatedScan(_Handle):
     def step(self, z, h, out_h=None, out_y=None, stream=None):
         """One step of any number of rows: z [R, 3H], h float32 [R, H]; returns (y [R, H], h).
         out_h may be h itself."""
-        import torch
+        torch = _torch
         R, H = h.shape[0], self.H
         _check("z", z, self._et, (R, 3 * H))
         _check("h", h, torch.float32, (R, H))
@@ -344,7 +357,7 @@ class TokenEmbed(_Handle):
         self.handle = lstm_dyn_embed_create(B, T_max, V, D, self.dtype)
 
     def _tokens(self, tokens, lengths):
-        import torch
+        torch = _torch
         _check("tokens", tokens, torch.int32, (self.B, self.T))
         if lengths is None:
             return 0
@@ -352,7 +365,7 @@ class TokenEmbed(_Handle):
         return lengths.data_ptr()
 
     def forward(self, tokens, lengths, table, out_x=None, stream=None):
-        import torch
+        torch = _torch
         L = self._tokens(tokens, lengths)
         _check("table", table, self._et, (self.V, self.D))
         if out_x is None:
@@ -368,7 +381,7 @@ class TokenEmbed(_Handle):
     def backward(self, tokens, lengths, dx, out=None, stream=None):
         """d_table float32 [V, D] (rows of tokens that do not occur are zero) from dx [B, T_max, D],
         float32 (as ``LstmDyn.backward`` gives it) or bfloat16."""
-        import torch
+        torch = _torch
         L = self._tokens(tokens, lengths)
         code = BF16 if isinstance(dx, torch.Tensor) and dx.dtype == torch.bfloat16 else F32
         _check("dx", dx, torch.bfloat16 if code == BF16 else torch.float32, (self.B, self.T, self.D))
@@ -393,7 +406,7 @@ class AdamW(_Handle):
 
     def __init__(self, params, copies=None, state_bits: int = 32, betas=(0.9, 0.999), eps: float = 1e-8,
                  weight_decay=0.01, steps_done: int = 0):
-        import torch
+        torch = _t()
         self.params = list(params)
         self.copies = list(copies) if copies is not None else [None] * len(self.params)
         if not self.params or len(self.copies) != len(self.params):
@@ -438,7 +451,7 @@ class AdamW(_Handle):
     def step(self, grads, lr: float, grad_scale: float = 1.0, stream=None):
         """One step from the gradients (all float32 or all bfloat16, in the parameters' shapes), each
         times grad_scale.  The step's number is a value of the call: a captured call repeats it."""
-        import torch
+        torch = _torch
         grads = list(grads)
         if len(grads) != len(self.params):
             raise ValueError(f"{len(self.params)} gradients are needed, got {len(grads)}")
@@ -457,7 +470,7 @@ class AdamW(_Handle):
         themselves; or with 8 bits (m, sqrt(v)) as bfloat16, which holds their values exactly."""
         if self.bits == 32:
             return self.m, self.v
-        import torch
+        torch = _torch
         m = [torch.empty(p.shape, dtype=torch.bfloat16, device=p.device) for p in self.params]
         v = [torch.empty_like(x) for x in m]
         lstm_dyn_adamw_states(self.handle, self._pointers(*[x.data_ptr() for x in m]),
@@ -484,7 +497,7 @@ class BeamSearch(_Handle):
         uint8 [B, K], states: tensors [B, K, ...] of any type (at most 8).  Returns
         (scores, parent int32, token int32, finished, states), all new, the states
         in out_states if given."""
-        import torch
+        torch = _torch
         B, K = self.B, self.K
         _check("logits", logits, self._et, (B, K, self.V))
         _check("scores", scores, torch.float32, (B, K))
@@ -497,17 +510,15 @@ class BeamSearch(_Handle):
             raise ValueError("out_states must be as many as states")
         rows = (BeamState * len(states))() if states else None
         for i, (s, d) in enumerate(zip(states, out_states)):
-            _check(f"states[{i}]", s, s.dtype, s.shape)
-            _check(f"out_states[{i}]", d, s.dtype, s.shape)
-            if s.shape[:2] != (B, K):
-                raise ValueError(f"states[{i}] must have shape ({B}, {K}, ...), got {tuple(s.shape)}")
-            rows[i] = (s.data_ptr(), d.data_ptr(), s.numel() // (B * K) * s.element_size())
-        dev = logits.device
-        out_scores = torch.empty((B, K), dtype=torch.float32, device=dev)
-        parent = torch.empty((B, K), dtype=torch.int32, device=dev)
-        token = torch.empty((B, K), dtype=torch.int32, device=dev)
-        done = torch.empty((B, K), dtype=torch.uint8, device=dev)
+            shape = s.shape
+            _check("a state", s, s.dtype, shape)
+            _check("a state's output", d, s.dtype, shape)
+            if shape[:2] != (B, K):
+                raise ValueError(f"states[{i}] must have shape ({B}, {K}, ...), got {tuple(shape)}")
+            rows[i] = (s.data_ptr(), d.data_ptr(), s.nbytes // (B * K))
+        out_scores, done = torch.empty_like(scores), torch.empty_like(finished)
+        parent, token = torch.empty_like(scores, dtype=torch.int32), torch.empty_like(scores, dtype=torch.int32)
         lstm_dyn_beam_step(self.handle, logits.data_ptr(), scores.data_ptr(), finished.data_ptr(), self.end,
                            out_scores.data_ptr(), parent.data_ptr(), token.data_ptr(), done.data_ptr(),
-                           rows, len(states), _stream(stream, dev))
+                           rows, len(states), _stream(stream, logits.device))
         return out_scores, parent, token, done, out_states
