@@ -16,9 +16,11 @@
 namespace ldyn {
 namespace {
 
-constexpr int SORT_THREADS = 256, SORT_WAVES = 4, SORT_ITEMS = 8;
-constexpr int SORT_TILE = SORT_THREADS * SORT_ITEMS;
+constexpr int SORT_THREADS = 512, SORT_WAVES = SORT_THREADS / 64, SORT_ITEMS = 16;
+constexpr int SORT_TILE = SORT_THREADS * SORT_ITEMS;  // places ranked at once
 constexpr int SORT_BITS = 9, SORT_BINS = 1 << SORT_BITS;
+constexpr int SORT_BLOCKS = 256;  // at most; each reads the counts of all
+static_assert(SORT_BINS == SORT_THREADS, "a thread per digit");
 
 struct EmbedParams {
     const int32_t* tokens;
@@ -76,110 +78,180 @@ struct SortPass {
     uint32_t* key_out;
     uint32_t* pos_out;
     int shift, bits, blocks;
+    int span;                // places of a block, a multiple of SORT_TILE
 };
 
 __device__ inline uint32_t sort_key(const EmbedParams& p, const SortPass& s, int n, bool report) {
     return s.key_in ? s.key_in[n] : key_of(p, n, report);
 }
 
-__global__ void __launch_bounds__(SORT_THREADS) sort_hist_kernel(EmbedParams p, SortPass s) {
-    __shared__ uint32_t cnt[SORT_BINS];
-    const int bins = 1 << s.bits;
-    for (int i = threadIdx.x; i < bins; i += SORT_THREADS) cnt[i] = 0;
-    __syncthreads();
-    const uint32_t now = *p.epoch + 1;
+// Ranks a wave's items among equal digits: 64 at a time, the lanes of a digit
+// told apart by one ballot per bit, the wave's count of the digit in LDS.
+template <int ITEMS>
+__device__ inline void rank_items(const uint32_t* key, const bool* on, int items, int shift, int bits, uint32_t* cnt,
+                                  uint32_t* rank) {
+    const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int j = 0; j < SORT_ITEMS; ++j) {
-        const int n = blockIdx.x * SORT_TILE + j * SORT_THREADS + threadIdx.x;
-        if (n >= p.N) break;
-        const uint32_t k = sort_key(p, s, n, true);
-        if (!s.key_in && k < (uint32_t)p.V) p.stamp[k] = now;
-        atomicAdd(&cnt[(k >> s.shift) & (bins - 1)], 1u);
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < bins; i += SORT_THREADS) p.hist[(long)blockIdx.x * bins + i] = cnt[i];
-}
-
-// Places of a block go behind those of smaller digits and of earlier blocks;
-// within the block in order (each wave holds a run of places and counts its
-// own digits, 64 places at a time).
-__global__ void __launch_bounds__(SORT_THREADS) sort_scatter_kernel(EmbedParams p, SortPass s) {
-    __shared__ uint32_t cnt[SORT_WAVES][SORT_BINS];
-    __shared__ uint32_t wsum[SORT_WAVES];
-    const int bins = 1 << s.bits, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    if (!s.key_in && blockIdx.x == 0 && threadIdx.x == 0) *p.epoch += 1;  // the stamps' reader comes later
-    for (int i = threadIdx.x; i < SORT_WAVES * SORT_BINS; i += SORT_THREADS) (&cnt[0][0])[i] = 0;
-    __syncthreads();
-
-    uint32_t key[SORT_ITEMS], rank[SORT_ITEMS];
-    const int first = blockIdx.x * SORT_TILE + w * 64 * SORT_ITEMS + lane;
-#pragma unroll
-    for (int j = 0; j < SORT_ITEMS; ++j) {
-        const int n = first + j * 64;
-        const bool on = n < p.N;
-        key[j] = on ? sort_key(p, s, n, false) : 0;
-        const uint32_t d = (key[j] >> s.shift) & (bins - 1);
-        unsigned long long peers = __ballot(on);
-        for (int bit = 0; bit < s.bits; ++bit) {
+    for (int j = 0; j < ITEMS; ++j) {
+        if (j >= items) break;
+        const uint32_t d = (key[j] >> shift) & ((1u << bits) - 1);
+        unsigned long long peers = __ballot(on[j]);
+        for (int bit = 0; bit < bits; ++bit) {
             const unsigned long long m = __ballot((d >> bit) & 1);
             peers &= (d >> bit) & 1 ? m : ~m;
         }
         const int before = __popcll(peers & ((1ull << lane) - 1));
         uint32_t old = 0;
-        if (on && before == 0) old = atomicAdd(&cnt[w][d], (uint32_t)__popcll(peers));
-        old = __shfl(old, on ? __ffsll(peers) - 1 : lane);
+        if (on[j] && before == 0) old = atomicAdd(&cnt[d], (uint32_t)__popcll(peers));
+        old = __shfl(old, on[j] ? __ffsll(peers) - 1 : lane);
         rank[j] = old + before;
     }
-    // the start of each digit: its total over all blocks, scanned; plus earlier blocks' counts
-    constexpr int PER = SORT_BINS / SORT_THREADS;
-    uint32_t total[PER], mine[PER], sum = 0;
-#pragma unroll
-    for (int q = 0; q < PER; ++q) {
-        const int d = threadIdx.x * PER + q;
-        uint32_t t = 0, m = 0;
-        if (d < bins) {
-#pragma unroll 8
-            for (int b = 0; b < s.blocks; ++b) {
-                const uint32_t c = p.hist[(long)b * bins + d];
-                t += c;
-                m += b < (int)blockIdx.x ? c : 0;
-            }
-        }
-        total[q] = t;
-        mine[q] = m;
-        sum += t;
-    }
-    uint32_t incl = sum;
+}
+
+// The sum of x over the workgroup's threads before this one.
+__device__ inline uint32_t sum_before(uint32_t x, uint32_t* wsum) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    uint32_t incl = x;
     for (int o = 1; o < 64; o <<= 1) {
         const uint32_t u = __shfl_up(incl, o);
         if (lane >= o) incl += u;
     }
     if (lane == 63) wsum[w] = incl;
     __syncthreads();
-    uint32_t run = incl - sum;
+    uint32_t run = incl - x;
     for (int i = 0; i < w; ++i) run += wsum[i];
-#pragma unroll
-    for (int q = 0; q < PER; ++q) {
-        const int d = threadIdx.x * PER + q;
-        if (d < bins) {
-            uint32_t at = run + mine[q];
-            for (int i = 0; i < SORT_WAVES; ++i) {
-                const uint32_t c = cnt[i][d];
-                cnt[i][d] = at;
-                at += c;
-            }
-        }
-        run += total[q];
+    return run;
+}
+
+__global__ void __launch_bounds__(SORT_THREADS) sort_hist_kernel(EmbedParams p, SortPass s) {
+    __shared__ uint32_t cnt[SORT_BINS];
+    const int bins = 1 << s.bits;
+    cnt[threadIdx.x] = 0;
+    __syncthreads();
+    const uint32_t now = *p.epoch + 1;
+    const int first = blockIdx.x * s.span, end = min(p.N, first + s.span);
+#pragma unroll 8
+    for (int n = first + threadIdx.x; n < end; n += SORT_THREADS) {
+        const uint32_t k = sort_key(p, s, n, true);
+        if (!s.key_in && k < (uint32_t)p.V) p.stamp[k] = now;
+        atomicAdd(&cnt[(k >> s.shift) & (bins - 1)], 1u);
     }
     __syncthreads();
+    if ((int)threadIdx.x < bins) p.hist[(long)blockIdx.x * bins + threadIdx.x] = cnt[threadIdx.x];
+}
+
+// Places of a block go behind those of smaller digits and of earlier blocks;
+// within the block in order (each wave holds a run of places).  Every block
+// adds up all blocks' counts itself: 32 blocks at 256 K places, 64 KB.
+__global__ void __launch_bounds__(SORT_THREADS) sort_scatter_kernel(EmbedParams p, SortPass s) {
+    __shared__ uint32_t cnt[SORT_WAVES][SORT_BINS];
+    __shared__ uint32_t wsum[SORT_WAVES];
+    const int bins = 1 << s.bits, lane = threadIdx.x & 63, w = threadIdx.x >> 6, d = threadIdx.x;
+    if (!s.key_in && blockIdx.x == 0 && threadIdx.x == 0) *p.epoch += 1;  // the stamps' reader comes later
+    uint32_t total = 0, earlier = 0;
+    if (d < bins) {
+#pragma unroll 16
+        for (int b = 0; b < s.blocks; ++b) {
+            const uint32_t c = p.hist[(long)b * bins + d];
+            total += c;
+            earlier += b < (int)blockIdx.x ? c : 0;
+        }
+    }
+    uint32_t base = sum_before(total, wsum) + earlier;  // where this block's next place of digit d goes
+    const int end = min(p.N, (int)(blockIdx.x + 1) * s.span);
+    for (int tile = blockIdx.x * s.span; tile < end; tile += SORT_TILE) {
+        for (int i = threadIdx.x; i < SORT_WAVES * SORT_BINS; i += SORT_THREADS) (&cnt[0][0])[i] = 0;
+        __syncthreads();
+        uint32_t key[SORT_ITEMS], rank[SORT_ITEMS];
+        bool on[SORT_ITEMS];
+        const int first = tile + w * 64 * SORT_ITEMS + lane;
+#pragma unroll
+        for (int j = 0; j < SORT_ITEMS; ++j) {
+            on[j] = first + j * 64 < end;
+            key[j] = on[j] ? sort_key(p, s, first + j * 64, false) : 0;
+        }
+        rank_items<SORT_ITEMS>(key, on, SORT_ITEMS, s.shift, s.bits, cnt[w], rank);
+        __syncthreads();
+        if (d < bins)
+            for (int i = 0; i < SORT_WAVES; ++i) {
+                const uint32_t c = cnt[i][d];
+                cnt[i][d] = base;
+                base += c;
+            }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < SORT_ITEMS; ++j) {
+            if (!on[j]) continue;
+            const int n = first + j * 64;
+            const uint32_t at = cnt[w][(key[j] >> s.shift) & (bins - 1)] + rank[j];
+            s.key_out[at] = key[j];
+            s.pos_out[at] = s.pos_in ? s.pos_in[n] : (uint32_t)n;
+        }
+        __syncthreads();
+    }
+}
+
+// All passes in one workgroup, for at most SORT_TILE places: the order is
+// exchanged through LDS between the passes.
+__global__ void __launch_bounds__(SORT_THREADS)
+sort_small_kernel(EmbedParams p, uint32_t* key_out, uint32_t* pos_out, int passes, int bits) {
+    __shared__ uint32_t cnt[SORT_WAVES][SORT_BINS];
+    __shared__ uint32_t wsum[SORT_WAVES];
+    __shared__ uint32_t skey[SORT_TILE];
+    __shared__ uint16_t spos[SORT_TILE];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, bins = 1 << bits, d = threadIdx.x;
+    const int items = (p.N + SORT_THREADS - 1) / SORT_THREADS;  // of a thread
+    const int first = w * 64 * items + lane;
+    const uint32_t now = *p.epoch + 1;
+    uint32_t key[SORT_ITEMS], pos[SORT_ITEMS], rank[SORT_ITEMS];
+    bool on[SORT_ITEMS];
 #pragma unroll
     for (int j = 0; j < SORT_ITEMS; ++j) {
         const int n = first + j * 64;
-        if (n >= p.N) continue;
-        const uint32_t at = cnt[w][(key[j] >> s.shift) & (bins - 1)] + rank[j];
-        s.key_out[at] = key[j];
-        s.pos_out[at] = s.pos_in ? s.pos_in[n] : (uint32_t)n;
+        on[j] = j < items && n < p.N;
+        key[j] = 0;
+        pos[j] = (uint32_t)n;
+        if (!on[j]) continue;
+        key[j] = key_of(p, n, true);
+        if (key[j] < (uint32_t)p.V) p.stamp[key[j]] = now;
     }
+    for (int pass = 0; pass < passes; ++pass) {
+        for (int i = threadIdx.x; i < SORT_WAVES * SORT_BINS; i += SORT_THREADS) (&cnt[0][0])[i] = 0;
+        __syncthreads();
+        rank_items<SORT_ITEMS>(key, on, items, pass * bits, bits, cnt[w], rank);
+        __syncthreads();
+        uint32_t total = 0;
+        for (int i = 0; i < SORT_WAVES; ++i) total += cnt[i][d];
+        uint32_t base = sum_before(total, wsum);
+        for (int i = 0; i < SORT_WAVES; ++i) {
+            const uint32_t c = cnt[i][d];
+            cnt[i][d] = base;
+            base += c;
+        }
+        __syncthreads();
+        const bool last = pass == passes - 1;
+#pragma unroll
+        for (int j = 0; j < SORT_ITEMS; ++j) {
+            if (!on[j]) continue;
+            const uint32_t at = cnt[w][(key[j] >> (pass * bits)) & (bins - 1)] + rank[j];
+            if (last) {
+                key_out[at] = key[j];
+                pos_out[at] = pos[j];
+            } else {
+                skey[at] = key[j];
+                spos[at] = (uint16_t)pos[j];
+            }
+        }
+        __syncthreads();
+        if (last) break;
+#pragma unroll
+        for (int j = 0; j < SORT_ITEMS; ++j) {
+            if (!on[j]) continue;
+            key[j] = skey[first + j * 64];
+            pos[j] = spos[first + j * 64];
+        }
+    }
+    if (threadIdx.x == 0) *p.epoch = now;
 }
 
 // --- sums over sorted places --------------------------------------------------------
@@ -338,10 +410,23 @@ using namespace ldyn;
 
 struct lstm_dyn_embed : OpsHandle {
     int B, T, V, D, dtype;
-    int N, passes, bits, blocks, R, pieces;
+    int N, passes, bits, blocks, span;
+    int W, tiles, R, pieces;  // columns of a lane, column tiles of a row; places of a piece
     uint32_t *epoch, *stamp, *hist, *key[2], *pos[2];
     float* part;
 };
+
+// Pieces of up to 64 places, shorter where they would leave fewer than eight
+// waves a CU on the gradient (945 places of 333 columns: 16 us with 64, DDDD us with 8).
+static void embed_shape(lstm_dyn_embed* h) {
+    int dev = 0, cus = 256;
+    if (hipGetDevice(&dev) == hipSuccess)
+        (void)hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
+    h->W = h->D % 4 == 0 ? 4 : h->D % 2 == 0 ? 2 : 1;
+    h->tiles = (h->D + 64 * h->W - 1) / (64 * h->W);
+    h->R = 64;
+    while (h->R > 8 && (long long)h->N / h->R * h->tiles < 8LL * cus) h->R /= 2;
+}
 
 extern "C" int lstm_dyn_check_embed_args(int B, int T, int V, int D, int dtype,
                                          const int32_t* tokens, const int32_t* lengths,
@@ -367,8 +452,11 @@ extern "C" int lstm_dyn_embed_create(lstm_dyn_embed_t** out, int B, int T, int V
     while ((1LL << bits) < (long long)V + 1) ++bits;
     h->passes = (bits + SORT_BITS - 1) / SORT_BITS;
     h->bits = (bits + h->passes - 1) / h->passes;
-    h->blocks = (int)((N + SORT_TILE - 1) / SORT_TILE);
-    h->R = 64;
+    // tiles of places, shared out over at most SORT_BLOCKS blocks
+    const long long tiles = (N + SORT_TILE - 1) / SORT_TILE, each = (tiles + SORT_BLOCKS - 1) / SORT_BLOCKS;
+    h->span = (int)(each * SORT_TILE);
+    h->blocks = (int)((N + h->span - 1) / h->span);
+    embed_shape(h);
     h->pieces = (int)((N + h->R - 1) / h->R);
     long long at = 256;
     auto take = [&](long long n) {
@@ -417,6 +505,7 @@ extern "C" int lstm_dyn_embed_forward(lstm_dyn_embed_t* h, const int32_t* tokens
         else LDYN_EMB(__bf16, 1);
     } else {
         if (h->D % 4 == 0) LDYN_EMB(float, 4);
+        else if (h->D % 2 == 0) LDYN_EMB(float, 2);
         else LDYN_EMB(float, 1);
     }
 #undef LDYN_EMB
@@ -432,16 +521,21 @@ extern "C" int lstm_dyn_embed_backward(lstm_dyn_embed_t* h, const int32_t* token
     if ((rc = ops_begin(h, stream)) != LSTM_DYN_OK) return rc;
     const EmbedParams p = embed_params(h, tokens, lengths, scale);
     int in = 0;
-    for (int i = 0; i < h->passes; ++i, in ^= 1) {
-        const SortPass s{i ? h->key[in] : nullptr, i ? h->pos[in] : nullptr, h->key[in ^ 1],
-                         h->pos[in ^ 1], i * h->bits, h->bits, h->blocks};
-        hipLaunchKernelGGL(sort_hist_kernel, dim3(h->blocks), dim3(SORT_THREADS), 0, h->last_stream, p, s);
+    if (h->blocks == 1) {
+        hipLaunchKernelGGL(sort_small_kernel, dim3(1), dim3(SORT_THREADS), 0, h->last_stream, p, h->key[0],
+                           h->pos[0], h->passes, h->bits);
         if ((rc = ops_launched(h)) != LSTM_DYN_OK) return rc;
-        hipLaunchKernelGGL(sort_scatter_kernel, dim3(h->blocks), dim3(SORT_THREADS), 0, h->last_stream, p, s);
-        if ((rc = ops_launched(h)) != LSTM_DYN_OK) return rc;
+    } else {
+        for (int i = 0; i < h->passes; ++i, in ^= 1) {
+            const SortPass s{i ? h->key[in] : nullptr, i ? h->pos[in] : nullptr, h->key[in ^ 1],
+                             h->pos[in ^ 1], i * h->bits, h->bits, h->blocks, h->span};
+            hipLaunchKernelGGL(sort_hist_kernel, dim3(h->blocks), dim3(SORT_THREADS), 0, h->last_stream, p, s);
+            if ((rc = ops_launched(h)) != LSTM_DYN_OK) return rc;
+            hipLaunchKernelGGL(sort_scatter_kernel, dim3(h->blocks), dim3(SORT_THREADS), 0, h->last_stream, p, s);
+            if ((rc = ops_launched(h)) != LSTM_DYN_OK) return rc;
+        }
     }
-    const int W = h->D % 4 ? 1 : 4;
-    const int tiles = (h->D + 64 * W - 1) / (64 * W);
+    const int W = h->W, tiles = h->tiles;
     const long zero_waves = h->V < 8L * h->num_cus ? h->V : 8L * h->num_cus;
     const long waves = (long)h->pieces * tiles + zero_waves;
     const unsigned grid = (unsigned)((waves + 3) / 4);
@@ -451,19 +545,18 @@ extern "C" int lstm_dyn_embed_backward(lstm_dyn_embed_t* h, const int32_t* token
                        tiles)
     if (dx_dtype == LSTM_DYN_BF16) {
         if (W == 4) LDYN_SUM(__bf16, 4);
+        else if (W == 2) LDYN_SUM(__bf16, 2);
         else LDYN_SUM(__bf16, 1);
     } else {
         if (W == 4) LDYN_SUM(float, 4);
+        else if (W == 2) LDYN_SUM(float, 2);
         else LDYN_SUM(float, 1);
     }
 #undef LDYN_SUM
     if ((rc = ops_launched(h)) != LSTM_DYN_OK || h->pieces < 2) return rc;
-    if (W == 4)
-        hipLaunchKernelGGL((embed_join_kernel<4>), dim3(h->pieces - 1, tiles), dim3(256), 0,
-                           h->last_stream, p, h->key[in], d_table, h->R, h->pieces);
-    else
-        hipLaunchKernelGGL((embed_join_kernel<1>), dim3(h->pieces - 1, tiles), dim3(256), 0,
-                           h->last_stream, p, h->key[in], d_table, h->R, h->pieces);
+    auto* join = W == 4 ? embed_join_kernel<4> : W == 2 ? embed_join_kernel<2> : embed_join_kernel<1>;
+    hipLaunchKernelGGL(join, dim3(h->pieces - 1, tiles), dim3(256), 0, h->last_stream, p, h->key[in],
+                       d_table, h->R, h->pieces);
     return ops_launched(h);
 }
 
