@@ -16,9 +16,10 @@
 namespace ldyn {
 namespace {
 
-constexpr int SORT_THREADS = 512, SORT_WAVES = SORT_THREADS / 64, SORT_ITEMS = 16;
+constexpr int SORT_THREADS = 512, SORT_WAVES = SORT_THREADS / 64, SORT_ITEMS = 8;
 constexpr int SORT_TILE = SORT_THREADS * SORT_ITEMS;  // places ranked at once
 constexpr int SORT_BITS = 9, SORT_BINS = 1 << SORT_BITS;
+constexpr long long LAST_CACHE = 256LL << 20;
 constexpr int SORT_BLOCKS = 256;  // at most; each reads the counts of all
 static_assert(SORT_BINS == SORT_THREADS, "a thread per digit");
 
@@ -34,12 +35,13 @@ struct EmbedParams {
     float scale;
 };
 
-// The sort key of place n: its token, or V.
+// The sort key of place n: its token, or V.  Length and token are loaded side
+// by side: the token of a place past the length lies in the array all the same.
 __device__ inline uint32_t key_of(const EmbedParams& p, int n, bool report) {
     const int b = n / p.T, t = n - b * p.T;
+    const int tok = p.tokens[n];
     const int L = row_length(p.lengths, b, p.T, p.status, report && t == 0);
     if (t >= L) return (uint32_t)p.V;
-    const int tok = p.tokens[n];
     if ((unsigned)tok < (unsigned)p.V) return (uint32_t)tok;
     if (report) atomicOr(p.status, STATUS_BAD_TOKENS);
     return (uint32_t)p.V;
@@ -47,7 +49,21 @@ __device__ inline uint32_t key_of(const EmbedParams& p, int n, bool report) {
 
 // --- lookup: one wave per row ---------------------------------------------------
 
-template <class E, int W>
+template <bool NT, class E, int W>
+__device__ inline void put(E* p, const float* in) {
+    typename Vec<E, W>::type x;
+    if constexpr (W == 1) {
+        x = (E)in[0];
+    } else {
+#pragma unroll
+        for (int i = 0; i < W; ++i) x[i] = (E)in[i];
+    }
+    auto* q = reinterpret_cast<typename Vec<E, W>::type*>(p);
+    if constexpr (NT) __builtin_nontemporal_store(x, q);
+    else *q = x;
+}
+
+template <bool NT, class E, int W>
 __global__ void __launch_bounds__(256)
 embed_forward_kernel(EmbedParams p, const E* __restrict__ table, E* __restrict__ x) {
     const int lane = threadIdx.x & 63;
@@ -65,7 +81,7 @@ embed_forward_kernel(EmbedParams p, const E* __restrict__ table, E* __restrict__
 #pragma unroll
                 for (int i = 0; i < W; ++i) q[i] = 0.0f;
             }
-            store_vec<E, W>(dst + c, q);
+            put<NT, E, W>(dst + c, q);
         }
     }
 }
@@ -130,11 +146,19 @@ __global__ void __launch_bounds__(SORT_THREADS) sort_hist_kernel(EmbedParams p, 
     __syncthreads();
     const uint32_t now = *p.epoch + 1;
     const int first = blockIdx.x * s.span, end = min(p.N, first + s.span);
-#pragma unroll 8
-    for (int n = first + threadIdx.x; n < end; n += SORT_THREADS) {
-        const uint32_t k = sort_key(p, s, n, true);
-        if (!s.key_in && k < (uint32_t)p.V) p.stamp[k] = now;
-        atomicAdd(&cnt[(k >> s.shift) & (bins - 1)], 1u);
+    for (int tile = first; tile < end; tile += SORT_TILE) {
+        uint32_t key[SORT_ITEMS];
+#pragma unroll
+        for (int j = 0; j < SORT_ITEMS; ++j) {
+            const int n = tile + j * SORT_THREADS + (int)threadIdx.x;
+            key[j] = n < end ? sort_key(p, s, n, true) : ~0u;
+        }
+#pragma unroll
+        for (int j = 0; j < SORT_ITEMS; ++j) {
+            if (key[j] == ~0u) continue;
+            if (!s.key_in && key[j] < (uint32_t)p.V) p.stamp[key[j]] = now;
+            atomicAdd(&cnt[(key[j] >> s.shift) & (bins - 1)], 1u);
+        }
     }
     __syncthreads();
     if ((int)threadIdx.x < bins) p.hist[(long)blockIdx.x * bins + threadIdx.x] = cnt[threadIdx.x];
@@ -256,20 +280,20 @@ sort_small_kernel(EmbedParams p, uint32_t* key_out, uint32_t* pos_out, int passe
 
 // --- sums over sorted places --------------------------------------------------------
 
-// Waves below `pieces * tiles`: piece w / tiles, columns of tile w % tiles (64 W
-// of them).  The waves after them write the zeros.
+// The first `zero_waves` waves write the zeros; beside them the others sum: piece
+// w / tiles, columns of tile w % tiles (64 W of them).
 template <class E, int W>
 __global__ void __launch_bounds__(256)
 embed_sum_kernel(EmbedParams p, const uint32_t* __restrict__ key, const uint32_t* __restrict__ pos,
-                 const E* __restrict__ dx, float* __restrict__ dt, int R, int pieces, int tiles) {
+                 const E* __restrict__ dx, float* __restrict__ dt, int R, int pieces, int tiles,
+                 int zero_waves) {
     const int lane = threadIdx.x & 63;
-    const long w = blockIdx.x * 4L + (threadIdx.x >> 6);
-    const long sums = (long)pieces * tiles;
-    if (w >= sums) {
+    const long w = blockIdx.x * 4L + (threadIdx.x >> 6) - zero_waves;
+    if (w >= (long)pieces * tiles) return;
+    if (w < 0) {
         const uint32_t now = *p.epoch;
-        const long waves = gridDim.x * 4L - sums;
         float zero[W] = {};
-        for (long v = w - sums; v < p.V; v += waves) {
+        for (long v = w + zero_waves; v < p.V; v += zero_waves) {
             if (p.stamp[v] == now) continue;
             for (int c = lane * W; c < p.D; c += 64 * W) store_vec<float, W>(dt + v * p.D + c, zero);
         }
@@ -328,53 +352,83 @@ embed_sum_kernel(EmbedParams p, const uint32_t* __restrict__ key, const uint32_t
     if (cur != V) close(after == cur);
 }
 
-// The tokens whose places span pieces: one workgroup per piece in which such
-// a token begins and per column tile, its waves a run of the partial sums each.
+// acc += the slots 0 of pieces [lo, hi), in order.
+template <int W>
+__device__ inline void add_parts(const EmbedParams& p, int lo, int hi, int c, float* acc) {
+    constexpr int U = 16;  // in flight, also the last few
+    for (int i0 = lo; i0 < hi; i0 += U) {
+        float q[U][W];
+#pragma unroll
+        for (int u = 0; u < U; ++u) load_vec<float, W>(p.part + (long)min(i0 + u, hi - 1) * 2 * p.D + c, q[u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < W; ++j) acc[j] += i0 + u < hi ? q[u][j] : 0.0f;
+    }
+}
+
+// The tokens whose places span pieces, one column tile: a wave takes the token
+// that begins in its piece and goes on, if there is one.  One with more than LONG parts
+// is shared out over the workgroup's waves.
 template <int W>
 __global__ void __launch_bounds__(256)
 embed_join_kernel(EmbedParams p, const uint32_t* __restrict__ key, float* __restrict__ dt, int R,
                   int pieces) {
+    constexpr int LONG = 32;
     __shared__ float sum[4][64 * W];
-    const int piece = blockIdx.x, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    __shared__ int parts_of[4];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, piece = blockIdx.x * 4 + w;
     const int c = blockIdx.y * 64 * W + lane * W;
-    const int end = (piece + 1) * R;
-    const uint32_t v = end < p.N ? key[end] : (uint32_t)p.V;
-    if (v == (uint32_t)p.V || key[end - 1] != v) return;
-    if (piece > 0 && key[piece * R] == v && key[piece * R - 1] == v) return;  // begins earlier
-    // the last piece with a place of v: whole pieces 64 at a time
-    int last = piece + 1;
-    for (;;) {
-        const long at = (long)(last + lane + 1) * R;  // the place after piece last + lane
-        const unsigned long long goes = __ballot(at < p.N && key[min(at, (long)p.N - 1)] == v);
-        const int whole = goes == ~0ull ? 64 : __ffsll(~goes) - 1;
-        last += whole;
-        if (whole < 64) break;
-    }
-    const int parts = last - piece;  // in slot 0 of pieces piece + 1 .. last
-    const int per = (parts + 3) / 4, lo = min(parts, w * per), hi = min(parts, lo + per);
     const bool on = c < p.D;
-    float acc[W] = {};
-    if (on) {
-        if (w == 0) load_vec<float, W>(p.part + ((long)piece * 2 + 1) * p.D + c, acc);
-#pragma unroll 8
-        for (int i = lo; i < hi; ++i) {
-            float q[W];
-            load_vec<float, W>(p.part + (long)(piece + 1 + i) * 2 * p.D + c, q);
-#pragma unroll
-            for (int j = 0; j < W; ++j) acc[j] += q[j];
+    int parts = 0;  // in slot 0 of the pieces after this one
+    const long end = (long)(piece + 1) * R;
+    const uint32_t V = (uint32_t)p.V, v = piece < pieces && end < p.N ? key[end] : V;
+    if (v != V && key[end - 1] == v && !(piece > 0 && key[end - R] == v && key[end - R - 1] == v)) {
+        // whole pieces 64 at a time
+        parts = 1;
+        for (;;) {
+            const long at = end + (long)(parts + lane) * R;  // the place after piece + parts + lane
+            const unsigned long long goes = __ballot(at < p.N && key[min(at, (long)p.N - 1)] == v);
+            const int whole = goes == ~0ull ? 64 : __ffsll(~goes) - 1;
+            parts += whole;
+            if (whole < 64) break;
         }
     }
+    auto write = [&](const float* acc) {
+        float o[W];
 #pragma unroll
-    for (int j = 0; j < W; ++j) sum[w][lane * W + j] = acc[j];
+        for (int j = 0; j < W; ++j) o[j] = acc[j] * p.scale;
+        store_vec<float, W>(dt + (long)key[(long)piece * R + R] * p.D + c, o);
+    };
+    if (parts > 0 && parts <= LONG && on) {
+        float acc[W];
+        load_vec<float, W>(p.part + ((long)piece * 2 + 1) * p.D + c, acc);
+        add_parts<W>(p, piece + 1, piece + 1 + parts, c, acc);
+        write(acc);
+    }
+    if (lane == 0) parts_of[w] = parts;
     __syncthreads();
-    if (w == 0 && on) {
-#pragma unroll
-        for (int j = 0; j < W; ++j) {
-            float a = acc[j];
-            for (int i = 1; i < 4; ++i) a += sum[i][lane * W + j];
-            acc[j] = a * p.scale;
+    for (int i = 0; i < 4; ++i) {
+        const int n = parts_of[i], from = blockIdx.x * 4 + i;
+        if (n <= LONG) continue;
+        const int per = (n + 3) / 4, lo = min(n, w * per), hi = min(n, lo + per);
+        float acc[W] = {};
+        if (on) {
+            if (w == 0) load_vec<float, W>(p.part + ((long)from * 2 + 1) * p.D + c, acc);
+            add_parts<W>(p, from + 1 + lo, from + 1 + hi, c, acc);
         }
-        store_vec<float, W>(dt + (long)v * p.D + c, acc);
+#pragma unroll
+        for (int j = 0; j < W; ++j) sum[w][lane * W + j] = acc[j];
+        __syncthreads();
+        if (w == i && on) {
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+                acc[j] = sum[0][lane * W + j];
+                for (int q = 1; q < 4; ++q) acc[j] += sum[q][lane * W + j];
+            }
+            write(acc);
+        }
+        __syncthreads();
     }
 }
 
@@ -416,15 +470,15 @@ struct lstm_dyn_embed : OpsHandle {
     float* part;
 };
 
-// Pieces of up to 64 places, shorter where they would leave fewer than eight
-// waves a CU on the gradient (945 places of 333 columns: 16 us with 64, DDDD us with 8).
+// Pieces of up to 32 places, shorter where they would leave fewer than eight
+// waves a CU on the gradient (945 places of 333 columns: 16 us with 64, 5.6 with 8).
 static void embed_shape(lstm_dyn_embed* h) {
     int dev = 0, cus = 256;
     if (hipGetDevice(&dev) == hipSuccess)
         (void)hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
     h->W = h->D % 4 == 0 ? 4 : h->D % 2 == 0 ? 2 : 1;
     h->tiles = (h->D + 64 * h->W - 1) / (64 * h->W);
-    h->R = 64;
+    h->R = 32;
     while (h->R > 8 && (long long)h->N / h->R * h->tiles < 8LL * cus) h->R /= 2;
 }
 
@@ -495,10 +549,14 @@ extern "C" int lstm_dyn_embed_forward(lstm_dyn_embed_t* h, const int32_t* tokens
     if ((rc = ops_begin(h, stream)) != LSTM_DYN_OK) return rc;
     const EmbedParams p = embed_params(h, tokens, lengths, scale);
     long grid = ((long)h->N + 3) / 4;
-    if (grid > 16L * h->num_cus) grid = 16L * h->num_cus;
-#define LDYN_EMB(E, W)                                                                              \
-    hipLaunchKernelGGL((embed_forward_kernel<E, W>), dim3((unsigned)grid), dim3(256), 0,            \
-                       h->last_stream, p, static_cast<const E*>(table), static_cast<E*>(out_x))
+    if (grid > 64L * h->num_cus) grid = 64L * h->num_cus;
+    // An x larger than the last cache is read from memory by whoever comes next: its
+    // stores bypass the caches (256 x 1000 x 1024 in bf16: 138 us against 156).
+    const bool far = (long long)h->N * h->D * dtype_bytes(h->dtype) > LAST_CACHE;
+#define LDYN_EMB(E, W)                                                                               \
+    hipLaunchKernelGGL((far ? embed_forward_kernel<true, E, W> : embed_forward_kernel<false, E, W>), \
+                       dim3((unsigned)grid), dim3(256), 0, h->last_stream, p,                        \
+                       static_cast<const E*>(table), static_cast<E*>(out_x))
     if (h->dtype == LSTM_DYN_BF16) {
         if (h->D % 8 == 0) LDYN_EMB(__bf16, 8);
         else if (h->D % 2 == 0) LDYN_EMB(__bf16, 2);
@@ -536,13 +594,13 @@ extern "C" int lstm_dyn_embed_backward(lstm_dyn_embed_t* h, const int32_t* token
         }
     }
     const int W = h->W, tiles = h->tiles;
-    const long zero_waves = h->V < 8L * h->num_cus ? h->V : 8L * h->num_cus;
+    const int zero_waves = h->V < 8 * h->num_cus ? h->V : 8 * h->num_cus;
     const long waves = (long)h->pieces * tiles + zero_waves;
     const unsigned grid = (unsigned)((waves + 3) / 4);
 #define LDYN_SUM(E, W)                                                                              \
     hipLaunchKernelGGL((embed_sum_kernel<E, W>), dim3(grid), dim3(256), 0, h->last_stream, p,       \
                        h->key[in], h->pos[in], static_cast<const E*>(dx), d_table, h->R, h->pieces, \
-                       tiles)
+                       tiles, zero_waves)
     if (dx_dtype == LSTM_DYN_BF16) {
         if (W == 4) LDYN_SUM(__bf16, 4);
         else if (W == 2) LDYN_SUM(__bf16, 2);
@@ -555,7 +613,7 @@ extern "C" int lstm_dyn_embed_backward(lstm_dyn_embed_t* h, const int32_t* token
 #undef LDYN_SUM
     if ((rc = ops_launched(h)) != LSTM_DYN_OK || h->pieces < 2) return rc;
     auto* join = W == 4 ? embed_join_kernel<4> : W == 2 ? embed_join_kernel<2> : embed_join_kernel<1>;
-    hipLaunchKernelGGL(join, dim3(h->pieces - 1, tiles), dim3(256), 0, h->last_stream, p, h->key[in],
+    hipLaunchKernelGGL(join, dim3((h->pieces + 3) / 4, tiles), dim3(256), 0, h->last_stream, p, h->key[in],
                        d_table, h->R, h->pieces);
     return ops_launched(h);
 }
