@@ -329,6 +329,7 @@ static int adamw_make(lstm_dyn_adamw* h, const lstm_dyn_adamw_tensor_t* t, int c
     }
     h->first.push_back((uint32_t)owner.size());
     const long long nt = ((long long)sizeof(Tensor) * count + 255) / 256 * 256;
+    if ((rc = ops_device(h)) != LSTM_DYN_OK) return rc;
     if ((rc = ops_init(h, 256 + nt + 4LL * (long long)owner.size())) != LSTM_DYN_OK) return rc;
     h->tensors = reinterpret_cast<const Tensor*>(h->block + 256);
     h->owner = reinterpret_cast<const uint32_t*>(h->block + 256 + nt);

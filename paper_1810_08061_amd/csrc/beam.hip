@@ -511,12 +511,12 @@ struct lstm_dyn_beam : OpsHandle {
 // How a beam's logits are cut: eight loads a thread, fewer where that would
 // leave fewer than four workgroups a CU; and no more slices than can be joined in a few rounds (a
 // workgroup takes its slice in pieces then).
-static void beam_shape(lstm_dyn_beam* h, int num_cus) {
+static void beam_shape(lstm_dyn_beam* h) {
     const int quad = 16 / dtype_bytes(h->dtype);
     const long quads = ((long)h->V + quad - 1) / quad + (h->V % quad ? 1 : 0), rows = (long)h->B * h->K;
     auto slices = [&](int n) { return (quads + THREADS * n - 1) / (THREADS * n); };
     int n = 8;
-    while (n > 1 && rows * slices(n) < 4L * num_cus) n /= 2;
+    while (n > 1 && rows * slices(n) < 4L * h->num_cus) n /= 2;
     long most = 2048 / (h->K * h->K);
     if (most < 8) most = 8;
     h->hold = n;
@@ -551,14 +551,11 @@ extern "C" int lstm_dyn_beam_create(lstm_dyn_beam_t** out, int B, int K, int V, 
     lstm_dyn_beam* h = new (std::nothrow) lstm_dyn_beam();
     if (!h) return LSTM_DYN_ERR_NOMEM;
     h->B = B; h->K = K; h->V = V; h->dtype = dtype;
-    int dev = 0, cus = 0;
-    if (hipGetDevice(&dev) != hipSuccess ||
-        hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) {
-        (void)hipGetLastError();
+    if ((rc = ops_device(h)) != LSTM_DYN_OK) {
         delete h;
-        return LSTM_DYN_ERR_HIP;
+        return rc;
     }
-    beam_shape(h, cus);
+    beam_shape(h);
     const long long na = 4LL * ARRIVED_WORDS * B, ns = 8LL * B * K * h->slices;
     if ((rc = ops_init(h, 256 + na + ns + ns * K)) != LSTM_DYN_OK) {
         delete h;

@@ -19,7 +19,6 @@ namespace {
 constexpr int SORT_THREADS = 512, SORT_WAVES = SORT_THREADS / 64, SORT_ITEMS = 8;
 constexpr int SORT_TILE = SORT_THREADS * SORT_ITEMS;  // places ranked at once
 constexpr int SORT_BITS = 9, SORT_BINS = 1 << SORT_BITS;
-constexpr long long LAST_CACHE = 256LL << 20;
 constexpr int SORT_BLOCKS = 256;  // at most; each reads the counts of all
 static_assert(SORT_BINS == SORT_THREADS, "a thread per digit");
 
@@ -48,20 +47,6 @@ __device__ inline uint32_t key_of(const EmbedParams& p, int n, bool report) {
 }
 
 // --- lookup: one wave per row ---------------------------------------------------
-
-template <bool NT, class E, int W>
-__device__ inline void put(E* p, const float* in) {
-    typename Vec<E, W>::type x;
-    if constexpr (W == 1) {
-        x = (E)in[0];
-    } else {
-#pragma unroll
-        for (int i = 0; i < W; ++i) x[i] = (E)in[i];
-    }
-    auto* q = reinterpret_cast<typename Vec<E, W>::type*>(p);
-    if constexpr (NT) __builtin_nontemporal_store(x, q);
-    else *q = x;
-}
 
 template <bool NT, class E, int W>
 __global__ void __launch_bounds__(256)
@@ -473,13 +458,10 @@ struct lstm_dyn_embed : OpsHandle {
 // Pieces of up to 32 places, shorter where they would leave fewer than eight
 // waves a CU on the gradient (945 places of 333 columns: 16 us with 64, 5.6 with 8).
 static void embed_shape(lstm_dyn_embed* h) {
-    int dev = 0, cus = 256;
-    if (hipGetDevice(&dev) == hipSuccess)
-        (void)hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
     h->W = h->D % 4 == 0 ? 4 : h->D % 2 == 0 ? 2 : 1;
     h->tiles = (h->D + 64 * h->W - 1) / (64 * h->W);
     h->R = 32;
-    while (h->R > 8 && (long long)h->N / h->R * h->tiles < 8LL * cus) h->R /= 2;
+    while (h->R > 8 && (long long)h->N / h->R * h->tiles < 8LL * h->num_cus) h->R /= 2;
 }
 
 extern "C" int lstm_dyn_check_embed_args(int B, int T, int V, int D, int dtype,
@@ -500,6 +482,10 @@ extern "C" int lstm_dyn_embed_create(lstm_dyn_embed_t** out, int B, int T, int V
     lstm_dyn_embed* h = new (std::nothrow) lstm_dyn_embed();
     if (!h) return LSTM_DYN_ERR_NOMEM;
     h->B = B; h->T = T; h->V = V; h->D = D; h->dtype = dtype;
+    if ((rc = ops_device(h)) != LSTM_DYN_OK) {
+        delete h;
+        return rc;
+    }
     const long long N = (long long)B * T;
     h->N = (int)N;
     int bits = 1;
@@ -552,7 +538,7 @@ extern "C" int lstm_dyn_embed_forward(lstm_dyn_embed_t* h, const int32_t* tokens
     if (grid > 64L * h->num_cus) grid = 64L * h->num_cus;
     // An x larger than the last cache is read from memory by whoever comes next: its
     // stores bypass the caches (256 x 1000 x 1024 in bf16: 138 us against 156).
-    const bool far = (long long)h->N * h->D * dtype_bytes(h->dtype) > LAST_CACHE;
+    const bool far = (long long)h->N * h->D * dtype_bytes(h->dtype) > FAR_BYTES;
 #define LDYN_EMB(E, W)                                                                               \
     hipLaunchKernelGGL((far ? embed_forward_kernel<true, E, W> : embed_forward_kernel<false, E, W>), \
                        dim3((unsigned)grid), dim3(256), 0, h->last_stream, p,                        \

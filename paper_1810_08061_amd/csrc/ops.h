@@ -61,13 +61,19 @@ struct OpsHandle {
     int32_t* status() const { return reinterpret_cast<int32_t*>(block); }
 };
 
-inline int ops_init(OpsHandle* h, long long bytes) {
+// The current device, for a handle that is being made.
+inline int ops_device(OpsHandle* h) {
     if (hipGetDevice(&h->device) != hipSuccess ||
         hipDeviceGetAttribute(&h->num_cus, hipDeviceAttributeMultiprocessorCount, h->device) != hipSuccess ||
         hipDeviceGetAttribute(&h->wclk_khz, hipDeviceAttributeWallClockRate, h->device) != hipSuccess) {
         (void)hipGetLastError();
         return LSTM_DYN_ERR_HIP;
     }
+    return LSTM_DYN_OK;
+}
+
+// Its workspace (after ops_device).
+inline int ops_init(OpsHandle* h, long long bytes) {
     void* p = nullptr;
     if (hipMalloc(&p, (size_t)bytes) != hipSuccess) {
         (void)hipGetLastError();
@@ -160,8 +166,10 @@ __device__ inline void load_vec(const E* p, float* out) {
         for (int i = 0; i < V; ++i) out[i] = (float)x[i];
     }
 }
-template <class E, int V>
-__device__ inline void store_vec(E* p, const float* in) {
+// The same store; FAR: past the caches, for an output larger than FAR_BYTES.
+constexpr long long FAR_BYTES = 32LL << 20;
+template <bool FAR, class E, int V>
+__device__ inline void put(E* p, const float* in) {
     typename Vec<E, V>::type x;
     if constexpr (V == 1) {
         x = (E)in[0];
@@ -169,8 +177,12 @@ __device__ inline void store_vec(E* p, const float* in) {
 #pragma unroll
         for (int i = 0; i < V; ++i) x[i] = (E)in[i];
     }
-    *reinterpret_cast<typename Vec<E, V>::type*>(p) = x;
+    auto* q = reinterpret_cast<typename Vec<E, V>::type*>(p);
+    if constexpr (FAR) __builtin_nontemporal_store(x, q);
+    else *q = x;
 }
+template <class E, int V>
+__device__ inline void store_vec(E* p, const float* in) { put<false, E, V>(p, in); }
 
 // A row's length, clamped to [0, T]; a bad one is reported once.
 __device__ inline int row_length(const int32_t* lengths, int b, int T, int32_t* status, bool report) {

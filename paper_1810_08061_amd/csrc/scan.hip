@@ -15,6 +15,10 @@
 namespace ldyn {
 namespace {
 
+// How a row's shares hang together: it has one; each waits for the one before;
+// or for the one NW before and the maps between.
+enum Way { ONE, CHAIN, WINDOW };
+
 // Steps one thread holds, and between two kept states.
 template <class E>
 constexpr int run_of() { return sizeof(E) == 2 ? 16 : 8; }
@@ -39,7 +43,7 @@ struct ScanParams {
     int B, T, H;
     int tiles, segs;      // column tiles of a row; shares of its steps
     unsigned long long* counters;  // [B tiles] shares taken, over all launches
-    uint64_t* carry;      // [B][segs][H] {value, launch} a share passes on
+    uint64_t* carry;      // [1 or 3][B][segs][H] {value, launch}: what a share passes on; its map
     unsigned long long timeout_ticks;
 };
 
@@ -80,9 +84,9 @@ __device__ inline Raw<E, V> load_raw(const E* base, unsigned off) {
     }
     return x;
 }
-template <class E, int V>
-__device__ inline void store_at(E* base, unsigned off, const float* x) {
-    store_vec<E, V>(reinterpret_cast<E*>(reinterpret_cast<char*>(base) + off), x);
+template <bool FAR, class E, int V>
+__device__ inline void store_at(E* base, unsigned off, const float* in) {
+    put<FAR, E, V>(reinterpret_cast<E*>(reinterpret_cast<char*>(base) + off), in);
 }
 
 // Which share of which row and columns this workgroup takes.  The shares of one
@@ -97,12 +101,13 @@ struct Item {
     unsigned launch;
 };
 constexpr int COUNTER_WORDS = 8;  // a counter per 64 bytes
+template <int WAY>
 __device__ inline Item take_item(const ScanParams& p, bool last_first, unsigned (*lds)[2]) {
     const unsigned chains = (unsigned)p.B * p.tiles;
     Item it;
     unsigned chain = blockIdx.x, seg = 0;
     it.launch = 0;
-    if (p.segs > 1) {
+    if constexpr (WAY != ONE) {
         chain = blockIdx.x % chains;
         if (threadIdx.x == 0) {
             const unsigned long long n = atomicAdd(p.counters + (long)chain * COUNTER_WORDS, 1ull);
@@ -251,15 +256,82 @@ struct Place {
     __device__ long step0(const ScanParams& p) const { return (long)b * p.T + first; }
 };
 
+// The state (or gradient) a share starts from, into start[], and what it passes
+// on.  `depth` shares of its row come before it, the nearest `dir` away; the
+// row's first one starts from `base`.  Share j passes on P_j = A_j P_{j-1} + S_j.
+// Where a row's chain is what takes the time (few chains), a share does not wait
+// for P_{j-1}: every share first publishes its map, and each wave fetches one of
+// the NW - 1 maps before this one, or P_{j-NW}, from which the same products and sums
+// give P_{j-1}, to the bit: the chain is NW times shorter.
+template <int WAY, class E, int V, int NT, int CL>
+__device__ inline void carry_on(const ScanParams& p, const Place<E, V, NT, CL>& at, int depth, int dir, bool last,
+                                const float* base, const float* A, const float* S, float* start,
+                                float (*seen)[2][CL * V], float* out) {
+    constexpr int NW = NT / 64;
+    const int w = threadIdx.x >> 6;
+    const long stride = (long)p.B * p.segs * p.H, cell = ((long)at.b * p.segs + at.seg) * p.H + at.c;
+    const bool mine = threadIdx.x < CL && at.on;
+    float x[V] = {};
+    if constexpr (WAY == WINDOW) {
+        if (mine && !last) {
+            publish<V>(p.carry + stride + cell, A, at.launch);
+            publish<V>(p.carry + 2 * stride + cell, S, at.launch);
+        }
+        if (w < depth && (int)(threadIdx.x & 63) < CL && at.on) {
+            uint64_t* q = p.carry + cell + (long)dir * (w + 1) * p.H;
+            float a[V] = {}, s[V];
+            if (w == NW - 1) {
+                await<V>(p, q, s, at.launch);
+            } else {
+                await<V>(p, q + stride, a, at.launch);
+                await<V>(p, q + 2 * stride, s, at.launch);
+            }
+#pragma unroll
+            for (int i = 0; i < V; ++i) seen[w][0][at.cl * V + i] = a[i], seen[w][1][at.cl * V + i] = s[i];
+        }
+        __syncthreads();
+        if (mine) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                x[i] = depth >= NW ? seen[NW - 1][1][at.cl * V + i] : base ? base[i] : 0.0f;
+                for (int j = min(depth, NW - 1) - 1; j >= 0; --j)
+                    x[i] = fmaf(seen[j][0][at.cl * V + i], x[i], seen[j][1][at.cl * V + i]);
+            }
+        }
+    } else if (mine) {
+        if (WAY == ONE || depth == 0) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) x[i] = base ? base[i] : 0.0f;
+        } else {
+            await<V>(p, p.carry + cell + (long)dir * p.H, x, at.launch);
+        }
+    }
+    if (mine) {
+        float e[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            start[at.cl * V + i] = x[i];
+            e[i] = at.L == 0 ? x[i] : fmaf(A[i], x[i], S[i]);
+        }
+        if (WAY == ONE || last) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) out[i] = e[i];
+        } else {
+            publish<V>(p.carry + cell, e, at.launch);
+        }
+    }
+    __syncthreads();
+}
+
 // The steps of a share.  WHOLE: all of them are valid, so loads and selects
 // depend on nothing; written out apart, because where the two ways would meet
 // the compiler waits for every load.
-template <bool WHOLE, class E, int V, int NT, int CL>
+template <bool WHOLE, bool FAR, int WAY, class E, int V, int NT, int CL>
 __device__ inline void forward_share(const ScanParams& p, const Place<E, V, NT, CL>& at,
-                                     float (*maps)[2][CL * V], float* start) {
+                                     float (*maps)[2][CL * V], float* start,
+                                      float (*seen)[2][CL * V]) {
     constexpr int R = run_of<E>(), G = NT / CL;
     const int H = p.H, L = at.L, t0 = at.t0;
-    const unsigned launch = at.launch;
     const long row = (long)at.b * H + at.c;
     const E* z = static_cast<const E*>(p.z) + at.step0(p) * 3 * H;
     E* y = static_cast<E*>(p.y) + at.step0(p) * H;
@@ -274,11 +346,6 @@ __device__ inline void forward_share(const ScanParams& p, const Place<E, V, NT, 
         }
     }
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        if (!WHOLE) o[r] = Raw<E, V>{};
-        if (WHOLE || t0 + r < L) o[r] = load_raw<E, V>(z + (long)r * 3 * H + 2 * H, at.zoff);
-    }
-#pragma unroll
     for (int i = 0; i < V; ++i) A[i] = 1.0f, S[i] = 0.0f;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -290,30 +357,17 @@ __device__ inline void forward_share(const ScanParams& p, const Place<E, V, NT, 
             if (WHOLE || t0 + r < L) S[i] = s, A[i] = a;
         }
     }
+    // The output gates are on their way while the runs are joined; earlier they would only
+    // hold registers.
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        if (!WHOLE) o[r] = Raw<E, V>{};
+        if (WHOLE || t0 + r < L) o[r] = load_raw<E, V>(z + (long)r * 3 * H + 2 * H, at.zoff);
+    }
     float tA[V], tS[V], h[V] = {};
     join_runs<V, NT, CL, false>(A, S, tA, tS, maps);
-    if (threadIdx.x < CL && at.on) {
-        uint64_t* w = p.carry + ((long)at.b * p.segs + at.seg) * H + at.c;
-        if (at.seg == 0) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) h[i] = p.h0[row + i];
-        } else {
-            await<V>(p, w - H, h, launch);
-        }
-        float e[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            start[at.cl * V + i] = h[i];
-            e[i] = L == 0 ? h[i] : fmaf(tA[i], h[i], tS[i]);
-        }
-        if (at.first + G * R < L) {
-            publish<V>(w, e, launch);
-        } else {
-#pragma unroll
-            for (int i = 0; i < V; ++i) p.out_h[row + i] = e[i];
-        }
-    }
-    __syncthreads();
+    carry_on<WAY>(p, at, at.seg, -1, at.first + G * R >= L, p.h0 + row, tA, tS, start, seen, p.out_h + row);
     if (!at.on) return;
 #pragma unroll
     for (int r = 0; r < R; ++r) v[r].hold(), o[r].hold();
@@ -333,34 +387,35 @@ __device__ inline void forward_share(const ScanParams& p, const Place<E, V, NT, 
             out[i] = logistic_neg(-o[r][i]) * h[i];
             if (!WHOLE && t0 + r >= L) out[i] = 0.0f;
         }
-        if (WHOLE || t0 + r < p.T) store_at<E, V>(y + (long)r * H, at.yoff, out);
+        if (WHOLE || t0 + r < p.T) store_at<FAR, E, V>(y + (long)r * H, at.yoff, out);
     }
 }
 
-template <class E, int V, int NT, int CL>
+template <bool FAR, int WAY, class E, int V, int NT, int CL>
 __global__ void __launch_bounds__(NT, 4) scan_forward_kernel(ScanParams p) {
     constexpr int R = run_of<E>(), NW = NT / 64;
     __shared__ unsigned turn[1][2];
     __shared__ float maps[NW][2][CL * V];
     __shared__ float start[CL * V];
-    const Place<E, V, NT, CL> at(p, take_item(p, false, turn));
+    __shared__ float seen[NW][2][CL * V];
+    const Place<E, V, NT, CL> at(p, take_item<WAY>(p, false, turn));
     if (at.full) {
-        forward_share<true, E, V, NT, CL>(p, at, maps, start);
+        forward_share<true, FAR, WAY, E, V, NT, CL>(p, at, maps, start, seen);
     } else if (at.first < at.L || at.first == 0) {
-        forward_share<false, E, V, NT, CL>(p, at, maps, start);
+        forward_share<false, FAR, WAY, E, V, NT, CL>(p, at, maps, start, seen);
     } else if (at.on) {  // past the row's end
         E* y = static_cast<E*>(p.y) + at.step0(p) * p.H;
         float zero[V] = {};
-        for (int r = 0; r < R && at.t0 + r < p.T; ++r) store_at<E, V>(y + (long)r * p.H, at.yoff, zero);
+        for (int r = 0; r < R && at.t0 + r < p.T; ++r) store_at<FAR, E, V>(y + (long)r * p.H, at.yoff, zero);
     }
 }
 
-template <bool WHOLE, class E, int V, int NT, int CL>
+template <bool WHOLE, bool FAR, int WAY, class E, int V, int NT, int CL>
 __device__ inline void backward_share(const ScanParams& p, const Place<E, V, NT, CL>& at,
-                                      float (*maps)[2][CL * V], float* start) {
+                                      float (*maps)[2][CL * V], float* start,
+                                      float (*seen)[2][CL * V]) {
     constexpr int R = run_of<E>(), G = NT / CL;
     const int H = p.H, L = at.L, t0 = at.t0;
-    const unsigned launch = at.launch;
     const long row = (long)at.b * H + at.c;
     const E* z = static_cast<const E*>(p.z) + at.step0(p) * 3 * H;
     const E* dy = static_cast<const E*>(p.dy) + at.step0(p) * H;
@@ -399,7 +454,7 @@ __device__ inline void backward_share(const ScanParams& p, const Place<E, V, NT,
             q[r][i] = valid ? qq : 0.0f;
             f[r][i] = -diff * kk * (1.0f - kk);
         }
-        if (at.on && (WHOLE || t0 + r < p.T)) store_at<E, V>(dz + ((long)r * 3 + 2) * H, at.zoff, out);
+        if (at.on && (WHOLE || t0 + r < p.T)) store_at<FAR, E, V>(dz + ((long)r * 3 + 2) * H, at.zoff, out);
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) A[i] = 1.0f, S[i] = 0.0f;
@@ -414,28 +469,8 @@ __device__ inline void backward_share(const ScanParams& p, const Place<E, V, NT,
     }
     float tA[V], tS[V], e[V] = {};
     join_runs<V, NT, CL, true>(A, S, tA, tS, maps);
-    if (threadIdx.x < CL && at.on) {
-        uint64_t* w = p.carry + ((long)at.b * p.segs + at.seg) * H + at.c;
-        if (at.first + G * R >= L) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) e[i] = p.d_out_h ? p.d_out_h[row + i] : 0.0f;
-        } else {
-            await<V>(p, w + H, e, launch);
-        }
-        float x[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            start[at.cl * V + i] = e[i];
-            x[i] = fmaf(tA[i], e[i], tS[i]);
-        }
-        if (at.seg > 0) {
-            publish<V>(w, x, launch);
-        } else {
-#pragma unroll
-            for (int i = 0; i < V; ++i) p.dh0[row + i] = x[i];
-        }
-    }
-    __syncthreads();
+    carry_on<WAY>(p, at, (L - 1) / (G * R) - at.seg, 1, at.seg == 0, p.d_out_h ? p.d_out_h + row : nullptr, tA, tS, start,
+             seen, p.dh0 + row);
     if (!at.on) return;
 #pragma unroll
     for (int i = 0; i < V; ++i) e[i] = fmaf(A[i], start[at.cl * V + i], S[i]);
@@ -451,29 +486,30 @@ __device__ inline void backward_share(const ScanParams& p, const Place<E, V, NT,
             e[i] = valid ? fmaf(-k[r][i], gr, gr) : e[i];
         }
         if (WHOLE || t0 + r < p.T) {
-            store_at<E, V>(dz + (long)r * 3 * H, at.zoff, df);
-            store_at<E, V>(dz + ((long)r * 3 + 1) * H, at.zoff, dv);
+            store_at<FAR, E, V>(dz + (long)r * 3 * H, at.zoff, df);
+            store_at<FAR, E, V>(dz + ((long)r * 3 + 1) * H, at.zoff, dv);
         }
     }
 }
 
-template <class E, int V, int NT, int CL>
+template <bool FAR, int WAY, class E, int V, int NT, int CL>
 __global__ void __launch_bounds__(NT, sizeof(E) == 2 && V == 2 ? 3 : 4) scan_backward_kernel(ScanParams p) {
     constexpr int R = run_of<E>(), NW = NT / 64;
     __shared__ unsigned turn[1][2];
     __shared__ float maps[NW][2][CL * V];
     __shared__ float start[CL * V];
-    const Place<E, V, NT, CL> at(p, take_item(p, true, turn));
+    __shared__ float seen[NW][2][CL * V];
+    const Place<E, V, NT, CL> at(p, take_item<WAY>(p, true, turn));
     if (at.full) {
-        backward_share<true, E, V, NT, CL>(p, at, maps, start);
+        backward_share<true, FAR, WAY, E, V, NT, CL>(p, at, maps, start, seen);
     } else if (at.first < at.L) {
-        backward_share<false, E, V, NT, CL>(p, at, maps, start);
+        backward_share<false, FAR, WAY, E, V, NT, CL>(p, at, maps, start, seen);
     } else if (at.on) {  // past the row's end
         E* dz = static_cast<E*>(p.dz) + at.step0(p) * 3 * p.H;
         float zero[V] = {};
         for (int r = 0; r < R && at.t0 + r < p.T; ++r)
 #pragma unroll
-            for (int j = 0; j < 3; ++j) store_at<E, V>(dz + ((long)r * 3 + j) * p.H, at.zoff, zero);
+            for (int j = 0; j < 3; ++j) store_at<FAR, E, V>(dz + ((long)r * 3 + j) * p.H, at.zoff, zero);
         if (at.L == 0 && at.t0 == 0) {
             const long row = (long)at.b * p.H + at.c;
 #pragma unroll
@@ -540,6 +576,7 @@ using namespace ldyn;
 struct Shape {
     int threads, lanes;  // of a workgroup; of those along the channels
     int segs, tiles;
+    int way;             // see carry_on
 };
 
 struct lstm_dyn_scan : OpsHandle {
@@ -553,42 +590,54 @@ struct lstm_dyn_scan : OpsHandle {
 
 // The smallest workgroup that holds all steps, up to `most` threads.
 static Shape scan_shape(const lstm_dyn_scan* h, int most) {
-    Shape w{64, 64, 0, 0};
+    Shape w{64, 64, 0, 0, ONE};
     while (w.threads < most && w.threads / 64 * h->run < h->T) w.threads *= 2;
     if (w.threads == most && most / 64 * h->run < h->T) w.lanes = 32;  // the longer share: fewer in a row's chain
     const int steps = w.threads / w.lanes * h->run;
     w.segs = (h->T + steps - 1) / steps;
     w.tiles = (h->H + w.lanes * h->vec - 1) / (w.lanes * h->vec);
+    // With as many chains as there are workgroups on the device, a share's predecessor is long
+    // done; with fewer the chain's own time counts (a prompt of 32768 steps, 32 chains: 149 us
+    // in a plain chain, 124 so).
+    if (w.segs > 1) w.way = w.segs > 2 && (long)h->B * w.tiles < 2L * h->num_cus ? WINDOW : CHAIN;
     return w;
 }
 
-template <class E, int V>
+template <bool FAR, class E, int V>
 static void scan_launch(const lstm_dyn_scan* h, const ScanParams& p, bool back) {
     const Shape& w = back ? h->bwd : h->fwd;
     void (*k)(ScanParams);
     if (back)
-        k = w.lanes == 32       ? scan_backward_kernel<E, V, BWD_THREADS, 32>
-            : w.threads == 64  ? scan_backward_kernel<E, V, 64, 64>
-            : w.threads == 128 ? scan_backward_kernel<E, V, 128, 64>
-                               : scan_backward_kernel<E, V, 256, 64>;
+        k = w.way == WINDOW    ? scan_backward_kernel<FAR, WINDOW, E, V, BWD_THREADS, 32>
+            : w.way == CHAIN   ? scan_backward_kernel<FAR, CHAIN, E, V, BWD_THREADS, 32>
+            : w.lanes == 32    ? scan_backward_kernel<FAR, ONE, E, V, BWD_THREADS, 32>
+            : w.threads == 64  ? scan_backward_kernel<FAR, ONE, E, V, 64, 64>
+            : w.threads == 128 ? scan_backward_kernel<FAR, ONE, E, V, 128, 64>
+                               : scan_backward_kernel<FAR, ONE, E, V, 256, 64>;
     else
-        k = w.lanes == 32       ? scan_forward_kernel<E, V, FWD_THREADS, 32>
-            : w.threads == 64  ? scan_forward_kernel<E, V, 64, 64>
-            : w.threads == 128 ? scan_forward_kernel<E, V, 128, 64>
-            : w.threads == 256 ? scan_forward_kernel<E, V, 256, 64>
-                               : scan_forward_kernel<E, V, 512, 64>;
+        k = w.way == WINDOW    ? scan_forward_kernel<FAR, WINDOW, E, V, FWD_THREADS, 32>
+            : w.way == CHAIN   ? scan_forward_kernel<FAR, CHAIN, E, V, FWD_THREADS, 32>
+            : w.lanes == 32    ? scan_forward_kernel<FAR, ONE, E, V, FWD_THREADS, 32>
+            : w.threads == 64  ? scan_forward_kernel<FAR, ONE, E, V, 64, 64>
+            : w.threads == 128 ? scan_forward_kernel<FAR, ONE, E, V, 128, 64>
+            : w.threads == 256 ? scan_forward_kernel<FAR, ONE, E, V, 256, 64>
+                               : scan_forward_kernel<FAR, ONE, E, V, 512, 64>;
     hipLaunchKernelGGL(k, dim3((unsigned)((long)h->B * w.tiles * w.segs)), dim3((unsigned)w.threads), 0,
                        h->last_stream, p);
 }
 
 static int scan_run(lstm_dyn_scan* h, const ScanParams& p, bool back) {
+    const long long out = (long long)h->B * h->T * h->H * (back ? 3 : 1) * dtype_bytes(h->dtype);
+    const bool far = out > FAR_BYTES;
+#define LDYN_RUN(E, V) (far ? scan_launch<true, E, V>(h, p, back) : scan_launch<false, E, V>(h, p, back))
     if (h->dtype == LSTM_DYN_BF16) {
-        if (h->vec == 2) scan_launch<__bf16, 2>(h, p, back);
-        else scan_launch<__bf16, 1>(h, p, back);
+        if (h->vec == 2) LDYN_RUN(__bf16, 2);
+        else LDYN_RUN(__bf16, 1);
     } else {
-        if (h->vec == 2) scan_launch<float, 2>(h, p, back);
-        else scan_launch<float, 1>(h, p, back);
+        if (h->vec == 2) LDYN_RUN(float, 2);
+        else LDYN_RUN(float, 1);
     }
+#undef LDYN_RUN
     return ops_launched(h);
 }
 
@@ -629,12 +678,16 @@ extern "C" int lstm_dyn_scan_create(lstm_dyn_scan_t** out, int B, int H, int T, 
     lstm_dyn_scan* h = new (std::nothrow) lstm_dyn_scan();
     if (!h) return LSTM_DYN_ERR_NOMEM;
     h->B = B; h->H = H; h->T = T; h->dtype = dtype;
+    if ((rc = ops_device(h)) != LSTM_DYN_OK) {
+        delete h;
+        return rc;
+    }
     h->run = dtype == LSTM_DYN_BF16 ? run_of<__bf16>() : run_of<float>();
     h->vec = H % 2 ? 1 : 2;
     h->fwd = scan_shape(h, FWD_THREADS);
     h->bwd = scan_shape(h, BWD_THREADS);
     auto bytes = [&](const Shape& w) {
-        return w.segs > 1 ? 8LL * COUNTER_WORDS * B * w.tiles + 8LL * B * w.segs * H : 0;
+        return w.segs > 1 ? 8LL * COUNTER_WORDS * B * w.tiles + (w.way == WINDOW ? 24LL : 8LL) * B * w.segs * H : 0;
     };
     if ((rc = ops_init(h, 256 + bytes(h->fwd) + bytes(h->bwd))) != LSTM_DYN_OK) {
         delete h;
