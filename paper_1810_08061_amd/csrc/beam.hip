@@ -138,7 +138,7 @@ __device__ inline void rank_keys(int K, Shared* sh) {
     for (unsigned i = threadIdx.x; i < n; i += THREADS) {
         const uint64_t q = sh->cand[i];
         int rank = 0;
-#pragma unroll 4
+#pragma unroll 8
         for (unsigned j = 0; j < n; ++j) rank += sh->cand[j] > q;
         if (rank < K) sh->best[rank] = q;
     }
@@ -508,15 +508,17 @@ struct lstm_dyn_beam : OpsHandle {
     unsigned* arrived;
 };
 
-// How a beam's logits are cut: eight loads a thread, fewer where that would
-// leave fewer than four workgroups a CU; and no more slices than can be joined in a few rounds (a
+// How a beam's logits are cut: eight loads a thread (64 x 16 beams over 65536
+// tokens 53 us; four 71, two 85, sixteen 54), fewer where that would leave
+// fewer workgroups than CUs (8 x 10 beams over 30000 tokens in fp32: 20.8 us so,
+// 26 for four a CU); and no more slices than can be joined in a few rounds (a
 // workgroup takes its slice in pieces then).
 static void beam_shape(lstm_dyn_beam* h) {
     const int quad = 16 / dtype_bytes(h->dtype);
     const long quads = ((long)h->V + quad - 1) / quad + (h->V % quad ? 1 : 0), rows = (long)h->B * h->K;
     auto slices = [&](int n) { return (quads + THREADS * n - 1) / (THREADS * n); };
     int n = 8;
-    while (n > 1 && rows * slices(n) < 4L * h->num_cus) n /= 2;
+    while (n > 1 && rows * slices(n) < h->num_cus) n /= 2;
     long most = 2048 / (h->K * h->K);
     if (most < 8) most = 8;
     h->hold = n;
