@@ -70,6 +70,12 @@ def _call(name, *args):
         raise LstmDynError(rc, name)
 
 
+def _ok(rc, name):
+    """For the wrappers below, whose calls are few microseconds: the function is called directly."""
+    if rc != OK:
+        raise LstmDynError(rc, name)
+
+
 def _create(name, *args) -> int:
     h = ctypes.c_void_p()
     _call(name, ctypes.byref(h), *args)
@@ -278,26 +284,26 @@ class GatedScan(_Handle):
         _check("lengths", lengths, torch.int32, (B,))
         _check("h0", h0, torch.float32, (B, H))
         if out_h is None:
-            out_h = torch.empty((B, H), dtype=torch.float32, device=z.device)
+            out_h = torch.empty_like(h0)
         else:
             _check("out_h", out_h, torch.float32, (B, H))
         if out_y is None:
             out_y = torch.empty((B, T, H), dtype=self._et, device=z.device)
         else:
             _check("out_y", out_y, self._et, (B, T, H))
-        call(self.handle, z.data_ptr(), lengths.data_ptr(), h0.data_ptr(), out_h.data_ptr(),
-             out_y.data_ptr(), _stream(stream, z.device))
+        _ok(getattr(_ready, call)(self.handle, z.data_ptr(), lengths.data_ptr(), h0.data_ptr(), out_h.data_ptr(),
+                                  out_y.data_ptr(), _stream(stream, z.device)), call)
         return out_y, out_h
 
     def forward(self, z, lengths, h0, out_h=None, out_y=None, stream=None):
         """Returns (y [B, T_max, H], zero past each length, and the state after each row's last step)."""
-        return self._forward(lstm_dyn_scan_forward, z, lengths, h0, out_h, out_y, stream)
+        return self._forward("lstm_dyn_scan_forward", z, lengths, h0, out_h, out_y, stream)
 
     __call__ = forward
 
     def forward_train(self, z, lengths, h0, out_h=None, out_y=None, stream=None):
         """``forward`` that also keeps what ``backward`` needs."""
-        return self._forward(lstm_dyn_scan_forward_train, z, lengths, h0, out_h, out_y, stream)
+        return self._forward("lstm_dyn_scan_forward_train", z, lengths, h0, out_h, out_y, stream)
 
     def backward(self, z, lengths, h0, dy, d_out_h=None, stream=None, out=None):
         """Gradients after ``forward_train`` with the same z, lengths and h0: a dict of dz
@@ -319,9 +325,10 @@ class GatedScan(_Handle):
                 raise ValueError("out must hold exactly ['dh0', 'dz']")
             _check("dz", out["dz"], self._et, (B, T, 3 * H))
             _check("dh0", out["dh0"], torch.float32, (B, H))
-        lstm_dyn_scan_backward(self.handle, z.data_ptr(), lengths.data_ptr(), h0.data_ptr(),
-                               dy.data_ptr(), d_out_h.data_ptr() if d_out_h is not None else 0,
-                               out["dz"].data_ptr(), out["dh0"].data_ptr(), _stream(stream, z.device))
+        _ok(_ready.lstm_dyn_scan_backward(self.handle, z.data_ptr(), lengths.data_ptr(), h0.data_ptr(),
+                                          dy.data_ptr(), d_out_h.data_ptr() if d_out_h is not None else 0,
+                                          out["dz"].data_ptr(), out["dh0"].data_ptr(), _stream(stream, z.device)),
+            "lstm_dyn_scan_backward")
         return out
 
     def step(self, z, h, out_h=None, out_y=None, stream=None):
@@ -336,11 +343,11 @@ class GatedScan(_Handle):
         else:
             _check("out_h", out_h, torch.float32, (R, H))
         if out_y is None:
-            out_y = torch.empty((R, H), dtype=self._et, device=z.device)
+            out_y = torch.empty_like(h, dtype=self._et)
         else:
             _check("out_y", out_y, self._et, (R, H))
-        lstm_dyn_scan_step(R, H, self.dtype, z.data_ptr(), h.data_ptr(), out_h.data_ptr(),
-                           out_y.data_ptr(), _stream(stream, z.device))
+        _ok(_ready.lstm_dyn_scan_step(R, H, self.dtype, z.data_ptr(), h.data_ptr(), out_h.data_ptr(),
+                                      out_y.data_ptr(), _stream(stream, z.device)), "lstm_dyn_scan_step")
         return out_y, out_h
 
 
@@ -372,8 +379,8 @@ class TokenEmbed(_Handle):
             out_x = torch.empty((self.B, self.T, self.D), dtype=self._et, device=table.device)
         else:
             _check("out_x", out_x, self._et, (self.B, self.T, self.D))
-        lstm_dyn_embed_forward(self.handle, tokens.data_ptr(), L, table.data_ptr(), self.scale,
-                               out_x.data_ptr(), _stream(stream, table.device))
+        _ok(_ready.lstm_dyn_embed_forward(self.handle, tokens.data_ptr(), L, table.data_ptr(), self.scale,
+                                          out_x.data_ptr(), _stream(stream, table.device)), "lstm_dyn_embed_forward")
         return out_x
 
     __call__ = forward
@@ -389,8 +396,8 @@ class TokenEmbed(_Handle):
             out = torch.empty((self.V, self.D), dtype=torch.float32, device=dx.device)
         else:
             _check("out", out, torch.float32, (self.V, self.D))
-        lstm_dyn_embed_backward(self.handle, tokens.data_ptr(), L, dx.data_ptr(), code, self.scale,
-                                out.data_ptr(), _stream(stream, dx.device))
+        _ok(_ready.lstm_dyn_embed_backward(self.handle, tokens.data_ptr(), L, dx.data_ptr(), code, self.scale,
+                                           out.data_ptr(), _stream(stream, dx.device)), "lstm_dyn_embed_backward")
         return out
 
 
@@ -458,11 +465,12 @@ class AdamW(_Handle):
         et = grads[0].dtype if isinstance(grads[0], torch.Tensor) else None
         if et not in (torch.float32, torch.bfloat16):
             raise TypeError("gradients must be float32 or bfloat16 device tensors")
-        for i, (g, p) in enumerate(zip(grads, self.params)):
-            _check(f"grads[{i}]", g, et, p.shape)
-        lstm_dyn_adamw_step(self.handle, self._pointers(*[g.data_ptr() for g in grads]),
-                            BF16 if et == torch.bfloat16 else F32, lr, self.betas[0], self.betas[1],
-                            self.eps, grad_scale, self.steps_done + 1, _stream(stream, grads[0].device))
+        for g, p in zip(grads, self.params):
+            _check("a gradient", g, et, p.shape)
+        _ok(_ready.lstm_dyn_adamw_step(self.handle, self._pointers(*[g.data_ptr() for g in grads]),
+                                       BF16 if et == torch.bfloat16 else F32, lr, self.betas[0], self.betas[1],
+                                       self.eps, grad_scale, self.steps_done + 1, _stream(stream, grads[0].device)),
+            "lstm_dyn_adamw_step")
         self.steps_done += 1
 
     def states(self, stream=None):
@@ -488,6 +496,7 @@ class BeamSearch(_Handle):
         self.B, self.K, self.V, self.end = B, K, V, -1 if end is None else int(end)
         self.dtype, self._et = _dtype(dtype)
         self.handle = lstm_dyn_beam_create(B, K, V, self.dtype)
+        self._rows = (BeamState * BEAM_MAX_STATES)()
 
     def step(self, logits, scores, finished, states=(), out_states=None, stream=None):
         """The K best of scores[b, k] + log_softmax(logits[b, k])[j] for every b (a finished beam goes
@@ -508,17 +517,19 @@ class BeamSearch(_Handle):
             out_states = [torch.empty_like(s) for s in states]
         elif len(out_states) != len(states):
             raise ValueError("out_states must be as many as states")
-        rows = (BeamState * len(states))() if states else None
+        rows = self._rows      # read before the call returns
         for i, (s, d) in enumerate(zip(states, out_states)):
             shape = s.shape
             _check("a state", s, s.dtype, shape)
             _check("a state's output", d, s.dtype, shape)
             if shape[:2] != (B, K):
                 raise ValueError(f"states[{i}] must have shape ({B}, {K}, ...), got {tuple(shape)}")
-            rows[i] = (s.data_ptr(), d.data_ptr(), s.nbytes // (B * K))
+            row = rows[i]
+            row.src, row.dst, row.row_bytes = s.data_ptr(), d.data_ptr(), s.nbytes // (B * K)
         out_scores, done = torch.empty_like(scores), torch.empty_like(finished)
         parent, token = torch.empty_like(scores, dtype=torch.int32), torch.empty_like(scores, dtype=torch.int32)
-        lstm_dyn_beam_step(self.handle, logits.data_ptr(), scores.data_ptr(), finished.data_ptr(), self.end,
-                           out_scores.data_ptr(), parent.data_ptr(), token.data_ptr(), done.data_ptr(),
-                           rows, len(states), _stream(stream, logits.device))
+        _ok(_ready.lstm_dyn_beam_step(self.handle, logits.data_ptr(), scores.data_ptr(), finished.data_ptr(),
+                                      self.end, out_scores.data_ptr(), parent.data_ptr(), token.data_ptr(),
+                                      done.data_ptr(), self._rows, len(states), _stream(stream, logits.device)),
+            "lstm_dyn_beam_step")
         return out_scores, parent, token, done, out_states
