@@ -185,12 +185,13 @@ template <class E, int V>
 __device__ inline void store_vec(E* p, const float* in) { put<false, E, V>(p, in); }
 
 // A row's length, clamped to [0, T]; a bad one is reported once.
-__device__ inline int row_length(const int32_t* lengths, int b, int T, int32_t* status, bool report) {
-    if (!lengths) return T;
-    const int L = lengths[b];
+__device__ inline int clamp_length(int L, int T, int32_t* status, bool report) {
     if ((unsigned)L <= (unsigned)T) return L;
     if (report) atomicOr(status, STATUS_BAD_LENGTHS);
     return L < 0 ? 0 : T;
+}
+__device__ inline int row_length(const int32_t* lengths, int b, int T, int32_t* status, bool report) {
+    return lengths ? clamp_length(lengths[b], T, status, report) : T;
 }
 
 }  // namespace ldyn

@@ -98,6 +98,7 @@ __device__ inline void store_at(E* base, unsigned off, const float* in) {
 // chains: an atomic on one address takes 40 ns, 0.33 ms for 4096 shares.)
 struct Item {
     int b, tile, seg;
+    int length;  // as passed: loaded while the counter answers
     unsigned launch;
 };
 constexpr int COUNTER_WORDS = 8;  // a counter per 64 bytes
@@ -105,10 +106,13 @@ template <int WAY>
 __device__ inline Item take_item(const ScanParams& p, bool last_first, unsigned (*lds)[2]) {
     const unsigned chains = (unsigned)p.B * p.tiles;
     Item it;
-    unsigned chain = blockIdx.x, seg = 0;
+    const unsigned chain = WAY == ONE ? blockIdx.x : blockIdx.x % chains;
+    unsigned seg = 0;
     it.launch = 0;
+    it.b = (int)(chain / p.tiles);
+    it.tile = (int)(chain - (unsigned)it.b * p.tiles);
+    it.length = p.lengths[it.b];
     if constexpr (WAY != ONE) {
-        chain = blockIdx.x % chains;
         if (threadIdx.x == 0) {
             const unsigned long long n = atomicAdd(p.counters + (long)chain * COUNTER_WORDS, 1ull);
             const unsigned long long l = n >> 32 ? n / (unsigned)p.segs : (unsigned)n / (unsigned)p.segs;
@@ -119,8 +123,6 @@ __device__ inline Item take_item(const ScanParams& p, bool last_first, unsigned 
         seg = (unsigned)__builtin_amdgcn_readfirstlane((int)(*lds)[0]);  // scalar addresses
         it.launch = (unsigned)__builtin_amdgcn_readfirstlane((int)(*lds)[1]);
     }
-    it.b = (int)(chain / p.tiles);
-    it.tile = (int)(chain - (unsigned)it.b * p.tiles);
     it.seg = last_first ? p.segs - 1 - (int)seg : (int)seg;
     return it;
 }
@@ -248,7 +250,7 @@ struct Place {
         c = on ? ch : 0;
         first = seg * G * R;
         t0 = first + g * R;
-        L = row_length(p.lengths, b, p.T, p.status, it.tile == 0 && seg == 0 && threadIdx.x == 0);
+        L = clamp_length(it.length, p.T, p.status, it.tile == 0 && seg == 0 && threadIdx.x == 0);
         full = first + G * R <= L;
         zoff = ((unsigned)(g * R * 3) * p.H + c) * sizeof(E);
         yoff = ((unsigned)(g * R) * p.H + c) * sizeof(E);
