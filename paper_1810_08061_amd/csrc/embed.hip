@@ -367,8 +367,12 @@ embed_join_kernel(EmbedParams p, const uint32_t* __restrict__ key, float* __rest
     const bool on = c < p.D;
     int parts = 0;  // in slot 0 of the pieces after this one
     const long end = (long)(piece + 1) * R;
-    const uint32_t V = (uint32_t)p.V, v = piece < pieces && end < p.N ? key[end] : V;
-    if (v != V && key[end - 1] == v && !(piece > 0 && key[end - R] == v && key[end - R - 1] == v)) {
+    // four keys at once: the waves that find nothing to do are most of them
+    const long far = p.N - 1;
+    const uint32_t next = key[min(end, far)], mine = key[min(end - 1, far)], begin = key[min(end - R, far)],
+                   before = key[min(max(end - R - 1, 0L), far)];
+    const uint32_t V = (uint32_t)p.V, v = piece < pieces && end < p.N ? next : V;
+    if (v != V && mine == v && !(piece > 0 && begin == v && before == v)) {
         // whole pieces 64 at a time
         parts = 1;
         for (;;) {
@@ -383,7 +387,7 @@ embed_join_kernel(EmbedParams p, const uint32_t* __restrict__ key, float* __rest
         float o[W];
 #pragma unroll
         for (int j = 0; j < W; ++j) o[j] = acc[j] * p.scale;
-        store_vec<float, W>(dt + (long)key[(long)piece * R + R] * p.D + c, o);
+        store_vec<float, W>(dt + (long)v * p.D + c, o);
     };
     if (parts > 0 && parts <= LONG && on) {
         float acc[W];
