@@ -10,6 +10,10 @@
 // are read and written once.  r instead of v: e4m3 with a power of two per
 // block spans 2^18, which v would need twice over.
 //
+// Bound by memory: 28 bytes an element with states in 32 bits, 16 with 8, 2 more with
+// a bf16 copy.  159 M elements, 8 bits and copies: 570 us (5.0 TB/s), their states'
+// values 175 us (5.4 TB/s); 2.9 M elements, 32 bits: 15 us (5.3 TB/s).
+//
 // One launch for up to 256 tensors: a workgroup takes CHUNK elements of one
 // tensor, found in a table made at create.  The gradients' addresses come with
 // the launch, since a program may have its gradients elsewhere in every step.

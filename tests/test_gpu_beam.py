@@ -92,6 +92,18 @@ def test_exact_ties(V, K, dtype):
                     assert all(j in mine for j in lower)
 
 
+def test_negative_zeros_are_zeros():
+    import torch
+    V, K = 3000, 8
+    g = torch.Generator().manual_seed(1)
+    logits = torch.where(torch.rand((1, K, V), generator=g) < 0.5, 0.0, -0.0)
+    for et in ("f32", "bf16"):
+        with ld.BeamSearch(1, K, V, et) as m:
+            x = logits if et == "f32" else logits.bfloat16()
+            got, parent, token, _, _ = _step(m, x, torch.zeros((1, K)), torch.zeros((1, K), dtype=torch.uint8))
+            assert (parent == 0).all() and token[0].tolist() == list(range(K))
+
+
 def test_masked_infinite_and_nan_logits():
     import torch
     inf, nan, low = float("inf"), float("nan"), torch.finfo(torch.float32).min

@@ -83,6 +83,35 @@ def test_lengths(lengths, dtype):
                 assert (h[b] == dev[2][b]).all()      # the state comes back bit for bit
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_chains(dtype):
+    """Many rows and columns, several shares a row: each share waits for the one before."""
+    dev, ref = _inputs(36, 1100, 70, dtype, 77)
+    with ld.GatedScan(36, 70, 1100, dtype) as m:
+        _run_and_check(m, dev, ref, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_few_and_many_chains_give_the_same_bits(dtype):
+    """One long row alone (its shares fetch the maps before them) and the same row 40 times (they wait for
+    the one before)."""
+    import torch
+    T, H, B = 5000, 64, 40
+    (z, L, h0, dy, dh), _ = _inputs(1, T, H, dtype, 78)
+    with ld.GatedScan(1, H, T, dtype) as m, ld.GatedScan(B, H, T, dtype) as m2:
+        for n in (T, T - 1, T - 300, 1300, 257):
+            L1 = torch.full((1,), n, dtype=torch.int32, device="cuda")
+            y, h = m.forward_train(z, L1, h0)
+            d = m.backward(z, L1, h0, dy, dh)
+            many = [t.expand(B, *t.shape[1:]).contiguous() for t in (z, L1, h0, dy, dh)]
+            y2, h2 = m2.forward_train(*many[:3])
+            d2 = m2.backward(*many)
+            bits = lambda t: torch.nan_to_num(t.float(), nan=9.0)
+            assert (bits(y2) == bits(y)).all() and (h2 == h).all()
+            assert (d2["dz"] == d["dz"]).all() and (d2["dh0"] == d["dh0"]).all(), n
+        assert m.status() == m2.status() == ld.OK
+
+
 def test_bad_lengths_are_clamped_and_reported():
     dev, ref = _inputs(4, 50, 24, "f32", 5, [50, 0, 7, 50], poison=False)
     z, L, h0, dy, dh = dev
