@@ -175,6 +175,19 @@ def test_without_the_states_gradient_and_in_place():
         assert h2 is state and (h2 == h).all() and (y2 == y).all()
 
 
+@pytest.mark.parametrize("T", [300, 700, 1300, 2047, 2500, 6000])
+def test_in_place_over_many_shares(T):
+    """The state in place where a row's shares are many: each that reads it does so before it is written."""
+    dev, _ = _inputs(1, T, 320, "bf16", T, [T])
+    z, L, h0 = dev[:3]
+    with ld.GatedScan(1, 320, T, "bf16") as m:
+        y, h = m.forward(z, L, h0)
+        for _ in range(20):
+            state = h0.clone()
+            y2, _ = m.forward(z, L, state, out_h=state)
+            assert (state == h).all() and (y2 == y).all()
+
+
 def test_backward_needs_a_forward_for_training():
     dev, _ = _inputs(2, 9, 8, "f32", 2)
     z, L, h0, dy, dh = dev
