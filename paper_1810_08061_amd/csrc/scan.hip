@@ -294,15 +294,13 @@ __device__ inline void carry_on(const ScanParams& p, const Place<E, V, NT, CL>& 
     const bool mine = threadIdx.x < CL && at.on;
     float x[V] = {};
     if constexpr (WAY == WINDOW) {
-        // The base is in registers before the map goes out: whoever writes the row's result, which
+        // The base is read (into LDS) before the map goes out: whoever writes the row's result, which
         // may lie where h0 does, has awaited every share's map, its own or through another's.
-        float from[V] = {};
-        if (mine && depth < NW && base) {
+        if (mine && depth < NW) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) from[i] = base[i];
+            for (int i = 0; i < V; ++i) start[at.cl * V + i] = base ? base[i] : 0.0f;
         }
-#pragma unroll
-        for (int i = 0; i < V; ++i) asm volatile("" : "+v"(from[i]) : : "memory");
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         if (mine && !last) {
             publish<V>(p.carry + stride + cell, A, at.launch);
             publish<V>(p.carry + 2 * stride + cell, S, at.launch);
@@ -323,7 +321,7 @@ __device__ inline void carry_on(const ScanParams& p, const Place<E, V, NT, CL>& 
         if (mine) {
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                x[i] = depth >= NW ? seen[NW - 1][1][at.cl * V + i] : from[i];
+                x[i] = depth >= NW ? seen[NW - 1][1][at.cl * V + i] : start[at.cl * V + i];
                 for (int j = min(depth, NW - 1) - 1; j >= 0; --j)
                     x[i] = fmaf(seen[j][0][at.cl * V + i], x[i], seen[j][1][at.cl * V + i]);
             }
