@@ -187,8 +187,9 @@ int lstm_dyn_check_adamw_args(const lstm_dyn_adamw_tensor_t* tensors, int count,
  * and for a finished beam the one candidate (k, end) = scores[k], all others -inf.
  * A NaN logit counts as -inf; a candidate that is not a number is -inf (a beam whose logits
  * are all -inf has no other).  The K largest candidates are taken, equal ones by the
- * lowest k V + j, in that order (within a beam the K largest logits are its
- * candidates, so two that differ only before rounding are not told apart wrongly):
+ * lowest k V + j, in that order.  Of a beam only the K largest logits are candidates
+ * (equal ones by the lowest token), so that sums that differ before they are rounded
+ * are not cut off in the wrong order:
  *     out_scores[k'], out_parent[k'] = k, out_token[k'] = j,
  *     out_finished[k'] = finished[k] or j = end,
  * and every state's rows follow their parents, dst[b][k'] = src[b][out_parent[k']].

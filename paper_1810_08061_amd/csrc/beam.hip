@@ -18,8 +18,8 @@
 // states too; large ones take a launch of their own.
 //
 // 64 x 16 beams over 65536 tokens in bf16: 43 us, 3.1 TB/s of logits.  About half of the
-// time the vector units are busy (46 instructions per 64 tokens: widening, maximum,
-// exp, sum), and the slices' ends wait for each other; the states (2 x 2048 floats a
+// time the vector units are busy (11.5 instructions per 64 tokens: widening, maximum,
+// exp, sum; and the bounds), and the slices' ends wait for each other; the states (2 x 2048 floats a
 // beam) 8 us more.  16 x 8 beams over 32768: 15 us, and one sequence with four
 // beams over 1000: 10 us, both a chain of loads, barriers and the join.
 #include "ops.h"

@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(SORT_THREADS) sort_hist_kernel(EmbedParams p, 
 
 // Places of a block go behind those of smaller digits and of earlier blocks;
 // within the block in order (each wave holds a run of places).  Every block
-// adds up all blocks' counts itself: 32 blocks at 256 K places, 64 KB.
+// adds up all blocks' counts itself: 64 blocks at 256 K places, 128 KB.
 __global__ void __launch_bounds__(SORT_THREADS) sort_scatter_kernel(EmbedParams p, SortPass s) {
     __shared__ uint32_t cnt[SORT_WAVES][SORT_BINS];
     __shared__ uint32_t wsum[SORT_WAVES];

@@ -59,6 +59,23 @@ def test_embed():
     assert d.abs().amax() == 0
 
 
+def test_more_places_than_the_sort_has_tiles():
+    """Over a million places: every block of the sort takes several tiles, one after another."""
+    import torch
+    B, T, V, D = 3, 500001, 5003, 4
+    g = torch.Generator(device="cuda").manual_seed(4)
+    tok = torch.randint(0, V, (B, T), generator=g, device="cuda", dtype=torch.int32)
+    tok[1] = torch.arange(T, device="cuda", dtype=torch.int32) // 200 % V       # long runs of one token
+    L = torch.tensor([T, T - 7, 300000], dtype=torch.int32, device="cuda")
+    dx = torch.randint(-4, 5, (B, T, D), generator=g, device="cuda").float()     # sums are exact
+    on = torch.arange(T, device="cuda")[None] < L[:, None]
+    want = torch.zeros((V, D), dtype=torch.float64, device="cuda")
+    want.index_add_(0, tok[on].long(), dx[on].double())
+    with ld.TokenEmbed(B, T, V, D, "f32", scale=0.5) as m:
+        assert (m.backward(tok, L, dx).double() == want * 0.5).all()
+        assert m.status() == ld.OK
+
+
 def test_beam():
     """The largest vocabulary and number of beams: indices up to 2^32, most logits equal."""
     import torch
