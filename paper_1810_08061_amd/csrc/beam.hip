@@ -129,7 +129,7 @@ struct Shared {
     uint64_t best[LSTM_DYN_BEAM_MAX_K];  // the K largest keys so far, in order; 0: none
     uint64_t cand[GATHER + LSTM_DYN_BEAM_MAX_K];
     float m[WAVES], s[WAVES];
-    float lse[LSTM_DYN_BEAM_MAX_K];
+    float top[LSTM_DYN_BEAM_MAX_K], lse[LSTM_DYN_BEAM_MAX_K];  // a beam's largest logit; log sum exp(x - top)
     int parent[LSTM_DYN_BEAM_MAX_K];
     unsigned n, quads;
     int last;
@@ -218,9 +218,12 @@ __device__ void join_slices(const BeamParams& p, const States& st, int b, Shared
                                                  __HIP_MEMORY_SCOPE_AGENT);
             join_sum(m, s, __uint_as_float((uint32_t)(q >> 32)), __uint_as_float((uint32_t)q));
         }
-        const float lse = m + logf(s);
+        // m and the log apart: their sum would be rounded at the size of m, which candidates of
+        // other beams, with another m, are compared with
+        const float lse = logf(s);
         const bool live = p.scores[row] > ninf && lse < __builtin_inff();
-        // a beam that is not live, or whose logits are all -inf, has no number among its candidates
+        // a beam that is not live has no number among its candidates
+        sh->top[threadIdx.x] = m;
         sh->lse[threadIdx.x] = live || p.finished[row] ? lse : __builtin_nanf("");
         sh->best[threadIdx.x] = 0;
     }
@@ -236,7 +239,7 @@ __device__ void join_slices(const BeamParams& p, const States& st, int b, Shared
             const unsigned k = at / per, r = at - k * per;
             const int row = b * K + (int)k;
             const bool done = p.finished[row] != 0;
-            const float score = p.scores[row], lse = sh->lse[k];
+            const float score = p.scores[row], top = sh->top[k], lse = sh->lse[k];
             if (done || lse != lse) {
                 const int end = done && score > ninf ? p.end : -1;
                 const int t = r < (unsigned)K ? plain_token((int)r, end, p.V) : p.V;
@@ -244,14 +247,14 @@ __device__ void join_slices(const BeamParams& p, const States& st, int b, Shared
             } else {
                 const uint64_t q = __hip_atomic_load(p.best + (long)row * per + r, __ATOMIC_RELAXED,
                                                      __HIP_MEMORY_SCOPE_AGENT);
-                if (q) key[i] = key_of(score + (unordered((uint32_t)(q >> 32)) - lse), k * (unsigned)p.V + ~(uint32_t)q);
+                if (q) key[i] = key_of(score + ((unordered((uint32_t)(q >> 32)) - top) - lse), k * (unsigned)p.V + ~(uint32_t)q);
             }
         }
         // no worse than the K-th so far, and than what K lanes of a wave have
-        uint64_t top = key[0];
+        uint64_t most = key[0];
 #pragma unroll
-        for (int i = 1; i < HOLD; ++i) top = key[i] > top ? key[i] : top;
-        const uint64_t bound = wave_bound<0>((uint32_t)(top >> 32), K, false, [] { return 0u; });
+        for (int i = 1; i < HOLD; ++i) most = key[i] > most ? key[i] : most;
+        const uint64_t bound = wave_bound<0>((uint32_t)(most >> 32), K, false, [] { return 0u; });
         if (lane == 0) sh->bound[w] = bound;
         __syncthreads();
         uint64_t least = sh->best[K - 1] | 1;

@@ -1,5 +1,5 @@
-"""A beam search step over vocabularies masked with large finite values: whole waves, whole slices and
-all but one token, against all candidates in 64 bits, in the very order.
+"""A beam search step over vocabularies masked with large finite values (whole waves, whole slices and
+all but one token) and with logits that lie anywhere, against all candidates in 64 bits, in the very order.
 
 The bound knows the logits that are not masked only.  The terms' exponents are within a few units of U of their size, and
 those of 2^-30 and less do not matter: 30 x 4 U of a term, 64 of a thread added one by one, then ten
@@ -91,3 +91,40 @@ def test_large_masks(V, K, mask, dtype):
                 x.scatter_(2, keep, logits.gather(2, keep))
             _check_order(m, x.to(et), scores, 40.0, name)
         assert m.status() == ld.OK
+
+
+@pytest.mark.parametrize("V,K", [(600, 4), (16384, 3), (70000, 2), (5003, 16)])
+@pytest.mark.parametrize("offset", [100.0, -300.0, 1000.0, -60000.0, 2.0 ** 17, -2.0 ** 19])
+def test_a_constant_on_a_beams_logits_changes_nothing(V, K, offset):
+    """Every beam's logits lie elsewhere.  The logits are multiples of 2^-3, so the shifted ones are exact."""
+    import torch
+    g = torch.Generator().manual_seed(V + K)
+    B = 8
+    logits = (torch.randn((B, K, V), generator=g) * 24).round() / 8
+    scores = -5 + torch.randn((B, K), generator=g) * 2
+    shifted = logits + (offset * torch.arange(K) / K).round()[None, :, None]
+    with ld.BeamSearch(B, K, V, "f32") as m:
+        _check_order(m, shifted, scores, 40.0, f"offset {offset:g}")
+        fin = torch.zeros((B, K), dtype=torch.uint8)
+        a, b = _step(m, logits, scores, fin), _step(m, shifted, scores, fin)
+        assert (a[1] == b[1]).all() and (a[2] == b[2]).all()
+        assert m.status() == ld.OK
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_beam_with_all_its_tokens_masked(dtype):
+    """Equal logits are equal chances, whatever their value: score - log V, the lowest tokens first."""
+    import torch
+    et = torch.float32 if dtype == "f32" else torch.bfloat16
+    K = 6
+    for V in (40, 3000, 33000):
+        logits = torch.zeros((1, K, V))
+        for k, x in enumerate((0.0, 40.0, -1e6, -1e10, -1e30, torch.finfo(et).min)):
+            logits[0, k] = x
+        scores = torch.tensor([[-1.0, -1.5, -2.0, -2.5, -3.0, -3.5]])
+        with ld.BeamSearch(1, K, V, dtype) as m:
+            for shift in range(K):      # each beam is the best one once
+                s = scores.roll(shift, 1)
+                _check_order(m, logits.to(et), s, 0.0, f"all masked, V {V}")
+                got, parent, token, _, _ = _step(m, logits.to(et), s, torch.zeros((1, K), dtype=torch.uint8))
+                assert (parent[0] == shift).all() and token[0].tolist() == list(range(K))
