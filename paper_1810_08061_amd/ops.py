@@ -5,7 +5,10 @@
 (one optimizer step over many tensors) and ``BeamSearch`` (one selection over
 beams and vocabulary).  As for ``LstmDyn``: every computation runs in the
 library's HIP kernels, torch owns device memory and names streams, a handle has
-one call in flight.  The ``lstm_dyn_*`` functions mirror the C ABI.
+one call in flight.  A call runs on the current stream; ``stream=`` (a torch stream or
+its address) is short for ``with torch.cuda.stream(stream)``: the results belong to
+that stream, which waits for no other by itself.  The ``lstm_dyn_*`` functions
+mirror the C ABI.
 """
 from __future__ import annotations
 
@@ -225,10 +228,18 @@ def _check(name, t, dtype, shape):
     raise ValueError(f"{name} must be contiguous")
 
 
-def _stream(stream, device):
-    if stream is None:
-        return _t().cuda.current_stream(device).cuda_stream
-    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+def _stream(device):
+    return _torch.cuda.current_stream(device).cuda_stream
+
+
+def _on(stream):
+    """The context of a call that names its stream (a torch stream or its address): as torch's own, so that
+    what the call allocates belongs to that stream, and neither earlier work of the
+    current stream nor its later allocations touch it."""
+    cuda = _torch.cuda
+    if not hasattr(stream, "cuda_stream"):
+        stream = cuda.ExternalStream(int(stream)) if int(stream) else cuda.default_stream()
+    return cuda.stream(stream)
 
 
 def _dtype(dtype):
@@ -278,6 +289,9 @@ class GatedScan(_Handle):
         self.handle = lstm_dyn_scan_create(B, H, T_max, self.dtype)
 
     def _forward(self, call, z, lengths, h0, out_h, out_y, stream):
+        if stream is not None:
+            with _on(stream):
+                return self._forward(call, z, lengths, h0, out_h, out_y, None)
         torch = _torch
         B, T, H = self.B, self.T, self.H
         _check("z", z, self._et, (B, T, 3 * H))
@@ -292,7 +306,7 @@ class GatedScan(_Handle):
         else:
             _check("out_y", out_y, self._et, (B, T, H))
         _ok(getattr(_ready, call)(self.handle, z.data_ptr(), lengths.data_ptr(), h0.data_ptr(), out_h.data_ptr(),
-                                  out_y.data_ptr(), _stream(stream, z.device)), call)
+                                  out_y.data_ptr(), _stream(z.device)), call)
         return out_y, out_h
 
     def forward(self, z, lengths, h0, out_h=None, out_y=None, stream=None):
@@ -310,6 +324,9 @@ class GatedScan(_Handle):
         [B, T_max, 3H] (the handle's dtype) and dh0 float32 [B, H].  dy in the
         handle's dtype; d_out_h float32 [B, H] or None.  out: a dict with those
         keys holding caller-owned tensors."""
+        if stream is not None:
+            with _on(stream):
+                return self.backward(z, lengths, h0, dy, d_out_h, None, out)
         torch = _torch
         B, T, H = self.B, self.T, self.H
         _check("z", z, self._et, (B, T, 3 * H))
@@ -327,13 +344,16 @@ class GatedScan(_Handle):
             _check("dh0", out["dh0"], torch.float32, (B, H))
         _ok(_ready.lstm_dyn_scan_backward(self.handle, z.data_ptr(), lengths.data_ptr(), h0.data_ptr(),
                                           dy.data_ptr(), d_out_h.data_ptr() if d_out_h is not None else 0,
-                                          out["dz"].data_ptr(), out["dh0"].data_ptr(), _stream(stream, z.device)),
+                                          out["dz"].data_ptr(), out["dh0"].data_ptr(), _stream(z.device)),
             "lstm_dyn_scan_backward")
         return out
 
     def step(self, z, h, out_h=None, out_y=None, stream=None):
         """One step of any number of rows: z [R, 3H], h float32 [R, H]; returns (y [R, H], h).
         out_h may be h itself."""
+        if stream is not None:
+            with _on(stream):
+                return self.step(z, h, out_h, out_y)
         torch = _torch
         R, H = h.shape[0], self.H
         _check("z", z, self._et, (R, 3 * H))
@@ -347,7 +367,7 @@ class GatedScan(_Handle):
         else:
             _check("out_y", out_y, self._et, (R, H))
         _ok(_ready.lstm_dyn_scan_step(R, H, self.dtype, z.data_ptr(), h.data_ptr(), out_h.data_ptr(),
-                                      out_y.data_ptr(), _stream(stream, z.device)), "lstm_dyn_scan_step")
+                                      out_y.data_ptr(), _stream(z.device)), "lstm_dyn_scan_step")
         return out_y, out_h
 
 
@@ -372,6 +392,9 @@ class TokenEmbed(_Handle):
         return lengths.data_ptr()
 
     def forward(self, tokens, lengths, table, out_x=None, stream=None):
+        if stream is not None:
+            with _on(stream):
+                return self.forward(tokens, lengths, table, out_x)
         torch = _torch
         L = self._tokens(tokens, lengths)
         _check("table", table, self._et, (self.V, self.D))
@@ -380,7 +403,7 @@ class TokenEmbed(_Handle):
         else:
             _check("out_x", out_x, self._et, (self.B, self.T, self.D))
         _ok(_ready.lstm_dyn_embed_forward(self.handle, tokens.data_ptr(), L, table.data_ptr(), self.scale,
-                                          out_x.data_ptr(), _stream(stream, table.device)), "lstm_dyn_embed_forward")
+                                          out_x.data_ptr(), _stream(table.device)), "lstm_dyn_embed_forward")
         return out_x
 
     __call__ = forward
@@ -388,6 +411,9 @@ class TokenEmbed(_Handle):
     def backward(self, tokens, lengths, dx, out=None, stream=None):
         """d_table float32 [V, D] (rows of tokens that do not occur are zero) from dx [B, T_max, D],
         float32 (as ``LstmDyn.backward`` gives it) or bfloat16."""
+        if stream is not None:
+            with _on(stream):
+                return self.backward(tokens, lengths, dx, out)
         torch = _torch
         L = self._tokens(tokens, lengths)
         code = BF16 if isinstance(dx, torch.Tensor) and dx.dtype == torch.bfloat16 else F32
@@ -397,7 +423,7 @@ class TokenEmbed(_Handle):
         else:
             _check("out", out, torch.float32, (self.V, self.D))
         _ok(_ready.lstm_dyn_embed_backward(self.handle, tokens.data_ptr(), L, dx.data_ptr(), code, self.scale,
-                                           out.data_ptr(), _stream(stream, dx.device)), "lstm_dyn_embed_backward")
+                                           out.data_ptr(), _stream(dx.device)), "lstm_dyn_embed_backward")
         return out
 
 
@@ -446,7 +472,7 @@ class AdamW(_Handle):
         self._pointers = ctypes.c_void_p * len(self.params)
 
     def load_state(self, m, v, m_exp=None, v_exp=None):
-        """Copy states kept before (in the layout of the attributes) into this optimizer."""
+        """Copy states kept before (in the layout of the attributes) into this optimizer, on the current stream."""
         for mine, given in ((self.m, m), (self.v, v), (self.m_exp, m_exp or []), (self.v_exp, v_exp or [])):
             if len(mine) != len(given):
                 raise ValueError("the states of every tensor are needed")
@@ -458,6 +484,9 @@ class AdamW(_Handle):
     def step(self, grads, lr: float, grad_scale: float = 1.0, stream=None):
         """One step from the gradients (all float32 or all bfloat16, in the parameters' shapes), each
         times grad_scale.  The step's number is a value of the call: a captured call repeats it."""
+        if stream is not None:
+            with _on(stream):
+                return self.step(grads, lr, grad_scale)
         torch = _torch
         grads = list(grads)
         if len(grads) != len(self.params):
@@ -469,7 +498,7 @@ class AdamW(_Handle):
             _check("a gradient", g, et, p.shape)
         _ok(_ready.lstm_dyn_adamw_step(self.handle, self._pointers(*[g.data_ptr() for g in grads]),
                                        BF16 if et == torch.bfloat16 else F32, lr, self.betas[0], self.betas[1],
-                                       self.eps, grad_scale, self.steps_done + 1, _stream(stream, grads[0].device)),
+                                       self.eps, grad_scale, self.steps_done + 1, _stream(grads[0].device)),
             "lstm_dyn_adamw_step")
         self.steps_done += 1
 
@@ -478,12 +507,15 @@ class AdamW(_Handle):
         themselves; or with 8 bits (m, sqrt(v)) as bfloat16, which holds their values exactly."""
         if self.bits == 32:
             return self.m, self.v
+        if stream is not None:
+            with _on(stream):
+                return self.states()
         torch = _torch
         m = [torch.empty(p.shape, dtype=torch.bfloat16, device=p.device) for p in self.params]
         v = [torch.empty_like(x) for x in m]
         lstm_dyn_adamw_states(self.handle, self._pointers(*[x.data_ptr() for x in m]),
                               self._pointers(*[x.data_ptr() for x in v]),
-                              _stream(stream, self.params[0].device))
+                              _stream(self.params[0].device))
         return m, v
 
 
@@ -506,6 +538,9 @@ class BeamSearch(_Handle):
         uint8 [B, K], states: tensors [B, K, ...] of any type (at most 8).  Returns
         (scores, parent int32, token int32, finished, states), all new, the states
         in out_states if given."""
+        if stream is not None:
+            with _on(stream):
+                return self.step(logits, scores, finished, states, out_states)
         torch = _torch
         B, K = self.B, self.K
         _check("logits", logits, self._et, (B, K, self.V))
@@ -530,6 +565,6 @@ class BeamSearch(_Handle):
         parent, token = torch.empty_like(scores, dtype=torch.int32), torch.empty_like(scores, dtype=torch.int32)
         _ok(_ready.lstm_dyn_beam_step(self.handle, logits.data_ptr(), scores.data_ptr(), finished.data_ptr(),
                                       self.end, out_scores.data_ptr(), parent.data_ptr(), token.data_ptr(),
-                                      done.data_ptr(), self._rows, len(states), _stream(stream, logits.device)),
+                                      done.data_ptr(), self._rows, len(states), _stream(logits.device)),
             "lstm_dyn_beam_step")
         return out_scores, parent, token, done, out_states
