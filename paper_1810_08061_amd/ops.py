@@ -213,21 +213,6 @@ def _t():
     return _torch
 
 
-def _check(name, t, dtype, shape):
-    try:
-        if t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous():
-            return
-    except AttributeError:
-        pass
-    if not isinstance(t, _t().Tensor) or not t.is_cuda:
-        raise TypeError(f"{name} must be a device tensor")
-    if t.dtype != dtype:
-        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    raise ValueError(f"{name} must be contiguous")
-
-
 def _stream(device):
     return _torch.cuda.current_stream(device).cuda_stream
 
@@ -248,9 +233,26 @@ def _dtype(dtype):
 
 
 class _Handle:
-    """What the operators' wrappers share: a handle, its query and its end."""
+    """What the operators' wrappers share: a handle, of the device that is current where it is made, the
+    checks of tensors, its query and its end."""
     _kind = ""
     handle = None
+
+    def _check(self, name, t, dtype, shape):
+        try:
+            if t.dtype is dtype and t.shape == shape and t.get_device() == self._device and t.is_contiguous():
+                return
+        except AttributeError:
+            pass
+        if not isinstance(t, _t().Tensor) or not t.is_cuda:
+            raise TypeError(f"{name} must be a device tensor")
+        if t.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+        if t.shape != shape:
+            raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+        if t.get_device() != self._device:
+            raise ValueError(f"{name} must be on the handle's device {self._device}, got {t.get_device()}")
+        raise ValueError(f"{name} must be contiguous")
 
     def query(self, what: int) -> int:
         return _query(f"lstm_dyn_{self._kind}_query", self.handle, what)
@@ -286,6 +288,7 @@ class GatedScan(_Handle):
     def __init__(self, B: int, H: int, T_max: int, dtype="bf16"):
         self.B, self.H, self.T = B, H, T_max
         self.dtype, self._et = _dtype(dtype)
+        self._device = _torch.cuda.current_device()
         self.handle = lstm_dyn_scan_create(B, H, T_max, self.dtype)
 
     def _forward(self, call, z, lengths, h0, out_h, out_y, stream):
@@ -294,17 +297,17 @@ class GatedScan(_Handle):
                 return self._forward(call, z, lengths, h0, out_h, out_y, None)
         torch = _torch
         B, T, H = self.B, self.T, self.H
-        _check("z", z, self._et, (B, T, 3 * H))
-        _check("lengths", lengths, torch.int32, (B,))
-        _check("h0", h0, torch.float32, (B, H))
+        self._check("z", z, self._et, (B, T, 3 * H))
+        self._check("lengths", lengths, torch.int32, (B,))
+        self._check("h0", h0, torch.float32, (B, H))
         if out_h is None:
             out_h = torch.empty_like(h0)
         else:
-            _check("out_h", out_h, torch.float32, (B, H))
+            self._check("out_h", out_h, torch.float32, (B, H))
         if out_y is None:
             out_y = torch.empty((B, T, H), dtype=self._et, device=z.device)
         else:
-            _check("out_y", out_y, self._et, (B, T, H))
+            self._check("out_y", out_y, self._et, (B, T, H))
         _ok(getattr(_ready, call)(self.handle, z.data_ptr(), lengths.data_ptr(), h0.data_ptr(), out_h.data_ptr(),
                                   out_y.data_ptr(), _stream(z.device)), call)
         return out_y, out_h
@@ -329,19 +332,19 @@ class GatedScan(_Handle):
                 return self.backward(z, lengths, h0, dy, d_out_h, None, out)
         torch = _torch
         B, T, H = self.B, self.T, self.H
-        _check("z", z, self._et, (B, T, 3 * H))
-        _check("lengths", lengths, torch.int32, (B,))
-        _check("h0", h0, torch.float32, (B, H))
-        _check("dy", dy, self._et, (B, T, H))
+        self._check("z", z, self._et, (B, T, 3 * H))
+        self._check("lengths", lengths, torch.int32, (B,))
+        self._check("h0", h0, torch.float32, (B, H))
+        self._check("dy", dy, self._et, (B, T, H))
         if d_out_h is not None:
-            _check("d_out_h", d_out_h, torch.float32, (B, H))
+            self._check("d_out_h", d_out_h, torch.float32, (B, H))
         if out is None:
             out = {"dz": torch.empty_like(z), "dh0": torch.empty_like(h0)}
         else:
             if sorted(out) != ["dh0", "dz"]:
                 raise ValueError("out must hold exactly ['dh0', 'dz']")
-            _check("dz", out["dz"], self._et, (B, T, 3 * H))
-            _check("dh0", out["dh0"], torch.float32, (B, H))
+            self._check("dz", out["dz"], self._et, (B, T, 3 * H))
+            self._check("dh0", out["dh0"], torch.float32, (B, H))
         _ok(_ready.lstm_dyn_scan_backward(self.handle, z.data_ptr(), lengths.data_ptr(), h0.data_ptr(),
                                           dy.data_ptr(), d_out_h.data_ptr() if d_out_h is not None else 0,
                                           out["dz"].data_ptr(), out["dh0"].data_ptr(), _stream(z.device)),
@@ -356,16 +359,16 @@ class GatedScan(_Handle):
                 return self.step(z, h, out_h, out_y)
         torch = _torch
         R, H = h.shape[0], self.H
-        _check("z", z, self._et, (R, 3 * H))
-        _check("h", h, torch.float32, (R, H))
+        self._check("z", z, self._et, (R, 3 * H))
+        self._check("h", h, torch.float32, (R, H))
         if out_h is None:
             out_h = torch.empty_like(h)
         else:
-            _check("out_h", out_h, torch.float32, (R, H))
+            self._check("out_h", out_h, torch.float32, (R, H))
         if out_y is None:
             out_y = torch.empty_like(h, dtype=self._et)
         else:
-            _check("out_y", out_y, self._et, (R, H))
+            self._check("out_y", out_y, self._et, (R, H))
         _ok(_ready.lstm_dyn_scan_step(R, H, self.dtype, z.data_ptr(), h.data_ptr(), out_h.data_ptr(),
                                       out_y.data_ptr(), _stream(z.device)), "lstm_dyn_scan_step")
         return out_y, out_h
@@ -381,14 +384,15 @@ class TokenEmbed(_Handle):
     def __init__(self, B: int, T_max: int, V: int, D: int, dtype="bf16", scale: float = 1.0):
         self.B, self.T, self.V, self.D, self.scale = B, T_max, V, D, float(scale)
         self.dtype, self._et = _dtype(dtype)
+        self._device = _torch.cuda.current_device()
         self.handle = lstm_dyn_embed_create(B, T_max, V, D, self.dtype)
 
     def _tokens(self, tokens, lengths):
         torch = _torch
-        _check("tokens", tokens, torch.int32, (self.B, self.T))
+        self._check("tokens", tokens, torch.int32, (self.B, self.T))
         if lengths is None:
             return 0
-        _check("lengths", lengths, torch.int32, (self.B,))
+        self._check("lengths", lengths, torch.int32, (self.B,))
         return lengths.data_ptr()
 
     def forward(self, tokens, lengths, table, out_x=None, stream=None):
@@ -397,11 +401,11 @@ class TokenEmbed(_Handle):
                 return self.forward(tokens, lengths, table, out_x)
         torch = _torch
         L = self._tokens(tokens, lengths)
-        _check("table", table, self._et, (self.V, self.D))
+        self._check("table", table, self._et, (self.V, self.D))
         if out_x is None:
             out_x = torch.empty((self.B, self.T, self.D), dtype=self._et, device=table.device)
         else:
-            _check("out_x", out_x, self._et, (self.B, self.T, self.D))
+            self._check("out_x", out_x, self._et, (self.B, self.T, self.D))
         _ok(_ready.lstm_dyn_embed_forward(self.handle, tokens.data_ptr(), L, table.data_ptr(), self.scale,
                                           out_x.data_ptr(), _stream(table.device)), "lstm_dyn_embed_forward")
         return out_x
@@ -417,11 +421,11 @@ class TokenEmbed(_Handle):
         torch = _torch
         L = self._tokens(tokens, lengths)
         code = BF16 if isinstance(dx, torch.Tensor) and dx.dtype == torch.bfloat16 else F32
-        _check("dx", dx, torch.bfloat16 if code == BF16 else torch.float32, (self.B, self.T, self.D))
+        self._check("dx", dx, torch.bfloat16 if code == BF16 else torch.float32, (self.B, self.T, self.D))
         if out is None:
             out = torch.empty((self.V, self.D), dtype=torch.float32, device=dx.device)
         else:
-            _check("out", out, torch.float32, (self.V, self.D))
+            self._check("out", out, torch.float32, (self.V, self.D))
         _ok(_ready.lstm_dyn_embed_backward(self.handle, tokens.data_ptr(), L, dx.data_ptr(), code, self.scale,
                                            out.data_ptr(), _stream(dx.device)), "lstm_dyn_embed_backward")
         return out
@@ -447,14 +451,15 @@ class AdamW(_Handle):
         if state_bits not in (8, 32):
             raise ValueError("state_bits must be 8 or 32")
         self.bits, self.betas, self.eps, self.steps_done = state_bits, betas, eps, int(steps_done)
+        self._device = torch.cuda.current_device()
         wd = [float(weight_decay)] * len(self.params) if isinstance(weight_decay, (int, float)) else list(weight_decay)
         if len(wd) != len(self.params):
             raise ValueError("weight_decay must be one number or one per tensor")
         self.m, self.v, self.m_exp, self.v_exp, rows = [], [], [], [], []
         for i, (p, c) in enumerate(zip(self.params, self.copies)):
-            _check(f"params[{i}]", p, torch.float32, p.shape)
+            self._check(f"params[{i}]", p, torch.float32, p.shape)
             if c is not None:
-                _check(f"copies[{i}]", c, torch.bfloat16, p.shape)
+                self._check(f"copies[{i}]", c, torch.bfloat16, p.shape)
             n, dev = p.numel(), p.device
             if state_bits == 32:
                 self.m.append(torch.zeros(p.shape, dtype=torch.float32, device=dev))
@@ -495,7 +500,7 @@ class AdamW(_Handle):
         if et not in (torch.float32, torch.bfloat16):
             raise TypeError("gradients must be float32 or bfloat16 device tensors")
         for g, p in zip(grads, self.params):
-            _check("a gradient", g, et, p.shape)
+            self._check("a gradient", g, et, p.shape)
         _ok(_ready.lstm_dyn_adamw_step(self.handle, self._pointers(*[g.data_ptr() for g in grads]),
                                        BF16 if et == torch.bfloat16 else F32, lr, self.betas[0], self.betas[1],
                                        self.eps, grad_scale, self.steps_done + 1, _stream(grads[0].device)),
@@ -527,6 +532,7 @@ class BeamSearch(_Handle):
     def __init__(self, B: int, K: int, V: int, dtype="bf16", end=None):
         self.B, self.K, self.V, self.end = B, K, V, -1 if end is None else int(end)
         self.dtype, self._et = _dtype(dtype)
+        self._device = _torch.cuda.current_device()
         self.handle = lstm_dyn_beam_create(B, K, V, self.dtype)
         self._rows = (BeamState * BEAM_MAX_STATES)()
 
@@ -543,9 +549,9 @@ class BeamSearch(_Handle):
                 return self.step(logits, scores, finished, states, out_states)
         torch = _torch
         B, K = self.B, self.K
-        _check("logits", logits, self._et, (B, K, self.V))
-        _check("scores", scores, torch.float32, (B, K))
-        _check("finished", finished, torch.uint8, (B, K))
+        self._check("logits", logits, self._et, (B, K, self.V))
+        self._check("scores", scores, torch.float32, (B, K))
+        self._check("finished", finished, torch.uint8, (B, K))
         if len(states) > BEAM_MAX_STATES:
             raise ValueError(f"at most {BEAM_MAX_STATES} states, got {len(states)}")
         if out_states is None:
@@ -555,8 +561,8 @@ class BeamSearch(_Handle):
         rows = self._rows      # read before the call returns
         for i, (s, d) in enumerate(zip(states, out_states)):
             shape = s.shape
-            _check("a state", s, s.dtype, shape)
-            _check("a state's output", d, s.dtype, shape)
+            self._check("a state", s, s.dtype, shape)
+            self._check("a state's output", d, s.dtype, shape)
             if shape[:2] != (B, K):
                 raise ValueError(f"states[{i}] must have shape ({B}, {K}, ...), got {tuple(shape)}")
             row = rows[i]
