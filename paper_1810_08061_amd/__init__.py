@@ -289,6 +289,8 @@ class LstmDyn:
         self.mode = _MODES[mode] if isinstance(mode, str) else int(mode)
         self.cell = _CELLS[cell] if isinstance(cell, str) else int(cell)
         self.handle = lstm_dyn_create_cell(B, D, H, T_max, self.dtype, self.mode, self.cell)
+        import torch
+        self._device = torch.cuda.current_device()
 
     def _check(self, name, t, dtype, shape):
         import torch
@@ -298,12 +300,12 @@ class LstmDyn:
             raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
         if tuple(t.shape) != tuple(shape):
             raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+        if t.get_device() != self._device:
+            raise ValueError(f"{name} must be on the handle's device {self._device}, got {t.get_device()}")
         if not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous")
 
-    def _inputs(self, x, lengths, W, U, b, h0, c0, out_h, out_c, stream):
-        """Check the inputs, allocate missing outputs; returns (c0 pointer,
-        out_h, out_c, stream handle)."""
+    def _check_inputs(self, x, lengths, W, U, b, h0, c0):
         import torch
         B, D, H, T = self.B, self.D, self.H, self.T
         et = torch.bfloat16 if self.dtype == BF16 else torch.float32
@@ -316,6 +318,13 @@ class LstmDyn:
             self._check(name, t, dt, shape)
         if c0 is not None or self.cell == CELL_LSTM:
             self._check("c0", c0, torch.float32, (B, H))
+
+    def _inputs(self, x, lengths, W, U, b, h0, c0, out_h, out_c, stream):
+        """Check the inputs, allocate missing outputs; returns (c0 pointer,
+        out_h, out_c, stream handle)."""
+        import torch
+        B, H = self.B, self.H
+        self._check_inputs(x, lengths, W, U, b, h0, c0)
         if out_h is None:
             out_h = torch.empty((B, H), dtype=torch.float32, device=x.device)
         if out_c is None:
@@ -403,6 +412,7 @@ class LstmDyn:
         B, D, H, T = self.B, self.D, self.H, self.T
         g, nb = _CELL_SHAPES[self.cell]
         lstm = self.cell == CELL_LSTM
+        self._check_inputs(x, lengths, W, U, b, h0, c0 if lstm else None)
         dev = x.device
         self._check("d_out_h", d_out_h, torch.float32, (B, H))
         if lstm or d_out_c is not None:

@@ -1,4 +1,4 @@
-"""The operators' wrappers refuse a tensor of another GPU than their handle's, argument by argument, before
+"""The loop's and the operators' wrappers refuse a tensor of another GPU than their handle's, argument by argument, before
 any call of the library: its address would be read by kernels of the handle's GPU.  The tensors
 here are CPU tensors that say which device they are on; the library is not called."""
 import types
@@ -79,3 +79,36 @@ def test_a_tensor_of_another_device_is_refused(name, no_library):
         with pytest.raises(ValueError, match="device"):
             call(m, *others)
         assert not [n for n in no_library if not n.endswith(("create", "destroy"))], a
+
+
+def test_the_loops_wrapper_refuses_them_too(monkeypatch):
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(ld, "lstm_dyn_create_cell", lambda *a: None)
+    called = []
+    for f in ("lstm_dyn_forward", "lstm_dyn_forward_seq", "lstm_dyn_forward_train", "lstm_dyn_backward", "lstm_dyn_forward_stop"):
+        monkeypatch.setattr(ld, f, lambda *a, f=f: called.append(f))
+    D = 3
+    m = ld.LstmDyn(B, D, H, T, "f32")
+    weights = {"x": (B, T, D), "lengths": (B,), "W": (D, 4 * H), "U": (H, 4 * H), "b": (4 * H,), "h0": (B, H), "c0": (B, H)}
+    outs = {"out_h": (B, H), "out_c": (B, H)}
+    seq = {"out_seq": (B, T, H)}
+    back = dict(weights, d_out_h=(B, H), d_out_c=(B, H), d_seq=(B, T, H))
+    grads = {"dx": (B, T, D), "dW": (D, 4 * H), "dU": (H, 4 * H), "db": (4 * H,), "dh0": (B, H), "dc0": (B, H)}
+    for call, shapes, extra in ((m.forward, dict(weights, **outs), {}), (m.forward_seq, dict(weights, **outs, **seq), {}),
+                                (m.forward_train, dict(weights, **outs, **seq), {}),
+                                (m.forward_stop, dict(weights, stop_v=(H,), **outs, out_steps=(B,), **seq), {"stop_c": 0.0}),
+                                (m.backward, back, {}), (m.backward, dict(back, **grads), {})):
+        for odd in [None] + list(shapes):
+            t = {n: _tensor(s, I if n in ("lengths", "out_steps") else F) for n, s in shapes.items()}
+            if odd:
+                t[odd].number = 1
+            if grads.keys() <= t.keys():
+                t["out"] = {n: t.pop(n) for n in grads}
+            del called[:]
+            if odd is None:
+                call(stream=5, **t, **extra)
+                assert len(called) == 1
+                continue
+            with pytest.raises(ValueError, match="device"):
+                call(stream=5, **t, **extra)
+            assert not called, odd
