@@ -271,6 +271,16 @@ def lstm_dyn_check_stop_args(B: int, D: int, H: int, T_max: int, dtype: int, cel
 
 # --- torch convenience wrapper ---------------------------------------------
 
+def _on(stream):
+    """The context of a call that names its stream (a torch stream or its address): as torch's own, so that
+    what the call allocates belongs to that stream, and neither earlier work of the
+    current stream nor its later allocations touch it."""
+    from torch import cuda
+    if not hasattr(stream, "cuda_stream"):
+        stream = cuda.ExternalStream(int(stream)) if int(stream) else cuda.default_stream()
+    return cuda.stream(stream)
+
+
 class LstmDyn:
     """One handle of the library for fixed (B, D, H, T_max, dtype, mode, cell).
 
@@ -280,6 +290,8 @@ class LstmDyn:
     h0/c0 float32 [B, H]; it returns (out_h, out_c) float32 [B, H].
     LSTM: G = 4H, b [4H].  GRU: G = 3H, b [6H] = b_ih ++ b_hh.  RNN: G = H,
     b [H].  GRU and RNN: c0 is ignored (may be None) and out_c is zeros.
+    A call runs on the current stream; ``stream=`` (a torch stream or its address)
+    is short for ``with torch.cuda.stream(stream)``.
     """
 
     def __init__(self, B: int, D: int, H: int, T_max: int, dtype="bf16", mode="persistent",
@@ -319,7 +331,7 @@ class LstmDyn:
         if c0 is not None or self.cell == CELL_LSTM:
             self._check("c0", c0, torch.float32, (B, H))
 
-    def _inputs(self, x, lengths, W, U, b, h0, c0, out_h, out_c, stream):
+    def _inputs(self, x, lengths, W, U, b, h0, c0, out_h, out_c):
         """Check the inputs, allocate missing outputs; returns (c0 pointer,
         out_h, out_c, stream handle)."""
         import torch
@@ -331,13 +343,14 @@ class LstmDyn:
             out_c = torch.empty((B, H), dtype=torch.float32, device=x.device)
         self._check("out_h", out_h, torch.float32, (B, H))
         self._check("out_c", out_c, torch.float32, (B, H))
-        if stream is None:
-            stream = torch.cuda.current_stream(x.device)
-        s = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+        s = torch.cuda.current_stream(x.device).cuda_stream
         return (c0.data_ptr() if c0 is not None else 0), out_h, out_c, s
 
     def forward(self, x, lengths, W, U, b, h0, c0=None, out_h=None, out_c=None, stream=None):
-        c0p, out_h, out_c, s = self._inputs(x, lengths, W, U, b, h0, c0, out_h, out_c, stream)
+        if stream is not None:
+            with _on(stream):
+                return self.forward(x, lengths, W, U, b, h0, c0, out_h, out_c)
+        c0p, out_h, out_c, s = self._inputs(x, lengths, W, U, b, h0, c0, out_h, out_c)
         lstm_dyn_forward(self.handle, x.data_ptr(), lengths.data_ptr(), W.data_ptr(),
                          U.data_ptr(), b.data_ptr(), h0.data_ptr(), c0p,
                          out_h.data_ptr(), out_c.data_ptr(), s)
@@ -350,8 +363,11 @@ class LstmDyn:
         """``forward``, and also the output sequence out_seq float32 [B, T_max, H]:
         the hidden state of row b after step t for t < L[b], zero after.
         Returns (out_h, out_c, out_seq)."""
+        if stream is not None:
+            with _on(stream):
+                return self.forward_seq(x, lengths, W, U, b, h0, c0, out_h, out_c, out_seq)
         import torch
-        c0p, out_h, out_c, s = self._inputs(x, lengths, W, U, b, h0, c0, out_h, out_c, stream)
+        c0p, out_h, out_c, s = self._inputs(x, lengths, W, U, b, h0, c0, out_h, out_c)
         if out_seq is None:
             out_seq = torch.empty((self.B, self.T, self.H), dtype=torch.float32, device=x.device)
         self._check("out_seq", out_seq, torch.float32, (self.B, self.T, self.H))
@@ -366,8 +382,12 @@ class LstmDyn:
         after a step that leaves stop_v . h + stop_c > 0 (stop_v float32 [H]);
         lengths are caps.  Returns (out_h, out_c, out_steps) and, with
         ``with_seq`` or a given ``out_seq``, the output sequence after them."""
+        if stream is not None:
+            with _on(stream):
+                return self.forward_stop(x, lengths, W, U, b, h0, c0, stop_v, stop_c, out_h, out_c, out_steps,
+                                         out_seq, with_seq)
         import torch
-        c0p, out_h, out_c, s = self._inputs(x, lengths, W, U, b, h0, c0, out_h, out_c, stream)
+        c0p, out_h, out_c, s = self._inputs(x, lengths, W, U, b, h0, c0, out_h, out_c)
         self._check("stop_v", stop_v, torch.float32, (self.H,))
         if out_steps is None:
             out_steps = torch.empty((self.B,), dtype=torch.int32, device=x.device)
@@ -388,8 +408,11 @@ class LstmDyn:
         """``forward`` that also keeps what ``backward`` needs.
         Returns (out_h, out_c) and, with ``with_seq`` or a given ``out_seq``,
         the output sequence after them."""
+        if stream is not None:
+            with _on(stream):
+                return self.forward_train(x, lengths, W, U, b, h0, c0, out_h, out_c, out_seq, with_seq)
         import torch
-        c0p, out_h, out_c, s = self._inputs(x, lengths, W, U, b, h0, c0, out_h, out_c, stream)
+        c0p, out_h, out_c, s = self._inputs(x, lengths, W, U, b, h0, c0, out_h, out_c)
         if out_seq is None and with_seq:
             out_seq = torch.empty((self.B, self.T, self.H), dtype=torch.float32, device=x.device)
         if out_seq is not None:
@@ -408,6 +431,9 @@ class LstmDyn:
         RNN ignore c0 and d_out_c (None allowed).  out: a dict with those keys
         holding caller-owned contiguous tensors of those shapes (4-byte
         aligned), which receive the gradients and are returned."""
+        if stream is not None:
+            with _on(stream):
+                return self.backward(x, lengths, W, U, b, h0, c0, d_out_h, d_out_c, d_seq, None, out)
         import torch
         B, D, H, T = self.B, self.D, self.H, self.T
         g, nb = _CELL_SHAPES[self.cell]
@@ -429,9 +455,7 @@ class LstmDyn:
                 raise ValueError(f"out must hold exactly {sorted(shapes)}")
             for k, v in shapes.items():
                 self._check(k, out[k], torch.float32, v)
-        if stream is None:
-            stream = torch.cuda.current_stream(dev)
-        s = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+        s = torch.cuda.current_stream(dev).cuda_stream
         ptr = lambda t: t.data_ptr() if t is not None else 0
         lstm_dyn_backward(self.handle, x.data_ptr(), lengths.data_ptr(), W.data_ptr(), U.data_ptr(),
                           b.data_ptr(), h0.data_ptr(), ptr(c0) if lstm else 0, d_out_h.data_ptr(),

@@ -14,7 +14,7 @@ from __future__ import annotations
 
 import ctypes
 
-from . import BF16, F32, OK, LstmDynError, _DTYPES, _load
+from . import BF16, F32, OK, LstmDynError, _DTYPES, _load, _on
 
 ERR_BAD_TOKENS = 8
 OPS_Q_STATUS, OPS_Q_WORKSPACE_BYTES, OPS_Q_LAUNCHES = range(3)
@@ -215,16 +215,6 @@ def _t():
 
 def _stream(device):
     return _torch.cuda.current_stream(device).cuda_stream
-
-
-def _on(stream):
-    """The context of a call that names its stream (a torch stream or its address): as torch's own, so that
-    what the call allocates belongs to that stream, and neither earlier work of the
-    current stream nor its later allocations touch it."""
-    cuda = _torch.cuda
-    if not hasattr(stream, "cuda_stream"):
-        stream = cuda.ExternalStream(int(stream)) if int(stream) else cuda.default_stream()
-    return cuda.stream(stream)
 
 
 def _dtype(dtype):

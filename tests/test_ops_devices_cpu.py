@@ -84,6 +84,7 @@ def test_a_tensor_of_another_device_is_refused(name, no_library):
 def test_the_loops_wrapper_refuses_them_too(monkeypatch):
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
     monkeypatch.setattr(ld, "lstm_dyn_create_cell", lambda *a: None)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device: types.SimpleNamespace(cuda_stream=0))
     called = []
     for f in ("lstm_dyn_forward", "lstm_dyn_forward_seq", "lstm_dyn_forward_train", "lstm_dyn_backward", "lstm_dyn_forward_stop"):
         monkeypatch.setattr(ld, f, lambda *a, f=f: called.append(f))
@@ -106,9 +107,9 @@ def test_the_loops_wrapper_refuses_them_too(monkeypatch):
                 t["out"] = {n: t.pop(n) for n in grads}
             del called[:]
             if odd is None:
-                call(stream=5, **t, **extra)
+                call(**t, **extra)
                 assert len(called) == 1
                 continue
             with pytest.raises(ValueError, match="device"):
-                call(stream=5, **t, **extra)
+                call(**t, **extra)
             assert not called, odd
