@@ -2,15 +2,17 @@
 // backward pass.
 //
 //   a_t = sigmoid(zf_t), k_t = 1 - a_t = sigmoid(-zf_t), s_t = sigmoid(zo_t)
-//   h_t = h_{t-1} + k_t (v_t - h_{t-1}),   y_t = s_t h_t
+//   h_t = a_t h_{t-1} + k_t v_t,   y_t = s_t h_t
 // and back, with e_t the gradient of h_t from later steps (e_{L-1} = d_out_h):
 //   g_t = s_t dy_t + e_t,   e_{t-1} = a_t g_t
 //   dzf = g_t (h_{t-1} - v_t) a_t k_t,   dzv = g_t k_t,   dzo = dy_t h_t s_t (1 - s_t)
 //
-// h_t is written as a correction of h_{t-1}, so that its error at small k_t is k_t's
-// own relative one and not that of 1 - a_t (after a reset, k_t = 1, the state is the
-// candidate to within a rounding of the larger of the two).  All of it is fp32; y and
-// dz are rounded once, to the data's type.
+// a and k are both formed to their own relative error (the smaller from exp(-|zf|), the
+// larger as one minus it), so a small k keeps its share over a long memory, and a
+// small a leaves nothing of a large state in the candidate that replaces it.  The sum of
+// the two products is finite where its operands are, and infinite where one of them
+// is; a correction h + k (v - h) is neither.  All of it is fp32; y and dz are
+// rounded once, to the data's type.
 //
 // Bound by memory: forward (3 + 1) and backward (4 + 3) elements of the data a step and
 // channel, each read or written once.  A step is an affine map of the state, so the time
@@ -69,6 +71,20 @@ struct ScanParams {
 // 1 / (1 + e^x), which is 1 and 0 at the infinities.
 __device__ inline float logistic_neg(float x) { return rcp_f(1.0f + __expf(x)); }
 
+// The smaller of a = sigmoid(x) and k = sigmoid(-x), with x's sign: one register holds both, each to its
+// own relative error.  gate_keep gives a, gate_take k.
+__device__ inline float gate_code(float x) {
+    const float e = __expf(-fabsf(x));
+    return copysignf(e * rcp_f(1.0f + e), x);
+}
+__device__ inline bool gate_low(float q) { return __float_as_int(q) < 0; }  // also where a is -0
+__device__ inline float gate_keep(float q) { return gate_low(q) ? -q : 1.0f - q; }
+__device__ inline float gate_take(float q) { return gate_low(q) ? 1.0f + q : q; }
+
+// The compiler may not form anything of x before here, nor keep what it formed of it (a bf16 pair widened
+// early, or both gates of a code kept, take twice the registers).
+__device__ inline void hold(float& x) { asm volatile("" : "+v"(x)); }
+
 // V elements as they lie in memory, in 32-bit words.
 template <class E, int V>
 struct Raw {
@@ -79,8 +95,6 @@ struct Raw {
         if constexpr (sizeof(E) == 4) return __uint_as_float(w[i]);
         else return __uint_as_float(i ? w[0] & 0xffff0000u : w[0] << 16);
     }
-    // The compiler may not form anything of this before here (a bf16 pair widened early takes
-    // twice the registers).
     __device__ void hold() {
 #pragma unroll
         for (int i = 0; i < N; ++i) asm volatile("" : "+v"(w[i]));
@@ -363,7 +377,7 @@ __device__ inline void forward_share(const ScanParams& p, const Place<E, V, NT, 
     const long row = (long)at.b * H + at.c;
     const E* z = static_cast<const E*>(p.z) + at.step0(p) * 3 * H;
     E* y = static_cast<E*>(p.y) + at.step0(p) * H;
-    float k[R][V], A[V], S[V];
+    float q[R][V], A[V], S[V];
     Raw<E, V> f[R], v[R], o[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -379,10 +393,10 @@ __device__ inline void forward_share(const ScanParams& p, const Place<E, V, NT, 
     for (int r = 0; r < R; ++r) {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            k[r][i] = logistic_neg(f[r][i]);
-            const float s = fmaf(k[r][i], v[r][i] - S[i], S[i]);
-            const float a = fmaf(-k[r][i], A[i], A[i]);
-            if (WHOLE || t0 + r < L) S[i] = s, A[i] = a;
+            q[r][i] = gate_code(f[r][i]);
+            const float a = gate_keep(q[r][i]);
+            const float s = fmaf(a, S[i], gate_take(q[r][i]) * v[r][i]);
+            if (WHOLE || t0 + r < L) S[i] = s, A[i] *= a;
         }
     }
     // The output gates are on their way while the runs are joined; earlier they would only
@@ -398,7 +412,11 @@ __device__ inline void forward_share(const ScanParams& p, const Place<E, V, NT, 
     carry_on<WAY>(p, at, at.seg, -1, at.first + G * R >= L, p.h0 + row, tA, tS, start, seen, p.out_h + row);
     if (!at.on) return;
 #pragma unroll
-    for (int r = 0; r < R; ++r) v[r].hold(), o[r].hold();
+    for (int r = 0; r < R; ++r) {
+        v[r].hold(), o[r].hold();
+#pragma unroll
+        for (int i = 0; i < V; ++i) hold(q[r][i]);
+    }
 #pragma unroll
     for (int i = 0; i < V; ++i) h[i] = fmaf(A[i], start[at.cl * V + i], S[i]);
     if (p.kept && t0 < L) {
@@ -411,7 +429,7 @@ __device__ inline void forward_share(const ScanParams& p, const Place<E, V, NT, 
         float out[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            h[i] = fmaf(k[r][i], v[r][i] - h[i], h[i]);
+            h[i] = fmaf(gate_keep(q[r][i]), h[i], gate_take(q[r][i]) * v[r][i]);
             out[i] = logistic_neg(-o[r][i]) * h[i];
             if (!WHOLE && t0 + r >= L) out[i] = 0.0f;
         }
@@ -470,17 +488,18 @@ __device__ inline void backward_share(const ScanParams& p, const Place<E, V, NT,
     for (int r = 0; r < R; ++r) {
         float out[V];
         const bool valid = WHOLE || t0 + r < L;
+
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const float kk = logistic_neg(zf[r][i]);
+            const float gf = gate_code(zf[r][i]), kk = gate_take(gf);
             const float s = logistic_neg(-zo[r][i]);
             const float qq = s * zd[r][i];
-            const float diff = zv[r][i] - h[i];
-            h[i] = fmaf(kk, diff, h[i]);
+            f[r][i] = (h[i] - zv[r][i]) * kk * (1.0f - kk);
+            h[i] = fmaf(gate_keep(gf), h[i], kk * zv[r][i]);
             out[i] = valid ? qq * h[i] * (1.0f - s) : 0.0f;
             k[r][i] = valid ? kk : 0.0f;
             q[r][i] = valid ? qq : 0.0f;
-            f[r][i] = -diff * kk * (1.0f - kk);
+            hold(f[r][i]), hold(q[r][i]);
         }
         if (at.on && (WHOLE || t0 + r < p.T)) store_at<FAR, E, V>(dz + ((long)r * 3 + 2) * H, at.zoff, out);
     }
@@ -564,7 +583,8 @@ scan_step_kernel(const E* z, const float* h, float* out_h, E* y, int rows, int H
     for (int j = 0; j < V; ++j) s[j] = h[r * H + c + j];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        s[j] = fmaf(logistic_neg(f[j]), v[j] - s[j], s[j]);
+        const float q = gate_code(f[j]);
+        s[j] = fmaf(gate_keep(q), s[j], gate_take(q) * v[j]);
         out[j] = logistic_neg(-o[j]) * s[j];
     }
 #pragma unroll
