@@ -72,7 +72,7 @@ struct ScanParams {
 __device__ inline float logistic_neg(float x) { return rcp_f(1.0f + __expf(x)); }
 
 // The smaller of a = sigmoid(x) and k = sigmoid(-x), with x's sign: one register holds both, each to its
-// own relative error.  gate_keep gives a, gate_take k.
+// own relative error.  gate_keep gives a, gate_take k; their product is gate_slope.
 __device__ inline float gate_code(float x) {
     const float e = __expf(-fabsf(x));
     return copysignf(e * rcp_f(1.0f + e), x);
@@ -80,6 +80,7 @@ __device__ inline float gate_code(float x) {
 __device__ inline bool gate_low(float q) { return __float_as_int(q) < 0; }  // also where a is -0
 __device__ inline float gate_keep(float q) { return gate_low(q) ? -q : 1.0f - q; }
 __device__ inline float gate_take(float q) { return gate_low(q) ? 1.0f + q : q; }
+__device__ inline float gate_slope(float q) { return fabsf(q) * (1.0f - fabsf(q)); }
 
 // The compiler may not form anything of x before here, nor keep what it formed of it (a bf16 pair widened
 // early, or both gates of a code kept, take twice the registers).
@@ -466,7 +467,7 @@ __device__ inline void backward_share(const ScanParams& p, const Place<E, V, NT,
     const E* z = static_cast<const E*>(p.z) + at.step0(p) * 3 * H;
     const E* dy = static_cast<const E*>(p.dy) + at.step0(p) * H;
     E* dz = static_cast<E*>(p.dz) + at.step0(p) * 3 * H;
-    // per step: the gate's complement, s dy, and dzf's factor of g
+    // per step: the gate's code, s dy, and dzf's factor of g
     float k[R][V], q[R][V], f[R][V], A[V], S[V], h[V] = {};
     Raw<E, V> zf[R], zv[R], zo[R], zd[R];
     if (WHOLE || t0 < L) {
@@ -488,17 +489,14 @@ __device__ inline void backward_share(const ScanParams& p, const Place<E, V, NT,
     for (int r = 0; r < R; ++r) {
         float out[V];
         const bool valid = WHOLE || t0 + r < L;
-
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const float gf = gate_code(zf[r][i]), kk = gate_take(gf);
-            const float s = logistic_neg(-zo[r][i]);
-            const float qq = s * zd[r][i];
-            f[r][i] = (h[i] - zv[r][i]) * kk * (1.0f - kk);
-            h[i] = fmaf(gate_keep(gf), h[i], kk * zv[r][i]);
-            out[i] = valid ? qq * h[i] * (1.0f - s) : 0.0f;
-            k[r][i] = valid ? kk : 0.0f;
-            q[r][i] = valid ? qq : 0.0f;
+            const float gf = gate_code(zf[r][i]), go = gate_code(zo[r][i]), d = zd[r][i];
+            f[r][i] = (h[i] - zv[r][i]) * gate_slope(gf);
+            h[i] = fmaf(gate_keep(gf), h[i], gate_take(gf) * zv[r][i]);
+            out[i] = valid ? d * h[i] * gate_slope(go) : 0.0f;
+            k[r][i] = valid ? gf : 0.0f;
+            q[r][i] = valid ? gate_keep(go) * d : 0.0f;
             hold(f[r][i]), hold(q[r][i]);
         }
         if (at.on && (WHOLE || t0 + r < p.T)) store_at<FAR, E, V>(dz + ((long)r * 3 + 2) * H, at.zoff, out);
@@ -509,9 +507,10 @@ __device__ inline void backward_share(const ScanParams& p, const Place<E, V, NT,
     for (int r = R - 1; r >= 0; --r) {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const float t = q[r][i] + S[i];
-            S[i] = fmaf(-k[r][i], t, t);
-            A[i] = fmaf(-k[r][i], A[i], A[i]);
+            hold(k[r][i]);
+            const float a = gate_keep(k[r][i]);
+            S[i] = a * (q[r][i] + S[i]);
+            A[i] *= a;
         }
     }
     float tA[V], tS[V], e[V] = {};
@@ -527,10 +526,11 @@ __device__ inline void backward_share(const ScanParams& p, const Place<E, V, NT,
         const bool valid = WHOLE || t0 + r < L;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
+            hold(k[r][i]);
             const float gr = q[r][i] + e[i];
             df[i] = valid ? gr * f[r][i] : 0.0f;
-            dv[i] = valid ? gr * k[r][i] : 0.0f;
-            e[i] = valid ? fmaf(-k[r][i], gr, gr) : e[i];
+            dv[i] = valid ? gr * gate_take(k[r][i]) : 0.0f;
+            e[i] = valid ? gate_keep(k[r][i]) * gr : e[i];
         }
         if (WHOLE || t0 + r < p.T) {
             store_at<FAR, E, V>(dz + (long)r * 3 * H, at.zoff, df);

@@ -142,3 +142,41 @@ def test_operands_at_the_ends_of_the_range():
         for t in range(T):
             _, x = m.step(z[:, t].contiguous().cuda(), x)
             _within(f"step {t}", x[0], h[t + 1], bound[t + 1])
+
+
+def _gradients(f, v, o, h, hb, dy, dh):
+    """dz (its three blocks) and dh0 with their bounds, in 64 bits: the gradient carried back is bounded as
+    the states are, a product by the sum of its factors' relative errors and its roundings."""
+    a, k, s, s1 = ou.sigmoid(f), ou.sigmoid(-f), ou.sigmoid(o), ou.sigmoid(-o)
+    e, ME, BE = dh, np.abs(dh), np.zeros_like(dh)
+    dz, bounds = np.zeros((3,) + f.shape), np.zeros((3,) + f.shape)
+    for t in reversed(range(len(f))):
+        q = s[t] * np.abs(dy[t])
+        g, MG, BG = s[t] * dy[t] + e, q + ME, BE + (_eps(o[t]) + 3 * U) * q
+        B, slope = BG + 64 * U * MG, a[t] * k[t]
+        d = h[t] - v[t]
+        dz[:, t] = g * d * slope, g * k[t], dy[t] * h[t + 1] * s[t] * s1[t]
+        bounds[:, t] = ((B + np.abs(g) * (2 * _eps(f[t]) + 8 * U)) * np.abs(d) * slope + (np.abs(g) + B) * slope * hb[t],
+                        B * k[t] + np.abs(g) * k[t] * (_eps(f[t]) + 2 * U),
+                        np.abs(dy[t]) * s[t] * s1[t] * (hb[t + 1] + np.abs(h[t + 1]) * (2 * _eps(o[t]) + 8 * U)))
+        e, ME = a[t] * g, a[t] * MG
+        BE = a[t] * (BG + MG * (_eps(f[t]) + 3 * U))
+    return dz, bounds * (1 + 1e-4), e, BE + 64 * U * ME
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("low,high", [(0, 4), (4, 12), (8, 20), (20, 40)])
+@pytest.mark.parametrize("T,H", [(1, 33), (7, 64), (40, 10), (700, 20)])
+def test_gradients(T, H, low, high, dtype):
+    z, L, h0, dy, dh = _inputs(T, H, dtype, 100 * T + high, low, high)
+    f, v, o = (q[0] for q in np.split(z.double().numpy(), 3, 2))
+    h, hb = _states(f, v, h0[0].double().numpy())
+    dz, bz, dh0, bh = _gradients(f, v, o, h, hb, dy[0].double().numpy(), dh[0].double().numpy())
+    rel = 2.0 ** -8 if dtype == "bf16" else 0.0
+    dev = [t.cuda() for t in (z, L, h0, dy, dh)]
+    with ld.GatedScan(1, H, T, dtype) as m:
+        m.forward_train(*dev[:3])
+        d = m.backward(*dev)
+        for i, name in enumerate(("dzf", "dzv", "dzo")):
+            _within(name, d["dz"][0, :, i * H:(i + 1) * H], dz[i], bz[i], rel)
+        _within("dh0", d["dh0"][0], dh0, bh)
