@@ -60,7 +60,9 @@ enum {
  * where it is infinite step by step. */
 typedef struct lstm_dyn_scan lstm_dyn_scan_t;
 
-/* B, H, T_max >= 1, B * T_max < 2^31, H < 2^18. */
+/* B, H, T_max >= 1, B * T_max < 2^31, H < 2^18, T_max < 2^31 - 256, and a launch of less than
+ * 2^32 threads: for a row and each 64 of its channels (32 of odd H) about two a step with bf16
+ * data, four with fp32, at least 64 a row.  Beyond these ERR_UNSUPPORTED. */
 int lstm_dyn_scan_create(lstm_dyn_scan_t** out, int B, int H, int T_max, int dtype);
 
 int lstm_dyn_scan_forward(lstm_dyn_scan_t* h, const void* z, const int32_t* lengths,
@@ -87,7 +89,9 @@ int lstm_dyn_scan_backward(lstm_dyn_scan_t* h, const void* z, const int32_t* len
 
 /* One step of `rows` independent rows (a decoder's): z [rows][3H], h and out_h
  * [rows][H] fp32 (out_h may be h itself), out_y [rows][H] dtype; z and out_y
- * aligned to their elements.  No handle. */
+ * aligned to their elements; rows, H >= 1, H < 2^18, less than about 2^32 elements, four times as
+ * many where H is a multiple of four and z and out_y are aligned to four elements (else
+ * ERR_UNSUPPORTED).  No handle. */
 int lstm_dyn_scan_step(int rows, int H, int dtype, const void* z, const float* h, float* out_h,
                        void* out_y, void* stream);
 

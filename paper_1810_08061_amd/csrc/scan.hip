@@ -592,9 +592,43 @@ scan_step_kernel(const E* z, const float* h, float* out_h, E* y, int rows, int H
     store_vec<E, V>(y + r * H + c, out);
 }
 
+struct Shape {
+    int threads, lanes;  // of a workgroup; of those along the channels
+    int steps;           // of a share
+    int segs, tiles;
+    int way;             // see carry_on
+};
+
+int scan_run_of(int dtype) { return dtype == LSTM_DYN_BF16 ? run_of<__bf16>() : run_of<float>(); }
+int scan_vec_of(int H) { return H % 2 ? 1 : 2; }
+
+// The smallest workgroup that holds all steps, up to `most` threads.
+Shape scan_shape(int B, int H, int T, int dtype, int num_cus, int most) {
+    const int run = scan_run_of(dtype), vec = scan_vec_of(H);
+    Shape w{64, 64, 0, 0, 0, ONE};
+    while (w.threads < most && w.threads / 64 * run < T) w.threads *= 2;
+    if (w.threads == most && most / 64 * run < T) w.lanes = 32;  // the longer share: fewer in a row's chain
+    w.steps = w.threads / w.lanes * run;
+    w.segs = (int)(((long long)T + w.steps - 1) / w.steps);
+    w.tiles = (H + w.lanes * vec - 1) / (w.lanes * vec);
+    // Some 16 shares of a chain on the device at once hide its waits (two rows of 16384 x 2048,
+    // 64 chains: 120 us in a plain chain, 123 with the maps); with fewer chains than that the chain's
+    // own time counts (one row of 32768 x 2048, 32 chains: 139 and 124; x 512, 8
+    // chains, with its backward: 255 and 131).
+    if (w.segs > 1) w.way = w.segs > 2 && 8LL * B * w.tiles <= num_cus ? WINDOW : CHAIN;
+    return w;
+}
+
 int check_scan_sizes(int B, int H, int T, int dtype) {
     if (B < 1 || H < 1 || T < 1 || !valid_dtype(dtype)) return LSTM_DYN_ERR_INVALID;
     if ((long long)B * T > 0x7fffffffLL || H >= 1 << 18) return LSTM_DYN_ERR_UNSUPPORTED;
+    // the kernels count steps up to a share past T in 32 bits, a launch its threads
+    for (int most : {FWD_THREADS, BWD_THREADS}) {
+        const Shape w = scan_shape(B, H, T, dtype, 0, most);
+        if ((long long)T + w.steps > 0x7fffffffLL) return LSTM_DYN_ERR_UNSUPPORTED;
+        const long long per_row = (long long)w.tiles * w.segs * w.threads;  // under 2^49
+        if (per_row > 0xffffffffLL || B * per_row > 0xffffffffLL) return LSTM_DYN_ERR_UNSUPPORTED;
+    }
     return LSTM_DYN_OK;
 }
 
@@ -621,12 +655,6 @@ int check_scan_backward(int B, int H, int T, int dtype, const void* z, const int
 
 using namespace ldyn;
 
-struct Shape {
-    int threads, lanes;  // of a workgroup; of those along the channels
-    int segs, tiles;
-    int way;             // see carry_on
-};
-
 struct lstm_dyn_scan : OpsHandle {
     int B, H, T, dtype;
     int run, vec;  // steps and channels of a thread
@@ -635,22 +663,6 @@ struct lstm_dyn_scan : OpsHandle {
     float* kept = nullptr;  // made by the first forward for training
     bool has_kept = false;
 };
-
-// The smallest workgroup that holds all steps, up to `most` threads.
-static Shape scan_shape(const lstm_dyn_scan* h, int most) {
-    Shape w{64, 64, 0, 0, ONE};
-    while (w.threads < most && w.threads / 64 * h->run < h->T) w.threads *= 2;
-    if (w.threads == most && most / 64 * h->run < h->T) w.lanes = 32;  // the longer share: fewer in a row's chain
-    const int steps = w.threads / w.lanes * h->run;
-    w.segs = (h->T + steps - 1) / steps;
-    w.tiles = (h->H + w.lanes * h->vec - 1) / (w.lanes * h->vec);
-    // Some 16 shares of a chain on the device at once hide its waits (two rows of 16384 x 2048,
-    // 64 chains: 120 us in a plain chain, 123 with the maps); with fewer chains than that the chain's
-    // own time counts (one row of 32768 x 2048, 32 chains: 139 and 124; x 512, 8
-    // chains, with its backward: 255 and 131).
-    if (w.segs > 1) w.way = w.segs > 2 && 8L * h->B * w.tiles <= h->num_cus ? WINDOW : CHAIN;
-    return w;
-}
 
 template <bool FAR, class E, int V>
 static void scan_launch(const lstm_dyn_scan* h, const ScanParams& p, bool back) {
@@ -731,10 +743,10 @@ extern "C" int lstm_dyn_scan_create(lstm_dyn_scan_t** out, int B, int H, int T, 
         delete h;
         return rc;
     }
-    h->run = dtype == LSTM_DYN_BF16 ? run_of<__bf16>() : run_of<float>();
-    h->vec = H % 2 ? 1 : 2;
-    h->fwd = scan_shape(h, FWD_THREADS);
-    h->bwd = scan_shape(h, BWD_THREADS);
+    h->run = scan_run_of(dtype);
+    h->vec = scan_vec_of(H);
+    h->fwd = scan_shape(B, H, T, dtype, h->num_cus, FWD_THREADS);
+    h->bwd = scan_shape(B, H, T, dtype, h->num_cus, BWD_THREADS);
     auto bytes = [&](const Shape& w) {
         return w.segs > 1 ? 8LL * COUNTER_WORDS * B * w.tiles + (w.way == WINDOW ? 24LL : 8LL) * B * w.segs * H : 0;
     };
@@ -805,8 +817,9 @@ extern "C" int lstm_dyn_scan_backward(lstm_dyn_scan_t* h, const void* z, const i
 
 extern "C" int lstm_dyn_scan_step(int rows, int H, int dtype, const void* z, const float* h,
                                   float* out_h, void* out_y, void* stream) {
-    int rc = check_scan_sizes(rows, H, 1, dtype);
-    if (rc != LSTM_DYN_OK) return rc;
+    if (rows < 1 || H < 1 || !valid_dtype(dtype)) return LSTM_DYN_ERR_INVALID;
+    if (H >= 1 << 18) return LSTM_DYN_ERR_UNSUPPORTED;
+    int rc;
     const long long e = dtype_bytes(dtype), n = (long long)rows * H;
     const Span s[] = {{z, 3 * n * e, (int)e, false}, {h, 4 * n, 4, false}, {out_h, 4 * n, 4, true, h},
                       {out_y, n * e, (int)e, true}};
@@ -815,6 +828,7 @@ extern "C" int lstm_dyn_scan_step(int rows, int H, int dtype, const void* z, con
     const bool vec = H % 4 == 0 && ((reinterpret_cast<uintptr_t>(z) | reinterpret_cast<uintptr_t>(out_y)) &
                                     (uintptr_t)(4 * e - 1)) == 0;
     const int V = vec ? 4 : 1;
+    if (n / V > 0xffffffffLL - 255) return LSTM_DYN_ERR_UNSUPPORTED;  // threads of a launch
     const unsigned grid = (unsigned)((n / V + 255) / 256);
     hipStream_t st = static_cast<hipStream_t>(stream);
 #define LDYN_STEP(E, VV)                                                                              \
