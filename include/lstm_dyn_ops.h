@@ -121,7 +121,9 @@ int lstm_dyn_check_scan_args(int B, int H, int T_max, int dtype, const void* z,
  * depend on the sizes alone: the same call gives the same bits. */
 typedef struct lstm_dyn_embed lstm_dyn_embed_t;
 
-/* All sizes >= 1; B * T_max < 2^30, V < 2^27, D < 2^21. */
+/* All sizes >= 1; B * T_max < 2^30, V < 2^27, D < 2^21; for the gradient also B * T_max / 32 times
+ * the tiles of 256 columns (128 where D is no multiple of four, 64 of odd D) under
+ * 2^26 - 2^16.  Beyond these ERR_UNSUPPORTED. */
 int lstm_dyn_embed_create(lstm_dyn_embed_t** out, int B, int T_max, int V, int D, int dtype);
 int lstm_dyn_embed_forward(lstm_dyn_embed_t* h, const int32_t* tokens, const int32_t* lengths,
                            const void* table, float scale, void* out_x, void* stream);

@@ -427,6 +427,10 @@ embed_join_kernel(EmbedParams p, const uint32_t* __restrict__ key, float* __rest
     }
 }
 
+constexpr int PIECE = 32;  // places of a piece, where there are many
+int columns_of(int D) { return D % 4 == 0 ? 4 : D % 2 == 0 ? 2 : 1; }  // of a lane
+int column_tiles(int D) { return (D + 64 * columns_of(D) - 1) / (64 * columns_of(D)); }
+
 int check_embed_sizes(int B, int T, int V, int D, int dtype) {
     if (B < 1 || T < 1 || V < 1 || D < 1 || !valid_dtype(dtype)) return LSTM_DYN_ERR_INVALID;
     if ((long long)B * T >= 1LL << 30 || V >= 1 << 27 || D >= 1 << 21) return LSTM_DYN_ERR_UNSUPPORTED;
@@ -445,6 +449,8 @@ int check_embed_backward(int B, int T, int V, int D, const int32_t* tokens, cons
                          const void* dx, int dx_dtype, const float* dt) {
     if (!valid_dtype(dx_dtype)) return LSTM_DYN_ERR_INVALID;
     const long long N = (long long)B * T;
+    // the sums' threads: a wave for 32 places and a tile of columns, and those that write the zeros
+    if ((N + PIECE - 1) / PIECE * column_tiles(D) + (1 << 16) >= 1LL << 26) return LSTM_DYN_ERR_UNSUPPORTED;
     const Span s[] = {{tokens, 4 * N, 4, false}, {dx, dtype_bytes(dx_dtype) * N * D, 16, false},
                       {dt, 4LL * V * D, 16, true}, {lengths, 4LL * B, 4, false}};
     return check_spans(s, lengths ? 4 : 3);
@@ -468,9 +474,9 @@ struct lstm_dyn_embed : OpsHandle {
 // Pieces of up to 32 places, shorter where they would leave fewer than eight
 // waves a CU on the gradient (945 places of 333 columns: 16 us with 64, 5.6 with 8).
 static void embed_shape(lstm_dyn_embed* h) {
-    h->W = h->D % 4 == 0 ? 4 : h->D % 2 == 0 ? 2 : 1;
-    h->tiles = (h->D + 64 * h->W - 1) / (64 * h->W);
-    h->R = 32;
+    h->W = columns_of(h->D);
+    h->tiles = column_tiles(h->D);
+    h->R = PIECE;
     while (h->R > 8 && (long long)h->N / h->R * h->tiles < 8LL * h->num_cus) h->R /= 2;
 }
 

@@ -45,3 +45,15 @@ def test_scan_step():
     assert step(2 ** 30, 16) == UNSUPPORTED           # four elements a thread
     assert step(4, 2 ** 18) == UNSUPPORTED
     assert step(0, 4) == step(4, 0) == step(4, 4, 9) == ld.ERR_INVALID
+
+
+@pytest.mark.parametrize("D,tiles", [(1, 1), (64, 1), (65, 2), (67, 2), (130, 2), (260, 2), (513, 9), (2048, 8)])
+def test_embed(D, tiles):
+    def chk(N):
+        V = 5
+        tok, table, x, dx, dt = _place([4 * N, 2 * V * D, 2 * N * D, 2 * N * D, 4 * V * D])
+        if N < 2 ** 30:     # the lookup has no such launch
+            assert ops.lstm_dyn_check_embed_args(1, N, V, D, ld.BF16, tok, 0, table, x, 0, ld.BF16, 0) == OK
+        return ops.lstm_dyn_check_embed_args(1, N, V, D, ld.BF16, tok, 0, 0, 0, dx, ld.BF16, dt)
+    last = min(2 ** 30 - 1, 32 * ((2 ** 26 - 2 ** 16 - 1) // tiles))
+    assert chk(last) == OK and chk(last + 1) == UNSUPPORTED
