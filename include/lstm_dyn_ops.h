@@ -17,7 +17,8 @@
  * As in lstm_dyn.h: buffers are caller-owned DEVICE memory, row-major and
  * contiguous; a handle is used from one host thread at a time with one call in
  * flight; calls only enqueue work on `stream` (a hipStream_t; NULL = the default
- * stream), never wait for the host and allocate nothing, so they can be captured
+ * stream), never wait for the host and allocate nothing (the first
+ * lstm_dyn_scan_forward_train of a handle apart), so they can be captured
  * in a graph; the handle owns its workspace, made at create for the current
  * device, and is used with that device current (else ERR_INVALID).  Host
  * argument problems are returned synchronously; problems in device data
@@ -70,7 +71,8 @@ int lstm_dyn_scan_forward(lstm_dyn_scan_t* h, const void* z, const int32_t* leng
 
 /* lstm_dyn_scan_forward, also keeping in the handle what lstm_dyn_scan_backward
  * needs (a state every few steps; the first call allocates room for them:
- * about B * T_max * H / 4 bytes with bf16 data, twice that with fp32).  out_h may
+ * about B * T_max * H / 4 bytes with bf16 data, twice that with fp32; under a
+ * capture it is refused with ERR_INVALID, later calls are not).  out_h may
  * not be h0.  Any other forward on the handle discards what was kept. */
 int lstm_dyn_scan_forward_train(lstm_dyn_scan_t* h, const void* z, const int32_t* lengths,
                                 const float* h0, float* out_h, void* out_y, void* stream);

@@ -766,6 +766,14 @@ static int scan_forward_impl(lstm_dyn_scan* h, const void* z, const int32_t* len
     int rc = check_scan_forward(h->B, h->H, h->T, h->dtype, z, lengths, h0, out_h, out_y);
     if (rc != LSTM_DYN_OK) return rc;
     if (train && out_h == h0) return LSTM_DYN_ERR_INVALID;  // the backward reads h0
+    if (train && !h->kept) {  // memory is not allocated under a capture, which the attempt would end
+        hipStreamCaptureStatus capture;
+        if (hipStreamIsCapturing(static_cast<hipStream_t>(stream), &capture) != hipSuccess) {
+            (void)hipGetLastError();
+            return LSTM_DYN_ERR_HIP;
+        }
+        if (capture != hipStreamCaptureStatusNone) return LSTM_DYN_ERR_INVALID;
+    }
     if ((rc = ops_begin(h, stream)) != LSTM_DYN_OK) return rc;
     h->has_kept = false;
     if (train && !h->kept) {
