@@ -28,6 +28,8 @@ constexpr int SORT_BITS = 9, SORT_BINS = 1 << SORT_BITS;
 constexpr int SORT_BLOCKS = 256;  // at most; each reads the counts of all
 static_assert(SORT_BINS == SORT_THREADS, "a thread per digit");
 
+constexpr long long FAR_BYTES = 256LL << 20;  // of x; see the launch
+
 struct EmbedParams {
     const int32_t* tokens;
     const int32_t* lengths;
@@ -552,9 +554,12 @@ extern "C" int lstm_dyn_embed_forward(lstm_dyn_embed_t* h, const int32_t* tokens
     const EmbedParams p = embed_params(h, tokens, lengths, scale);
     long grid = ((long)h->N + 3) / 4;
     if (grid > 64L * h->num_cus) grid = 64L * h->num_cus;
-    // An x larger than the last cache is read from memory by whoever comes next: its
-    // stores bypass the caches (256 x 1000 x 1024 in bf16: 138 us against 156).
-    const bool far = (long long)h->N * h->D * dtype_bytes(h->dtype) > FAR_BYTES;
+    // An x about as large as the last cache is read from memory by whoever comes next: its stores
+    // bypass the caches, which then keep what else there is.  The lookup alone takes the same
+    // time; with a product that reads x behind it 128 MB take 75 us so and 78 past the caches, 192 MB
+    // 122 and 119, 256 MB 161 and 157, 512 MB 318 and 299; with a plain reading pass 192 MB 98
+    // and 116, 256 MB 164 and 151.
+    const bool far = (long long)h->N * h->D * dtype_bytes(h->dtype) >= FAR_BYTES;
 #define LDYN_EMB(E, W)                                                                               \
     hipLaunchKernelGGL((far ? embed_forward_kernel<true, E, W> : embed_forward_kernel<false, E, W>), \
                        dim3((unsigned)grid), dim3(256), 0, h->last_stream, p,                        \

@@ -166,8 +166,7 @@ __device__ inline void load_vec(const E* p, float* out) {
         for (int i = 0; i < V; ++i) out[i] = (float)x[i];
     }
 }
-// The same store; FAR: past the caches, for an output larger than FAR_BYTES.
-constexpr long long FAR_BYTES = 32LL << 20;
+// The same store; FAR: past the caches, for an output that its reader finds in memory anyway.
 template <bool FAR, class E, int V>
 __device__ inline void put(E* p, const float* in) {
     typename Vec<E, V>::type x;
