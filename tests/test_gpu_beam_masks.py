@@ -128,3 +128,17 @@ def test_a_beam_with_all_its_tokens_masked(dtype):
                 _check_order(m, logits.to(et), s, 0.0, f"all masked, V {V}")
                 got, parent, token, _, _ = _step(m, logits.to(et), s, torch.zeros((1, K), dtype=torch.uint8))
                 assert (parent[0] == shift).all() and token[0].tolist() == list(range(K))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("K,V", [(1, 1), (1, 2), (3, 3), (4, 63), (2, 64), (5, 65), (8, 1000), (32, 33), (3, 255), (16, 4096),
+                                 (7, 4097), (4, 8193), (2, 50001), (32, 20000), (8, 32768), (4, 300)])
+def test_the_very_order(K, V, dtype):
+    """Ordinary logits: each sequence's choice in order, equal logits of a beam by the lowest token."""
+    import torch
+    g = torch.Generator().manual_seed(10 * K + V)
+    logits = (torch.randn((6, K, V), generator=g) * 3).to(torch.float32 if dtype == "f32" else torch.bfloat16)
+    scores = -5 + torch.randn((6, K), generator=g)
+    with ld.BeamSearch(6, K, V, dtype) as m:
+        _check_order(m, logits, scores, 40.0, "order")
+        assert m.status() == ld.OK
