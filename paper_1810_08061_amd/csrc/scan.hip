@@ -27,8 +27,8 @@
 // states are formed again.
 //
 // Measured: 32 x 4096 x 2048 in bf16, ragged, forward 0.34 ms (4.0 TB/s of what it has to
-// move), backward 0.59 ms (4.6 TB/s); a 2 GiB copy reaches 4.9.  One row of
-// 32768 x 2048: 0.12 ms (4.3 TB/s).  One thread a channel, step by step: 7.5 ms and 17.8.
+// move), backward 0.60 ms (4.5 TB/s); a 2 GiB copy reaches 4.9.  One row of
+// 32768 x 2048: 0.126 ms (4.2 TB/s).  One thread a channel, step by step: 7.5 ms and 17.8.
 #include "ops.h"
 
 #include <type_traits>
@@ -44,9 +44,9 @@ enum Way { ONE, CHAIN, WINDOW };
 template <class E>
 constexpr int run_of() { return sizeof(E) == 2 ? 16 : 8; }
 
-// The largest workgroups.  The backward holds 160 registers a thread with bf16
-// data, so three waves a SIMD: workgroups of 256 (0.63 ms for 32 x 4096 x 2048;
-// of 512 it spills, 0.79 ms).
+// The largest workgroups.  The backward holds 140 registers a thread with bf16
+// data, so three waves a SIMD: workgroups of 256 (a training step of 32 x 4096 x 2048
+// 946 us, of 512 962).
 constexpr int FWD_THREADS = 512, BWD_THREADS = 256;
 
 constexpr long long FAR_BYTES = 32LL << 20;  // of y or dz; see the launch
@@ -614,9 +614,9 @@ Shape scan_shape(int B, int H, int T, int dtype, int num_cus, int most) {
     w.segs = (int)(((long long)T + w.steps - 1) / w.steps);
     w.tiles = (H + w.lanes * vec - 1) / (w.lanes * vec);
     // Some 16 shares of a chain on the device at once hide its waits (two rows of 16384 x 2048,
-    // 64 chains: 120 us in a plain chain, 123 with the maps); with fewer chains than that the chain's
-    // own time counts (one row of 32768 x 2048, 32 chains: 139 and 124; x 512, 8
-    // chains, with its backward: 255 and 131).
+    // 64 chains: 121 us in a plain chain, 127 with the maps); with fewer chains than that the chain's
+    // own time counts (one row of 32768 x 2048, 32 chains: 141 and 127; x 512, 8
+    // chains, with its backward: 256 and 128).
     if (w.segs > 1) w.way = w.segs > 2 && 8LL * B * w.tiles <= num_cus ? WINDOW : CHAIN;
     return w;
 }
