@@ -492,3 +492,4 @@ class LstmDyn:
 
 
 from .ops import AdamW, BeamSearch, GatedScan, TokenEmbed  # noqa: E402  (they use the names above)
+from .layer import GradClip, LayerNorm, LinearAttention, TokenSample  # noqa: E402

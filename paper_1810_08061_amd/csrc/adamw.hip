@@ -18,6 +18,7 @@
 // tensor, found in a table made at create.  The gradients' addresses come with
 // the launch, since a program may have its gradients elsewhere in every step.
 #include "ops.h"
+#include "../../include/lstm_dyn_layer.h"
 
 #include <algorithm>
 #include <cmath>
@@ -57,6 +58,7 @@ struct AdamwParams {
     uint32_t chunk0;
     int tensor0;
     float lr, b1, nb1, b2, nb2, eps, gs, c1, rc2;  // nb = 1 - b, rounded once
+    const float* clip;       // gradients are each times clip[1] in place of gs, if not NULL
 };
 
 template <class E>
@@ -143,6 +145,7 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamwParams a, Grads grads) 
     const Tensor t = a.tensors[ti];
     const G* g = static_cast<const G*>(grads.g[ti - a.tensor0]);
     const bool gvec = (reinterpret_cast<uintptr_t>(g) & (4 * sizeof(G) - 1)) == 0;
+    const float gs = a.clip ? a.clip[1] : a.gs;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const long long base = (long long)(chunk - t.first) * CHUNK;
     for (int j = w; j < CHUNK / BLOCK; j += 4) {
@@ -168,7 +171,7 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamwParams a, Grads grads) 
             // Every product and sum is rounded by itself (no fused multiply-add),
             // so the same formula in plain fp32 gives the same codes.
 #pragma clang fp contract(off)
-            const float gi = gr[i] * a.gs;
+            const float gi = gr[i] * gs;
             m[i] = a.b1 * m[i] + a.nb1 * gi;
             if constexpr (EIGHT) {
                 // v[i] holds r.  Where both squares would leave fp32's range below, they are
@@ -366,9 +369,8 @@ extern "C" int lstm_dyn_adamw_create(lstm_dyn_adamw_t** out, const lstm_dyn_adam
     return LSTM_DYN_OK;
 }
 
-extern "C" int lstm_dyn_adamw_step(lstm_dyn_adamw_t* h, const void* const* grads, int grad_dtype,
-                                   double lr, double beta1, double beta2, double eps,
-                                   double grad_scale, long long step, void* stream) {
+static int adamw_run(lstm_dyn_adamw* h, const void* const* grads, int grad_dtype, double lr, double beta1,
+                     double beta2, double eps, double grad_scale, const float* clip, long long step, void* stream) {
     if (!h) return LSTM_DYN_ERR_INVALID;
     if (!(beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0 && eps >= 0.0) || lr != lr ||
         grad_scale != grad_scale || step < 1)
@@ -386,13 +388,26 @@ extern "C" int lstm_dyn_adamw_step(lstm_dyn_adamw_t* h, const void* const* grads
         for (int i = 0; i < GROUP; ++i) g.g[i] = i < n ? grads[i0 + i] : nullptr;
         const AdamwParams a{h->tensors, h->owner, c0, i0, (float)lr, (float)beta1, (float)(1.0 - beta1),
                             (float)beta2, (float)(1.0 - beta2), (float)eps, (float)grad_scale,
-                            (float)c1, (float)std::sqrt(c2)};
+                            (float)c1, (float)std::sqrt(c2), clip};
         auto* k = h->bits == 8 ? (grad_dtype == LSTM_DYN_BF16 ? adamw_kernel<true, __bf16> : adamw_kernel<true, float>)
                                : (grad_dtype == LSTM_DYN_BF16 ? adamw_kernel<false, __bf16> : adamw_kernel<false, float>);
         hipLaunchKernelGGL(k, dim3(cn), dim3(256), 0, h->last_stream, a, g);
         if ((rc = ops_launched(h)) != LSTM_DYN_OK) return rc;
     }
     return LSTM_DYN_OK;
+}
+
+extern "C" int lstm_dyn_adamw_step(lstm_dyn_adamw_t* h, const void* const* grads, int grad_dtype,
+                                   double lr, double beta1, double beta2, double eps,
+                                   double grad_scale, long long step, void* stream) {
+    return adamw_run(h, grads, grad_dtype, lr, beta1, beta2, eps, grad_scale, nullptr, step, stream);
+}
+
+extern "C" int lstm_dyn_adamw_step_clipped(lstm_dyn_adamw_t* h, const void* const* grads, int grad_dtype,
+                                           double lr, double beta1, double beta2, double eps,
+                                           const float* result, long long step, void* stream) {
+    if (!h || !result || !is_aligned(result, 4) || on_written(h->written, result, 8)) return LSTM_DYN_ERR_INVALID;
+    return adamw_run(h, grads, grad_dtype, lr, beta1, beta2, eps, 1.0, result, step, stream);
 }
 
 extern "C" int lstm_dyn_adamw_states(lstm_dyn_adamw_t* h, void* const* out_m, void* const* out_v,
@@ -416,7 +431,7 @@ extern "C" int lstm_dyn_adamw_states(lstm_dyn_adamw_t* h, void* const* out_m, vo
             o.m[i] = static_cast<__bf16*>(out_m[i0 + i]);
             o.v[i] = static_cast<__bf16*>(out_v[i0 + i]);
         }
-        const AdamwParams a{h->tensors, h->owner, c0, i0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+        const AdamwParams a{h->tensors, h->owner, c0, i0, 0, 0, 0, 0, 0, 0, 0, 0, 0, nullptr};
         hipLaunchKernelGGL(adamw_states_kernel, dim3(cn), dim3(256), 0, h->last_stream, a, o);
         if ((rc = ops_launched(h)) != LSTM_DYN_OK) return rc;
     }

@@ -1,0 +1,846 @@
+// attend.hip -- linear attention with a decay for each head: S_t = a S_{t-1} + k_t v_t^T,
+// y_t = S_t^T q_t, over whole sequences, its backward pass, and single steps.
+//
+// All four products over a sequence have one form (a "pass"), with a state M [P][R]:
+//     out_i = sum_j a^|i-j| (x_i . y_j) z_j + a^e(i) M^T x_i
+// over j <= i going forward, j >= i going back:
+//            x   y   z   M      direction
+//     y      q   k   v   S      forward
+//     dq     dy  v   k   S^T    forward
+//     dk     v   dy  q   R^T    back        (R_t = q_t dy_t^T + a R_{t+1})
+//     dv     k   q   dy  R      back, leaves dS0
+// so the backward forms S and R again and needs nothing kept.
+//
+// A workgroup goes through a sequence (or a share of it) of one head in chunks, M in its
+// registers in fp32: inside a chunk the products are those of attention under a mask of decays,
+// between chunks they go through M.  A wave owns columns of M and of out.  The
+// layout in which a product leaves M (four rows of one column a lane) is the one in which
+// the next product takes it as an operand, if the other operand's rows are fetched in the
+// same order, so M never leaves the registers.
+//
+// bf16 data: operands of the matrix units are bf16.  x, y and z are that already; the
+// masked products and M are given as two parts (16 bits, 2^-17 of them is left: far
+// below the rounding of out), what is added to M, a^. z, as three (24 bits: the state is fp32).
+// fp32 data: the matrix units' fp32 products.
+//
+// Where rows and heads are fewer than workgroups should be, the time axis is cut into shares:
+// a launch forms what each share adds to the state, one joins them in their order, and
+// the pass's shares start from the joined states.
+#include "ops.h"
+#include "../../include/lstm_dyn_layer.h"
+
+#include <cmath>
+#include <vector>
+
+namespace ldyn {
+namespace {
+
+constexpr int MAX_D = 128;
+constexpr int TABLE = 65;        // powers of a head's decay
+constexpr int WANT_GROUPS = 512; // workgroups that a pass should have
+
+typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+
+// One pass: addresses of its operands in [B][T][ld], their widths, its state.
+struct Pass {
+    const void *x, *y, *z;
+    void* out;
+    long long ldx, ldy, ldz, ldo;   // elements from one step to the next
+    int P, R;
+    int back;                       // direction
+    int transposed;                 // M [P][R] is the transpose of the state as it is kept
+    const float* start;             // [B][heads][Dk][Dv], or NULL: zeros
+    float* end;                     // the same (written), or NULL
+    float* share;                   // [B heads][shares][Dk][Dv]
+};
+
+struct AttendParams {
+    Pass pass[3];
+    const int32_t* lengths;
+    int32_t* status;
+    const float* powers;    // [heads][TABLE]
+    const double* log2a;    // [heads]
+    int passes, T, heads, rows, shares, span, Dv, vec;   // rows = B heads; span: steps of a share
+};
+
+template <class E>
+struct Chunk;
+template <>
+struct Chunk<__bf16> { static constexpr int C = 64; };
+template <>
+struct Chunk<float> { static constexpr int C = 32; };
+constexpr int waves_of(int DP) { return DP == 32 ? 2 : 4; }
+
+__device__ inline double power(const double* log2a, int head, int n) { return n ? exp2(log2a[head] * n) : 1.0; }
+
+// x as the sum of bf16 parts
+__device__ inline void parts(float x, __bf16& hi, __bf16& lo) {
+    hi = (__bf16)x;
+    lo = (__bf16)(x - (float)hi);
+}
+
+// N elements at row t, column c of an operand; zeros where the row or the column is not there
+template <class E, int N>
+__device__ inline typename Vec<E, N>::type fetch(const E* p, bool on, int c, int width, bool vec) {
+    typename Vec<E, N>::type v;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = (E)0.0f;
+    if (!on) return v;
+    if (vec) {
+        if (c < width) v = *reinterpret_cast<const typename Vec<E, N>::type*>(p + c);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (c + i < width) v[i] = p[c + i];
+    }
+    return v;
+}
+
+// A chunk's x, y and z: fetched into registers while the chunk before is worked on, then put into LDS.
+template <class E, int DP, bool STATE>
+struct Stage {
+    static constexpr int C = Chunk<E>::C, THREADS = 64 * waves_of(DP), N = 16 / (int)sizeof(E);
+    static constexpr int COLS = DP / N, ROWS = C * COLS / THREADS;  // a thread's rows, one after another
+    typedef typename Vec<E, N>::type piece_t;
+    piece_t x[ROWS], y[ROWS], z[ROWS];
+
+    __device__ void get(const E* px, const E* py, const E* pz, const Pass& a, int n, bool vec) {
+        const int c = ((int)threadIdx.x % COLS) * N, r0 = ((int)threadIdx.x / COLS) * ROWS;
+#pragma unroll
+        for (int q = 0; q < ROWS; ++q) {
+            const bool on = r0 + q < n;
+            if constexpr (!STATE) x[q] = fetch<E, N>(px + (r0 + q) * a.ldx, on, c, a.P, vec);
+            y[q] = fetch<E, N>(py + (r0 + q) * a.ldy, on, c, a.P, vec);
+            z[q] = fetch<E, N>(pz + (r0 + q) * a.ldz, on, c, a.R, vec);
+        }
+    }
+};
+
+// --- bf16 ------------------------------------------------------------------
+
+// LDS rows of 16-byte pieces, whose places are exchanged within a row by the row's number, so
+// that a column of pieces lies in different banks.
+template <int PIECES>
+__device__ inline int swap_of(int row) {
+    return (row ^ (row >> 3)) & (PIECES < 8 ? PIECES - 1 : 7);
+}
+template <int PIECES>
+__device__ inline __bf16* at(__bf16* base, int row, int piece) {
+    return base + (row * PIECES + (piece ^ swap_of<PIECES>(row))) * 8;
+}
+
+template <int DP, bool STATE>
+struct LdsBf16 {
+    // y by steps makes room for the masked products, two parts of 64 x 64, once they are formed
+    __bf16 x[STATE ? 8 : 64 * DP];
+    __bf16 y[STATE ? 8 : (DP > 64 ? 64 * DP : 64 * 128)];
+    __bf16 yt[DP * 64];
+    __bf16 zt[DP * 64];
+    float powers[TABLE + 3];
+};
+
+template <int DP, bool STATE>
+__device__ inline void put_chunk(LdsBf16<DP, STATE>& s, const Stage<__bf16, DP, STATE>& g) {
+    typedef Stage<__bf16, DP, STATE> G;
+    constexpr int ROWS = G::ROWS, COLS = G::COLS;
+    const int o = (int)threadIdx.x % COLS, r0 = ((int)threadIdx.x / COLS) * ROWS;
+    if constexpr (!STATE) {
+#pragma unroll
+        for (int q = 0; q < ROWS; ++q) {
+            *reinterpret_cast<bf16x8_t*>(at<COLS>(s.x, r0 + q, o)) = g.x[q];
+            *reinterpret_cast<bf16x8_t*>(at<COLS>(s.y, r0 + q, o)) = g.y[q];
+        }
+    }
+    typedef typename Vec<__bf16, ROWS>::type run_t;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        run_t y, z;
+#pragma unroll
+        for (int q = 0; q < ROWS; ++q) {
+            y[q] = g.y[q][e];
+            z[q] = g.z[q][e];
+        }
+        *reinterpret_cast<run_t*>(at<8>(s.yt, 8 * o + e, r0 / 8) + r0 % 8) = y;
+        *reinterpret_cast<run_t*>(at<8>(s.zt, 8 * o + e, r0 / 8) + r0 % 8) = z;
+    }
+}
+
+__device__ inline f32x4_t mfma(bf16x8_t a, bf16x8_t b, f32x4_t c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ inline bf16x8_t join(bf16x4_t a, bf16x4_t b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
+
+// One chunk: n steps, out at its first step.
+template <int DP, bool STATE>
+__device__ inline void work(LdsBf16<DP, STATE>& s, const Pass& a, f32x4_t (&M)[DP / 16][DP / 16 / waves_of(DP)], int n,
+                            __bf16* out) {
+    constexpr int W = waves_of(DP), RT = DP / 16 / W, PT = DP / 16, KB = DP / 32, IT = 4 / W, COLS = DP / 8;
+    const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4;
+    const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    if constexpr (!STATE) {
+        // the products under the mask: this wave's steps i against all j, one column i a lane
+        f32x4_t A[IT][4];
+#pragma unroll
+        for (int q = 0; q < IT; ++q) {
+            const int it = w * IT + q;
+#pragma unroll
+            for (int jt = 0; jt < 4; ++jt) A[q][jt] = f32x4_t{0, 0, 0, 0};
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {
+                const bf16x8_t b = *reinterpret_cast<const bf16x8_t*>(at<COLS>(s.x, 16 * it + l, 4 * kb + g));
+#pragma unroll
+                for (int jt = 0; jt < 4; ++jt)
+                    if (a.back ? jt >= it : jt <= it)
+                        A[q][jt] = mfma(*reinterpret_cast<const bf16x8_t*>(at<COLS>(s.y, 16 * jt + l, 4 * kb + g)), b, A[q][jt]);
+            }
+#pragma unroll
+            for (int jt = 0; jt < 4; ++jt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int d = (16 * it + l) - (16 * jt + 4 * g + r), dist = a.back ? -d : d;
+                    A[q][jt][r] = dist >= 0 ? A[q][jt][r] * s.powers[dist] : 0.0f;
+                }
+        }
+        __syncthreads();   // y by steps has been read
+#pragma unroll
+        for (int q = 0; q < IT; ++q)
+#pragma unroll
+            for (int jt = 0; jt < 4; ++jt) {
+                bf16x4_t hi, lo;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    __bf16 h, o;
+                    parts(A[q][jt][r], h, o);
+                    hi[r] = h;
+                    lo[r] = o;
+                }
+                const int i = 16 * (w * IT + q) + l;
+                *reinterpret_cast<bf16x4_t*>(at<8>(s.y, i, 2 * jt + g / 2) + 4 * (g & 1)) = hi;
+                *reinterpret_cast<bf16x4_t*>(at<8>(s.y + 64 * 64, i, 2 * jt + g / 2) + 4 * (g & 1)) = lo;
+            }
+        __syncthreads();
+    }
+    bf16x8_t z[2][RT];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+            z[kb][rt] = *reinterpret_cast<const bf16x8_t*>(at<8>(s.zt, 16 * (w * RT + rt) + l, 4 * kb + g));
+    if constexpr (!STATE) {
+        f32x4_t O[4][RT];
+#pragma unroll
+        for (int it = 0; it < 4; ++it)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) O[it][rt] = f32x4_t{0, 0, 0, 0};
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            bf16x8_t hi[RT], lo[RT];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    __bf16 h, o;
+                    parts(M[2 * kb + e / 4][rt][e % 4], h, o);
+                    hi[rt][e] = h;
+                    lo[rt][e] = o;
+                }
+#pragma unroll
+            for (int it = 0; it < 4; ++it) {
+                // rows of M in the order in which a lane holds them
+                const bf16x8_t x = join(*reinterpret_cast<const bf16x4_t*>(at<COLS>(s.x, 16 * it + l, 4 * kb + g / 2) + 4 * (g & 1)),
+                                        *reinterpret_cast<const bf16x4_t*>(at<COLS>(s.x, 16 * it + l, 4 * kb + 2 + g / 2) + 4 * (g & 1)));
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) O[it][rt] = mfma(x, lo[rt], mfma(x, hi[rt], O[it][rt]));
+            }
+        }
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = 16 * it + 4 * g + r, e = a.back ? n - 1 - i : i + 1;
+                const float f = s.powers[e < 0 ? 0 : e];   // a row that is not there is all zeros
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) O[it][rt][r] *= f;
+            }
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+                if (a.back ? kb == 1 || it <= 1 : kb == 0 || it >= 2) {
+                    const bf16x8_t hi = *reinterpret_cast<const bf16x8_t*>(at<8>(s.y, 16 * it + l, 4 * kb + g));
+                    const bf16x8_t lo = *reinterpret_cast<const bf16x8_t*>(at<8>(s.y + 64 * 64, 16 * it + l, 4 * kb + g));
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) O[it][rt] = mfma(lo, z[kb][rt], mfma(hi, z[kb][rt], O[it][rt]));
+                }
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const int c = 16 * (w * RT + rt) + l;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int i = 16 * it + 4 * g + r;
+                    if (i < n && c < a.R) out[i * a.ldo + c] = (__bf16)O[it][rt][r];
+                }
+            }
+        }
+    }
+    // the state
+    const float keep = s.powers[n];
+#pragma unroll
+    for (int pt = 0; pt < PT; ++pt)
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) M[pt][rt] *= keep;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+        bf16x8_t z1[RT], z2[RT], z3[RT];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int j = 32 * kb + 8 * g + e, d = a.back ? j + 1 : n - 1 - j;
+            const float f = s.powers[d < 0 ? 0 : d];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const float v = (float)z[kb][rt][e] * f;
+                const __bf16 hi = (__bf16)v;
+                const float left = v - (float)hi;
+                __bf16 mid, lo;
+                parts(left, mid, lo);
+                z1[rt][e] = hi;
+                z2[rt][e] = mid;
+                z3[rt][e] = lo;
+            }
+        }
+#pragma unroll
+        for (int pt = 0; pt < PT; ++pt) {
+            const bf16x8_t y = *reinterpret_cast<const bf16x8_t*>(at<8>(s.yt, 16 * pt + l, 4 * kb + g));
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) M[pt][rt] = mfma(y, z1[rt], mfma(y, z2[rt], mfma(y, z3[rt], M[pt][rt])));
+        }
+    }
+}
+
+// --- fp32 ------------------------------------------------------------------
+
+template <int DP, bool STATE>
+struct LdsF32 {
+    static constexpr int LD = DP + 4;
+    float x[STATE ? 4 : 32 * LD];
+    float y[32 * LD];
+    float z[32 * LD];
+    float a[STATE ? 4 : 32 * 36];
+    float powers[TABLE + 3];
+};
+
+template <int DP, bool STATE>
+__device__ inline void put_chunk(LdsF32<DP, STATE>& s, const Stage<float, DP, STATE>& g) {
+    typedef Stage<float, DP, STATE> G;
+    constexpr int LD = LdsF32<DP, STATE>::LD;
+    const int c = ((int)threadIdx.x % G::COLS) * 4, r0 = ((int)threadIdx.x / G::COLS) * G::ROWS;
+#pragma unroll
+    for (int q = 0; q < G::ROWS; ++q) {
+        if constexpr (!STATE) *reinterpret_cast<f32x4_t*>(s.x + (r0 + q) * LD + c) = g.x[q];
+        *reinterpret_cast<f32x4_t*>(s.y + (r0 + q) * LD + c) = g.y[q];
+        *reinterpret_cast<f32x4_t*>(s.z + (r0 + q) * LD + c) = g.z[q];
+    }
+}
+
+__device__ inline f32x4_t mfma(float a, float b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+
+template <int DP, bool STATE>
+__device__ inline void work(LdsF32<DP, STATE>& s, const Pass& a, f32x4_t (&M)[DP / 16][DP / 16 / waves_of(DP)], int n,
+                            float* out) {
+    constexpr int W = waves_of(DP), RT = DP / 16 / W, PT = DP / 16, LD = LdsF32<DP, STATE>::LD;
+    const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4;
+    const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    if constexpr (!STATE) {
+#pragma unroll
+        for (int pair = 0; pair < 4; ++pair) {
+            if (pair % W != w) continue;
+            const int it = pair >> 1, jt = pair & 1;
+            f32x4_t A = {0, 0, 0, 0};
+            if (a.back ? jt >= it : jt <= it)
+#pragma unroll
+                for (int pt = 0; pt < PT; ++pt) {
+                    const f32x4_t y = *reinterpret_cast<const f32x4_t*>(s.y + (16 * jt + l) * LD + 16 * pt + 4 * g);
+                    const f32x4_t x = *reinterpret_cast<const f32x4_t*>(s.x + (16 * it + l) * LD + 16 * pt + 4 * g);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) A = mfma(y[r], x[r], A);
+                }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int d = (16 * it + l) - (16 * jt + 4 * g + r), dist = a.back ? -d : d;
+                A[r] = dist >= 0 ? A[r] * s.powers[dist] : 0.0f;
+            }
+            *reinterpret_cast<f32x4_t*>(s.a + (16 * it + l) * 36 + 16 * jt + 4 * g) = A;
+        }
+        __syncthreads();
+    }
+    float z[2][RT][4];
+#pragma unroll
+    for (int jt = 0; jt < 2; ++jt)
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) z[jt][rt][r] = s.z[(16 * jt + 4 * g + r) * LD + 16 * (w * RT + rt) + l];
+    if constexpr (!STATE) {
+#pragma unroll
+        for (int it = 0; it < 2; ++it) {
+            f32x4_t O[RT];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) O[rt] = f32x4_t{0, 0, 0, 0};
+#pragma unroll
+            for (int pt = 0; pt < PT; ++pt) {
+                const f32x4_t x = *reinterpret_cast<const f32x4_t*>(s.x + (16 * it + l) * LD + 16 * pt + 4 * g);
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) O[rt] = mfma(x[r], M[pt][rt][r], O[rt]);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = 16 * it + 4 * g + r, e = a.back ? n - 1 - i : i + 1;
+                const float f = s.powers[e < 0 ? 0 : e];
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) O[rt][r] *= f;
+            }
+#pragma unroll
+            for (int jt = 0; jt < 2; ++jt)
+                if (a.back ? jt >= it : jt <= it) {
+                    const f32x4_t A = *reinterpret_cast<const f32x4_t*>(s.a + (16 * it + l) * 36 + 16 * jt + 4 * g);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) O[rt] = mfma(A[r], z[jt][rt][r], O[rt]);
+                }
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const int c = 16 * (w * RT + rt) + l;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int i = 16 * it + 4 * g + r;
+                    if (i < n && c < a.R) out[i * a.ldo + c] = O[rt][r];
+                }
+            }
+        }
+    }
+    const float keep = s.powers[n];
+#pragma unroll
+    for (int pt = 0; pt < PT; ++pt)
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) M[pt][rt] *= keep;
+#pragma unroll
+    for (int jt = 0; jt < 2; ++jt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int j = 16 * jt + 4 * g + r, d = a.back ? j + 1 : n - 1 - j;
+            const float f = s.powers[d < 0 ? 0 : d];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) z[jt][rt][r] *= f;
+#pragma unroll
+            for (int pt = 0; pt < PT; ++pt) {
+                const float y = s.y[j * LD + 16 * pt + l];
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) M[pt][rt] = mfma(y, z[jt][rt][r], M[pt][rt]);
+            }
+        }
+}
+
+template <class E, int DP, bool STATE>
+struct LdsOf { typedef LdsBf16<DP, STATE> type; };
+template <int DP, bool STATE>
+struct LdsOf<float, DP, STATE> { typedef LdsF32<DP, STATE> type; };
+
+// --- the passes ----------------------------------------------------------------
+
+// STATE: what each share adds to the state, alone.
+template <class E, int DP, bool STATE>
+__global__ void __launch_bounds__(64 * waves_of(DP), 2) attend_kernel(AttendParams p) {
+    constexpr int C = Chunk<E>::C, W = waves_of(DP), RT = DP / 16 / W, PT = DP / 16;
+    __shared__ typename LdsOf<E, DP, STATE>::type s;
+    // the passes of one share, which read the same rows, go to one chiplet (eight in turn) one after another
+    const unsigned item = blockIdx.x / (8u * p.passes) * 8u + blockIdx.x % 8u;
+    if (item >= (unsigned)p.rows * (unsigned)p.shares) return;
+    const Pass& a = p.pass[blockIdx.x / 8u % (unsigned)p.passes];
+    const int row = (int)(item / (unsigned)p.shares), share = (int)(item % (unsigned)p.shares);
+    const int b = row / p.heads, head = row % p.heads;
+    const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4, w = threadIdx.x >> 6;
+    const int L = row_length(p.lengths, b, p.T, p.status, head == 0 && share == 0 && threadIdx.x == 0);
+    const int t0 = share * p.span, span = min(p.span, p.T - t0);
+    const int len = max(0, min(L - t0, span));
+    // the last share has no successor going forward, the first none going back
+    if (STATE && (len == 0 || share == (a.back ? 0 : p.shares - 1))) return;
+
+    for (int i = threadIdx.x; i <= C; i += 64 * W) s.powers[i] = p.powers[head * TABLE + i];
+    const long long step0 = (long long)b * p.T + t0;
+    const E* px = static_cast<const E*>(a.x) + step0 * a.ldx + head * a.P;
+    const E* py = static_cast<const E*>(a.y) + step0 * a.ldy + head * a.P;
+    const E* pz = static_cast<const E*>(a.z) + step0 * a.ldz + head * a.R;
+    E* out = STATE ? nullptr : static_cast<E*>(a.out) + step0 * a.ldo + head * a.R;
+
+    f32x4_t M[PT][RT];
+    const int PR = a.P * a.R;
+    const float* start = p.shares > 1 ? a.share + ((long long)row * p.shares + share) * PR
+                                      : (a.start ? a.start + (long long)row * PR : nullptr);
+#pragma unroll
+    for (int pt = 0; pt < PT; ++pt)
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = 16 * pt + 4 * g + r, c = 16 * (w * RT + rt) + l;
+                M[pt][rt][r] = !STATE && start && i < a.P && c < a.R ? start[a.transposed ? c * p.Dv + i : i * p.Dv + c] : 0.0f;
+            }
+
+    const int chunks = (len + C - 1) / C;
+    Stage<E, DP, STATE> stage;
+    auto chunk_of = [&](int c) { return a.back ? chunks - 1 - c : c; };
+    auto fetch_chunk = [&](int c) {
+        const int k = chunk_of(c) * C;
+        stage.get(px + (long long)k * a.ldx, py + (long long)k * a.ldy, pz + (long long)k * a.ldz, a, min(C, len - k),
+                  p.vec != 0);
+    };
+    if (chunks) fetch_chunk(0);
+    for (int c = 0; c < chunks; ++c) {
+        const int k = chunk_of(c) * C;
+        put_chunk(s, stage);
+        __syncthreads();
+        if (c + 1 < chunks) fetch_chunk(c + 1);
+        work(s, a, M, min(C, len - k), out + (long long)k * a.ldo);
+        __syncthreads();
+    }
+
+    float* end = STATE ? a.share + ((long long)row * p.shares + share) * PR : a.end ? a.end + (long long)row * PR : nullptr;
+    if (!STATE && share != (a.back || L == 0 ? 0 : (L - 1) / p.span)) end = nullptr;
+    if (end) {
+#pragma unroll
+        for (int pt = 0; pt < PT; ++pt)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int i = 16 * pt + 4 * g + r, c = 16 * (w * RT + rt) + l;
+                    if (i < a.P && c < a.R) end[a.transposed ? c * p.Dv + i : i * p.Dv + c] = M[pt][rt][r];
+                }
+    }
+    if constexpr (!STATE) {
+        // rows past the length: zeros
+        const int c = threadIdx.x % DP;
+        if (c < a.R)
+            for (int i = len + (int)threadIdx.x / DP; i < span; i += 64 * W / DP) out[i * a.ldo + c] = (E)0.0f;
+    }
+}
+
+// The state every share starts from, in place of what it adds.
+__global__ void __launch_bounds__(256) attend_join_kernel(AttendParams p) {
+    const Pass& a = p.pass[blockIdx.z];
+    const int row = blockIdx.y, PR = a.P * a.R, e = blockIdx.x * 256 + threadIdx.x;
+    if (e >= PR) return;
+    const int b = row / p.heads, head = row % p.heads;
+    const int L = row_length(p.lengths, b, p.T, p.status, false);
+    float* share = a.share + (long long)row * p.shares * PR + e;
+    float state = a.start ? a.start[(long long)row * PR + e] : 0.0f;
+    const float whole = (float)power(p.log2a, head, p.span);
+    for (int i = 0; i < p.shares; ++i) {
+        const int k = a.back ? p.shares - 1 - i : i, len = max(0, min(L - k * p.span, p.span));
+        const float add = len && i < p.shares - 1 ? share[(long long)k * PR] : 0.0f;
+        share[(long long)k * PR] = state;
+        if (len) state = (len == p.span ? whole : (float)power(p.log2a, head, len)) * state + add;
+    }
+}
+
+// --- one step --------------------------------------------------------------------
+
+struct StepParams {
+    const void* z;
+    const float* S;
+    float* out_S;
+    void* out_y;
+    const float* powers;
+    int heads, Dk, Dv;
+};
+
+// A workgroup holds one head of one row; V columns of the state a lane.
+template <class E, int V>
+__global__ void __launch_bounds__(256) attend_step_kernel(StepParams a) {
+    __shared__ float kq[2][MAX_D], y[256 * V];
+    const long long n = blockIdx.x, row = n / a.heads;
+    const int head = (int)(n % a.heads), Dk = a.Dk, Dv = a.Dv;
+    const E* z = static_cast<const E*>(a.z) + row * a.heads * (2 * Dk + Dv);
+    for (int i = threadIdx.x; i < 2 * Dk; i += 256)
+        kq[i >= Dk][i >= Dk ? i - Dk : i] = (float)z[(i >= Dk ? a.heads * Dk + i - Dk : i) + head * Dk];
+    __syncthreads();
+    const float decay = a.powers[head * TABLE + 1];
+    const int cols = (Dv + V - 1) / V, groups = 256 / cols;
+    const int col = threadIdx.x % cols, group = threadIdx.x / cols, c = col * V;
+    float sum[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum[j] = 0.0f;
+    if (group < groups) {
+        float v[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] = (float)z[2 * a.heads * Dk + head * Dv + c + j];
+        const float* S = a.S + n * Dk * Dv + c;
+        float* O = a.out_S + n * Dk * Dv + c;
+#pragma unroll 4
+        for (int i = group; i < Dk; i += groups) {
+            float s[V];
+            load_vec<float, V>(S + i * Dv, s);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                s[j] = decay * s[j] + kq[1][i] * v[j];
+                sum[j] += kq[0][i] * s[j];
+            }
+            store_vec<float, V>(O + i * Dv, s);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) y[threadIdx.x * V + j] = sum[j];
+    __syncthreads();
+    E* out = static_cast<E*>(a.out_y) + n * Dv;
+    for (int e = threadIdx.x; e < Dv; e += 256) {
+        float t = 0.0f;
+        for (int k = 0; k < groups; ++k) t += y[(k * cols) * V + e];
+        out[e] = (E)t;
+    }
+}
+
+// --- host ----------------------------------------------------------------------
+
+int check_sizes(int B, int heads, int Dk, int Dv, int T, int dtype, const float* decay) {
+    if (B < 1 || heads < 1 || Dk < 1 || Dv < 1 || T < 1 || !valid_dtype(dtype) || !decay) return LSTM_DYN_ERR_INVALID;
+    if (Dk > MAX_D || Dv > MAX_D || (long long)B * heads >= 1 << 20 || (long long)B * T >= 1LL << 31 || T >= 1 << 30)
+        return LSTM_DYN_ERR_UNSUPPORTED;
+    for (int i = 0; i < heads; ++i)
+        if (!(decay[i] >= 0.0f && decay[i] <= 1.0f)) return LSTM_DYN_ERR_INVALID;
+    return LSTM_DYN_OK;
+}
+
+int check_buffers(int B, int heads, int Dk, int Dv, int T, int dtype, const void* z, const int32_t* lengths,
+                  const float* S0, const float* out_S, const void* out_y, const void* dy, const float* d_out_S,
+                  const void* dz, const float* dS0) {
+    const int e = dtype_bytes(dtype);
+    const long long nz = (long long)B * T * heads * (2 * Dk + Dv) * e, ny = (long long)B * T * heads * Dv * e;
+    const long long ns = 4LL * B * heads * Dk * Dv;
+    Span s[8];
+    int k = 0;
+    s[k++] = Span{z, nz, e, false};
+    s[k++] = Span{S0, ns, 4, false};
+    if (lengths) s[k++] = Span{lengths, 4LL * B, 4, false};
+    if (!dy && !dz && !dS0) {
+        s[k++] = Span{out_S, ns, 4, true, S0};
+        s[k++] = Span{out_y, ny, e, true};
+    } else {
+        s[k++] = Span{dy, ny, e, false};
+        if (d_out_S) s[k++] = Span{d_out_S, ns, 4, false};
+        s[k++] = Span{dz, nz, e, true};
+        s[k++] = Span{dS0, ns, 4, true};
+    }
+    return check_spans(s, k);
+}
+
+}  // namespace
+}  // namespace ldyn
+
+using namespace ldyn;
+
+struct lstm_dyn_attend : OpsHandle {
+    int B = 0, heads = 0, Dk = 0, Dv = 0, T = 0, dtype = 0;
+    int shares = 1, span = 0;
+    const float* powers = nullptr;
+    const double* log2a = nullptr;
+    float* share = nullptr;   // [2][B heads][shares][Dk][Dv]: going forward, going back
+    long long share_floats() const { return (long long)B * heads * shares * Dk * Dv; }
+};
+
+extern "C" int lstm_dyn_check_attend_args(int B, int heads, int Dk, int Dv, int T, int dtype, const float* decay,
+                                          const void* z, const int32_t* lengths, const float* S0, const float* out_S,
+                                          const void* out_y, const void* dy, const float* d_out_S, const void* dz,
+                                          const float* dS0) {
+    const int rc = check_sizes(B, heads, Dk, Dv, T, dtype, decay);
+    if (rc != LSTM_DYN_OK || !z) return rc;
+    return check_buffers(B, heads, Dk, Dv, T, dtype, z, lengths, S0, out_S, out_y, dy, d_out_S, dz, dS0);
+}
+
+static int attend_make(lstm_dyn_attend* h, const float* decay) {
+    // shares of four chunks and more, as many as bring WANT_GROUPS workgroups
+    const int C = h->dtype == LSTM_DYN_BF16 ? Chunk<__bf16>::C : Chunk<float>::C;
+    const int rows = h->B * h->heads, chunks = (h->T + C - 1) / C;
+    const int want = rows >= WANT_GROUPS ? 1 : (WANT_GROUPS + rows - 1) / rows;
+    int each = (chunks + want - 1) / want;
+    if (each < 4) each = 4;
+    h->shares = (chunks + each - 1) / each;
+    h->span = each * C;
+    std::vector<float> powers((size_t)h->heads * TABLE);
+    std::vector<double> logs((size_t)h->heads);
+    for (int i = 0; i < h->heads; ++i) {
+        const double a = (double)decay[i];
+        for (int n = 0; n < TABLE; ++n) powers[(size_t)i * TABLE + n] = (float)std::pow(a, n);
+        logs[(size_t)i] = a > 0.0 ? std::log2(a) : -1e9;
+    }
+    const long long np = (4LL * (long long)powers.size() + 255) / 256 * 256, nl = (8LL * h->heads + 255) / 256 * 256;
+    const long long ns = h->shares > 1 ? 8 * h->share_floats() : 0;
+    int rc = ops_device(h);
+    if (rc != LSTM_DYN_OK || (rc = ops_init(h, 256 + np + nl + ns)) != LSTM_DYN_OK) return rc;
+    h->powers = reinterpret_cast<const float*>(h->block + 256);
+    h->log2a = reinterpret_cast<const double*>(h->block + 256 + np);
+    h->share = reinterpret_cast<float*>(h->block + 256 + np + nl);
+    if (hipMemcpy(h->block + 256, powers.data(), 4 * powers.size(), hipMemcpyHostToDevice) != hipSuccess ||
+        hipMemcpy(h->block + 256 + np, logs.data(), 8 * logs.size(), hipMemcpyHostToDevice) != hipSuccess) {
+        (void)hipGetLastError();
+        (void)ops_free(h);
+        return LSTM_DYN_ERR_HIP;
+    }
+    return LSTM_DYN_OK;
+}
+
+extern "C" int lstm_dyn_attend_create(lstm_dyn_attend_t** out, int B, int heads, int Dk, int Dv, int T, int dtype,
+                                      const float* decay) {
+    if (!out) return LSTM_DYN_ERR_INVALID;
+    *out = nullptr;
+    const int ok = check_sizes(B, heads, Dk, Dv, T, dtype, decay);
+    if (ok != LSTM_DYN_OK) return ok;
+    lstm_dyn_attend* h = nullptr;
+    try {
+        h = new lstm_dyn_attend();
+        h->B = B;
+        h->heads = heads;
+        h->Dk = Dk;
+        h->Dv = Dv;
+        h->T = T;
+        h->dtype = dtype;
+        const int rc = attend_make(h, decay);
+        if (rc != LSTM_DYN_OK) {
+            delete h;
+            return rc;
+        }
+    } catch (...) {
+        delete h;
+        return LSTM_DYN_ERR_NOMEM;
+    }
+    *out = h;
+    return LSTM_DYN_OK;
+}
+
+template <class E, bool STATE>
+static int launch_pass(lstm_dyn_attend* h, const AttendParams& p) {
+    const int d = h->Dk > h->Dv ? h->Dk : h->Dv;
+    const long long items = (long long)p.rows * p.shares, grid = (items + 7) / 8 * 8 * p.passes;
+    if (d <= 32)
+        hipLaunchKernelGGL((attend_kernel<E, 32, STATE>), dim3((unsigned)grid), dim3(64 * waves_of(32)), 0, h->last_stream, p);
+    else if (d <= 64)
+        hipLaunchKernelGGL((attend_kernel<E, 64, STATE>), dim3((unsigned)grid), dim3(64 * waves_of(64)), 0, h->last_stream, p);
+    else
+        hipLaunchKernelGGL((attend_kernel<E, 128, STATE>), dim3((unsigned)grid), dim3(64 * waves_of(128)), 0, h->last_stream, p);
+    return ops_launched(h);
+}
+
+// The shares' starts for passes `state`, then passes `p`.
+static int run_passes(lstm_dyn_attend* h, const AttendParams& state, const AttendParams& p) {
+    int rc;
+    const bool bf16 = h->dtype == LSTM_DYN_BF16;
+    if (h->shares > 1) {
+        if ((rc = bf16 ? launch_pass<__bf16, true>(h, state) : launch_pass<float, true>(h, state)) != LSTM_DYN_OK) return rc;
+        hipLaunchKernelGGL(attend_join_kernel, dim3((unsigned)((h->Dk * h->Dv + 255) / 256), (unsigned)p.rows, (unsigned)state.passes),
+                           dim3(256), 0, h->last_stream, state);
+        if ((rc = ops_launched(h)) != LSTM_DYN_OK) return rc;
+    }
+    return bf16 ? launch_pass<__bf16, false>(h, p) : launch_pass<float, false>(h, p);
+}
+
+// Addresses of q, k and v (or their gradients) in z.
+struct Parts {
+    char *q, *k, *v;
+    long long ld;
+    Parts(const lstm_dyn_attend* h, const void* z) {
+        const long long e = dtype_bytes(h->dtype);
+        q = static_cast<char*>(const_cast<void*>(z));
+        k = q + e * h->heads * h->Dk;
+        v = k + e * h->heads * h->Dk;
+        ld = (long long)h->heads * (2 * h->Dk + h->Dv);
+    }
+};
+
+static AttendParams attend_params(const lstm_dyn_attend* h, const int32_t* lengths) {
+    AttendParams p{};
+    p.lengths = lengths;
+    p.status = h->status();
+    p.powers = h->powers;
+    p.log2a = h->log2a;
+    p.T = h->T;
+    p.heads = h->heads;
+    p.rows = h->B * h->heads;
+    p.shares = h->shares;
+    p.span = h->span;
+    p.Dv = h->Dv;
+    return p;
+}
+
+// Whether every head's rows of these buffers start at 16 bytes and are whole pieces of 16.
+static bool by_pieces(const lstm_dyn_attend* h, const void* a, const void* b, const void* c) {
+    const int n = 16 / dtype_bytes(h->dtype);
+    const uintptr_t low = reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b) | reinterpret_cast<uintptr_t>(c);
+    return h->Dk % n == 0 && h->Dv % n == 0 && (low & 15) == 0;
+}
+
+extern "C" int lstm_dyn_attend_forward(lstm_dyn_attend_t* h, const void* z, const int32_t* lengths, const float* S0,
+                                       float* out_S, void* out_y, void* stream) {
+    if (!h) return LSTM_DYN_ERR_INVALID;
+    int rc = check_buffers(h->B, h->heads, h->Dk, h->Dv, h->T, h->dtype, z, lengths, S0, out_S, out_y, nullptr, nullptr,
+                           nullptr, nullptr);
+    if (rc != LSTM_DYN_OK || (rc = ops_begin(h, stream)) != LSTM_DYN_OK) return rc;
+    const Parts in(h, z);
+    AttendParams p = attend_params(h, lengths);
+    p.passes = 1;
+    p.vec = by_pieces(h, z, out_y, nullptr);
+    p.pass[0] = Pass{in.q, in.k, in.v, out_y, in.ld, in.ld, in.ld, (long long)h->heads * h->Dv, h->Dk, h->Dv, 0, 0, S0,
+                     out_S, h->share};
+    return run_passes(h, p, p);
+}
+
+extern "C" int lstm_dyn_attend_backward(lstm_dyn_attend_t* h, const void* z, const int32_t* lengths, const float* S0,
+                                        const void* dy, const float* d_out_S, void* dz, float* dS0, void* stream) {
+    if (!h || !dz) return LSTM_DYN_ERR_INVALID;
+    int rc = check_buffers(h->B, h->heads, h->Dk, h->Dv, h->T, h->dtype, z, lengths, S0, nullptr, nullptr, dy, d_out_S,
+                           dz, dS0);
+    if (rc != LSTM_DYN_OK || (rc = ops_begin(h, stream)) != LSTM_DYN_OK) return rc;
+    const Parts in(h, z), out(h, dz);
+    const long long ld = in.ld, ly = (long long)h->heads * h->Dv;
+    float *fw = h->share, *bw = h->share + (h->shares > 1 ? h->share_floats() : 0);
+    AttendParams p = attend_params(h, lengths);
+    p.vec = by_pieces(h, z, dy, dz);
+    AttendParams state = p;
+    state.passes = 2;
+    state.pass[0] = Pass{nullptr, in.k, in.v, nullptr, 0, ld, ld, 0, h->Dk, h->Dv, 0, 0, S0, nullptr, fw};
+    state.pass[1] = Pass{nullptr, in.q, dy, nullptr, 0, ld, ly, 0, h->Dk, h->Dv, 1, 0, d_out_S, nullptr, bw};
+    p.passes = 3;
+    p.pass[0] = Pass{dy, in.v, in.k, out.q, ly, ld, ld, ld, h->Dv, h->Dk, 0, 1, S0, nullptr, fw};
+    p.pass[1] = Pass{in.v, dy, in.q, out.k, ld, ly, ld, ld, h->Dv, h->Dk, 1, 1, d_out_S, nullptr, bw};
+    p.pass[2] = Pass{in.k, in.q, dy, out.v, ld, ld, ly, ld, h->Dk, h->Dv, 1, 0, d_out_S, dS0, bw};
+    return run_passes(h, state, p);
+}
+
+extern "C" int lstm_dyn_attend_step(lstm_dyn_attend_t* h, int rows, const void* z, const float* S, float* out_S,
+                                    void* out_y, void* stream) {
+    if (!h || rows < 1) return LSTM_DYN_ERR_INVALID;
+    const long long n = (long long)rows * h->heads;
+    if (n >= 1LL << 24) return LSTM_DYN_ERR_UNSUPPORTED;
+    const int e = dtype_bytes(h->dtype);
+    const long long ns = 4 * n * h->Dk * h->Dv;
+    const Span s[4] = {{z, n * (2 * h->Dk + h->Dv) * e, e, false}, {S, ns, 4, false}, {out_S, ns, 4, true, S},
+                       {out_y, n * h->Dv * e, e, true}};
+    int rc = check_spans(s, 4);
+    if (rc != LSTM_DYN_OK || (rc = ops_begin(h, stream)) != LSTM_DYN_OK) return rc;
+    const StepParams a{z, S, out_S, out_y, h->powers, h->heads, h->Dk, h->Dv};
+    const bool four = h->Dv % 4 == 0 && ((reinterpret_cast<uintptr_t>(S) | reinterpret_cast<uintptr_t>(out_S)) & 15) == 0;
+    auto* k = h->dtype == LSTM_DYN_BF16 ? (four ? attend_step_kernel<__bf16, 4> : attend_step_kernel<__bf16, 1>)
+                                        : (four ? attend_step_kernel<float, 4> : attend_step_kernel<float, 1>);
+    hipLaunchKernelGGL(k, dim3((unsigned)n), dim3(256), 0, h->last_stream, a);
+    return ops_launched(h);
+}
+
+extern "C" int lstm_dyn_attend_query(lstm_dyn_attend_t* h, int what, long long* value) {
+    return ops_query(h, what, value);
+}
+
+extern "C" int lstm_dyn_attend_destroy(lstm_dyn_attend_t* h) {
+    if (!h) return LSTM_DYN_OK;
+    const int rc = ops_free(h);
+    delete h;
+    return rc;
+}

@@ -1,0 +1,457 @@
+// sample.hip -- one token a row from its logits and a given random number:
+// temperature, top-k, top-p, min-p, and the inverse of the running sum.
+//
+// A token's weight is exp((x - largest) / T) in fixed point, so sums of weights are
+// integers: the order in which they are formed changes nothing, and no sort is needed.
+// The kept tokens are a start of the tokens in order (largest first, equal ones by index),
+// that is all whose 64-bit key, the logit's bits in an order-preserving form above the
+// complement of the index, reaches a cut.  The cut for a count (top-k) or a sum of weights (top-p) is
+// found by a histogram over 2048 ranges of the exponent, which leaves one range with the cut
+// in it; its few tokens are ranked by counting.  Where they are more than LIST
+// (many equal logits), the range is cut again by key until they are not.  Then the kept weights of each
+// segment of the row are summed, and one wave walks the segment that u falls into.
+//
+// A workgroup holds a row: its two to six passes come from the L2 after the first.
+#include "ops.h"
+#include "../../include/lstm_dyn_layer.h"
+
+#include <cmath>
+
+namespace ldyn {
+namespace {
+
+typedef unsigned long long u64;
+
+constexpr int BINS = 2048, LIST = 512, SEGMENTS = 1024;
+constexpr float REACH = 48.0f;   // powers of two that the histogram spans: 2^-47 has no weight
+constexpr int ROW_THREADS = 1024, SHORT_ROW_THREADS = 256, SHORT_ROW = 4096;
+
+struct SampleParams {
+    const void* logits;
+    const float* u;
+    lstm_dyn_sample_filter_t filter;
+    int32_t* token;
+    float* logp;
+    int V, bits;       // weights are multiples of 2^-bits
+};
+
+struct RowLds {
+    u64 hist[BINS];
+    u64 key[LIST], weight[LIST];
+    u64 segment[SEGMENTS];
+    u64 part[16];
+    float fpart[16];
+    u64 found, rest, total;
+    int range, count, first;
+};
+
+// A larger logit, then a lower index, is a larger key.  x is no NaN and no -0.
+__device__ inline u64 key_of(float x, int i) {
+    const uint32_t b = __float_as_uint(x);
+    return (u64)(b & 0x80000000u ? ~b : b | 0x80000000u) << 32 | (uint32_t)~i;
+}
+
+// NaN as -inf, -0 as 0.
+__device__ inline float clean(float x) { return x == x ? x + 0.0f : -__builtin_inff(); }
+
+// exp((x - largest) / T): 1 / (T ln 2) is held in two parts, so its rounding does not
+// tilt the weights of tokens far from the largest.
+struct Weigh {
+    float largest, hi, lo, unit;
+    __device__ float power(float x) const {
+        const float d = x == largest ? 0.0f : x - largest;
+        const float t = d * hi;
+        const float e = __builtin_amdgcn_exp2f(t);
+        if (!(t > -100.0f)) return 0.0f;
+        return e + e * ((__builtin_fmaf(d, hi, -t) + d * lo) * 0.69314718f);
+    }
+    __device__ u64 weight(float p) const { return (u64)rintf(p * unit); }
+};
+
+// A row in pieces of 16 bytes, the first and the last perhaps in part.
+template <class E>
+struct Row {
+    static constexpr int N = 16 / (int)sizeof(E);
+    const E* p;
+    int V, off, pieces;
+
+    __device__ Row(const E* row, int V_) : p(row), V(V_) {
+        off = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(E));
+        pieces = (V + off + N - 1) / N;
+    }
+    __device__ typename Vec<E, N>::type piece(int k) const {
+        const int i0 = k * N - off;
+        typename Vec<E, N>::type x;
+        if (i0 >= 0 && i0 + N <= V) {
+            x = *reinterpret_cast<const typename Vec<E, N>::type*>(p + i0);
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j) x[j] = i0 + j >= 0 && i0 + j < V ? p[i0 + j] : (E)-__builtin_inff();
+        }
+        return x;
+    }
+    // f(x, index) of every element of pieces begin, begin + step, ... below end; the next two are on their way.
+    template <class F>
+    __device__ void each(int begin, int end, int step, F f) const {
+        if (begin >= end) return;
+        auto next = piece(begin), after = piece(min(begin + step, end - 1));
+#pragma unroll 1
+        for (int k = begin; k < end; k += step) {
+            const auto x = next;
+            next = after;
+            after = piece(min(k + 2 * step, end - 1));
+#pragma unroll
+            for (int j = 0; j < N; ++j) f(clean((float)x[j]), k * N - off + j);
+        }
+    }
+};
+
+__device__ inline u64 wave_sum(u64 v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+// The sum over the lanes up to this one.
+__device__ inline u64 wave_scan(u64 v) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const u64 w = __shfl_up(v, o);
+        if (lane >= o) v += w;
+    }
+    return v;
+}
+
+// The first of n sums (a power of two, at least the workgroup's threads) at which their running sum reaches `target`:
+// writes its index, what is left of the target before it and the sum of all.
+template <int THREADS, class G>
+__device__ inline void crossing(RowLds& s, int n, u64 target, G value) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, per = n / THREADS;
+    u64 mine = 0;
+    for (int i = 0; i < per; ++i) mine += value((int)threadIdx.x * per + i);
+    const u64 up = wave_scan(mine);
+    if (lane == 63) s.part[w] = up;
+    __syncthreads();
+    u64 before = up - mine, all = 0;
+    for (int i = 0; i < THREADS / 64; ++i) {
+        if (i < w) before += s.part[i];
+        all += s.part[i];
+    }
+    if (threadIdx.x == 0) s.total = all;
+    if (before < target && before + mine >= target) {
+        for (int i = 0; i < per; ++i) {
+            const u64 v = value((int)threadIdx.x * per + i);
+            if (before + v >= target) {
+                s.range = (int)threadIdx.x * per + i;
+                s.rest = target - before;
+                break;
+            }
+            before += v;
+        }
+    }
+    __syncthreads();
+}
+
+// The least key of the shortest start of the tokens in order whose measure (their number, or with
+// MASS their weight) reaches the target, among the tokens of some weight with keys of `least` or more.
+// aim(all): the target, given the sum of all measures; if it is no less than all there is, `least` is returned.
+template <int THREADS, bool MASS, class E, class A>
+__device__ inline u64 find_cut(RowLds& s, const Row<E>& row, const Weigh& weigh, u64 least, A aim) {
+    const int tid = threadIdx.x;
+    // the largest key is in range 0
+    auto range_of = [&](float x) {
+        const float d = x == weigh.largest ? 0.0f : weigh.largest - x;
+        return (int)fminf(d * weigh.hi * (BINS / REACH), (float)(BINS - 1));
+    };
+    for (int i = tid; i < BINS; i += THREADS) s.hist[i] = 0;
+    __syncthreads();
+    row.each(tid, row.pieces, THREADS, [&](float x, int i) {
+        if (key_of(x, i) < least) return;
+        const u64 w = weigh.weight(weigh.power(x));
+        if (w) atomicAdd(&s.hist[range_of(x)], MASS ? w : 1ull);
+    });
+    __syncthreads();
+    crossing<THREADS>(s, BINS, 0, [&](int i) { return s.hist[i]; });  // the sum alone
+    const u64 all = s.total, target = aim(all);
+    if (target >= all) return least;
+    crossing<THREADS>(s, BINS, target, [&](int i) { return s.hist[i]; });
+    const int range = s.range;
+    u64 rest = s.rest, lo = least, hi = ~0ull;
+    for (bool by_key = false;; by_key = true) {
+        // the tokens of the range, if they are few
+        if (tid == 0) s.count = 0;
+        __syncthreads();
+        row.each(tid, row.pieces, THREADS, [&](float x, int i) {
+            const u64 key = key_of(x, i);
+            if (key < lo || key > hi || range_of(x) != range) return;
+            const u64 w = weigh.weight(weigh.power(x));
+            if (!w) return;
+            const int at = atomicAdd(&s.count, 1);
+            if (at < LIST) {
+                s.key[at] = key;
+                s.weight[at] = MASS ? w : 1ull;
+            }
+        });
+        __syncthreads();
+        const int n = s.count;
+        if (n <= LIST) {
+            for (int e = tid; e < n; e += THREADS) {
+                const u64 key = s.key[e];
+                u64 before = 0;
+                for (int f = 0; f < n; ++f) before += s.key[f] > key ? s.weight[f] : 0ull;
+                if (before < rest && before + s.weight[e] >= rest) s.found = key;
+            }
+            __syncthreads();
+            return s.found;
+        }
+        // cut [lo, hi] again: at first by the keys that are in it
+        if (!by_key) {
+            u64 a = ~0ull, b = 0;
+            row.each(tid, row.pieces, THREADS, [&](float x, int i) {
+                const u64 key = key_of(x, i);
+                if (key < lo || range_of(x) != range || !weigh.weight(weigh.power(x))) return;
+                a = key < a ? key : a;
+                b = key > b ? key : b;
+            });
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) {
+                const u64 a2 = __shfl_xor(a, o), b2 = __shfl_xor(b, o);
+                a = a2 < a ? a2 : a;
+                b = b2 > b ? b2 : b;
+            }
+            if ((tid & 63) == 0) {
+                s.part[tid >> 6] = a;
+                s.weight[tid >> 6] = b;
+            }
+            __syncthreads();
+            for (int i = 0; i < THREADS / 64; ++i) {
+                a = s.part[i] < a ? s.part[i] : a;
+                b = s.weight[i] > b ? s.weight[i] : b;
+            }
+            lo = a;
+            hi = b;
+        }
+        int shift = 0;
+        while ((hi - lo) >> shift >= BINS) ++shift;
+        __syncthreads();
+        for (int i = tid; i < BINS; i += THREADS) s.hist[i] = 0;
+        __syncthreads();
+        row.each(tid, row.pieces, THREADS, [&](float x, int i) {
+            const u64 key = key_of(x, i);
+            if (key < lo || key > hi || range_of(x) != range) return;
+            const u64 w = weigh.weight(weigh.power(x));
+            if (w) atomicAdd(&s.hist[(hi - key) >> shift], MASS ? w : 1ull);
+        });
+        __syncthreads();
+        crossing<THREADS>(s, BINS, rest, [&](int i) { return s.hist[i]; });
+        rest = s.rest;
+        const u64 top = hi - ((u64)s.range << shift), width = (1ull << shift) - 1;
+        lo = top - lo > width ? top - width : lo;
+        hi = top;
+    }
+}
+
+template <class E, int THREADS>
+__global__ void __launch_bounds__(THREADS) sample_kernel(SampleParams a) {
+    __shared__ RowLds s;
+    const int n = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const Row<E> row(static_cast<const E*>(a.logits) + (size_t)n * a.V, a.V);
+
+    float mx = -__builtin_inff();
+    row.each(tid, row.pieces, THREADS, [&](float x, int) { mx = fmaxf(mx, x); });
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+    if (lane == 0) s.fpart[wave] = mx;
+    if (tid == 0) s.first = a.V;
+    __syncthreads();
+    for (int i = 0; i < THREADS / 64; ++i) mx = fmaxf(mx, s.fpart[i]);
+    if (mx == -__builtin_inff()) {
+        if (tid == 0) {
+            a.token[n] = -1;
+            a.logp[n] = mx;
+        }
+        return;
+    }
+
+    const lstm_dyn_sample_filter_t& f = a.filter;
+    const float T = f.temperatures ? f.temperatures[n] : f.temperature;
+    float top_p = f.top_ps ? f.top_ps[n] : f.top_p;
+    const float min_p = fminf(f.min_ps ? f.min_ps[n] : f.min_p, 1.0f);
+    int top_k = f.top_ks ? f.top_ks[n] : f.top_k;
+    if (top_k <= 0 || top_k >= a.V) top_k = 0;
+    const double per = 1.0 / (double)T * 1.4426950408889634;
+    const bool least_p = f.min_ps ? f.min_ps[n] > 0.0f : f.min_p > 0.0f;   // a NaN is no filter
+    if (!(T > 0.0f) || !((float)per < __builtin_inff()) || top_k == 1 || top_p <= 0.0f) {
+        // the first token of the order
+        int first = a.V;
+        row.each(tid, row.pieces, THREADS, [&](float x, int i) { first = x == mx && i < first ? i : first; });
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) first = min(first, __shfl_xor(first, o));
+        if (lane == 0) atomicMin(&s.first, first);
+        __syncthreads();
+        if (tid == 0) {
+            a.token[n] = s.first;
+            a.logp[n] = 0.0f;
+        }
+        return;
+    }
+
+    Weigh weigh;
+    weigh.largest = mx;
+    weigh.hi = (float)per;
+    weigh.lo = (float)(per - (double)weigh.hi);
+    weigh.unit = __uint_as_float((uint32_t)(a.bits + 127) << 23);
+    u64 cut = 0;
+    if (top_k) cut = find_cut<THREADS, false>(s, row, weigh, cut, [&](u64) { return (u64)top_k; });
+    if (top_p < 1.0f)
+        cut = find_cut<THREADS, true>(s, row, weigh, cut, [&](u64 all) {
+            const u64 t = (u64)ceil((double)top_p * (double)all);
+            return t ? t : 1ull;
+        });
+
+    // a kept token's weight, or zero
+    auto kept = [&](float x, int i) -> u64 {
+        if (key_of(x, i) < cut) return 0;
+        const float p = weigh.power(x);
+        return least_p && p < min_p ? 0 : weigh.weight(p);
+    };
+    // segments of 64 `rounds` pieces, each the work of one wave
+    const int rounds = (row.pieces + 64 * SEGMENTS - 1) / (64 * SEGMENTS);
+    for (int i = tid; i < SEGMENTS; i += THREADS) s.segment[i] = 0;
+    __syncthreads();
+    const int segments = (row.pieces + 64 * rounds - 1) / (64 * rounds);
+    for (int g = wave; g < segments; g += THREADS / 64) {
+        u64 sum = 0;
+        const int k0 = g * 64 * rounds;
+        row.each(k0 + lane, min(row.pieces, k0 + 64 * rounds), 64, [&](float x, int i) { sum += kept(x, i); });
+        sum = wave_sum(sum);
+        if (lane == 0) s.segment[g] = sum;
+    }
+    __syncthreads();
+    crossing<THREADS>(s, SEGMENTS, 0, [&](int i) { return s.segment[i]; });
+    const u64 all = s.total;
+    const float u = fminf(fmaxf(a.u[n], 0.0f), 1.0f);   // (a NaN is 0)
+    u64 target = (u64)((double)u * (double)all) + 1;    // the first running sum above u of all
+    if (target > all) target = all;
+    crossing<THREADS>(s, SEGMENTS, target, [&](int i) { return s.segment[i]; });
+    if (wave != 0) return;
+    u64 rest = s.rest;
+    const int k0 = s.range * 64 * rounds;
+    for (int r = 0; r < rounds; ++r) {
+        const int k = k0 + r * 64 + lane;
+        constexpr int M = Row<E>::N;
+        float x[M];
+        u64 w[M], sum = 0;
+        if (k < row.pieces) {
+            const auto raw = row.piece(k);
+#pragma unroll
+            for (int j = 0; j < M; ++j) x[j] = clean((float)raw[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < M; ++j) {
+            w[j] = k < row.pieces ? kept(x[j], k * M - row.off + j) : 0;
+            sum += w[j];
+        }
+        const u64 up = wave_scan(sum);
+        if (up >= rest && up - sum < rest) {
+            u64 before = up - sum;
+#pragma unroll
+            for (int j = 0; j < M; ++j) {
+                if (before < rest && before + w[j] >= rest) {
+                    const double d = x[j] == mx ? 0.0 : (double)x[j] - (double)mx;
+                    a.token[n] = k * M - row.off + j;
+                    a.logp[n] = (float)(d / (double)T - log((double)all * exp2(-(double)a.bits)));
+                }
+                before += w[j];
+            }
+        }
+        const u64 whole = __shfl(up, 63);
+        if (whole >= rest) break;
+        rest -= whole;
+    }
+}
+
+int check_sizes(int N, int V, int dtype) {
+    if (N < 1 || V < 1 || !valid_dtype(dtype)) return LSTM_DYN_ERR_INVALID;
+    return V >= 1 << 27 || N >= 1 << 22 ? LSTM_DYN_ERR_UNSUPPORTED : LSTM_DYN_OK;
+}
+
+int check_buffers(int N, int V, int dtype, const void* logits, const float* u, const lstm_dyn_sample_filter_t* f,
+                  const int32_t* token, const float* logp) {
+    Span s[8];
+    int k = 0;
+    const long long n = 4LL * N;
+    s[k++] = Span{logits, (long long)N * V * dtype_bytes(dtype), dtype_bytes(dtype), false};
+    s[k++] = Span{u, n, 4, false};
+    s[k++] = Span{token, n, 4, true};
+    s[k++] = Span{logp, n, 4, true};
+    if (f)
+        for (const void* p : {(const void*)f->temperatures, (const void*)f->top_ps, (const void*)f->min_ps,
+                              (const void*)f->top_ks})
+            if (p) s[k++] = Span{p, n, 4, false};
+    return check_spans(s, k);
+}
+
+}  // namespace
+}  // namespace ldyn
+
+using namespace ldyn;
+
+struct lstm_dyn_sample : OpsHandle {
+    int N = 0, V = 0, dtype = 0, bits = 0;
+};
+
+extern "C" int lstm_dyn_check_sample_args(int N, int V, int dtype, const void* logits, const float* u,
+                                          const lstm_dyn_sample_filter_t* filter, const int32_t* out_token,
+                                          const float* out_logp) {
+    const int rc = check_sizes(N, V, dtype);
+    return rc != LSTM_DYN_OK ? rc : check_buffers(N, V, dtype, logits, u, filter, out_token, out_logp);
+}
+
+extern "C" int lstm_dyn_sample_create(lstm_dyn_sample_t** out, int N, int V, int dtype) {
+    if (!out) return LSTM_DYN_ERR_INVALID;
+    *out = nullptr;
+    int rc = check_sizes(N, V, dtype);
+    if (rc != LSTM_DYN_OK) return rc;
+    auto* h = new (std::nothrow) lstm_dyn_sample();
+    if (!h) return LSTM_DYN_ERR_NOMEM;
+    h->N = N;
+    h->V = V;
+    h->dtype = dtype;
+    h->bits = 46;
+    while ((long long)V > 1LL << (62 - h->bits)) --h->bits;
+    if ((rc = ops_device(h)) == LSTM_DYN_OK) rc = ops_init(h, 256);
+    if (rc != LSTM_DYN_OK) {
+        delete h;
+        return rc;
+    }
+    *out = h;
+    return LSTM_DYN_OK;
+}
+
+extern "C" int lstm_dyn_sample_step(lstm_dyn_sample_t* h, const void* logits, const float* u,
+                                    const lstm_dyn_sample_filter_t* filter, int32_t* out_token, float* out_logp,
+                                    void* stream) {
+    if (!h) return LSTM_DYN_ERR_INVALID;
+    int rc = check_buffers(h->N, h->V, h->dtype, logits, u, filter, out_token, out_logp);
+    if (rc != LSTM_DYN_OK || (rc = ops_begin(h, stream)) != LSTM_DYN_OK) return rc;
+    const lstm_dyn_sample_filter_t none{1.0f, 1.0f, 0.0f, 0, nullptr, nullptr, nullptr, nullptr};
+    const SampleParams p{logits, u, filter ? *filter : none, out_token, out_logp, h->V, h->bits};
+    const bool small = h->V <= SHORT_ROW;
+    auto* k = h->dtype == LSTM_DYN_BF16
+                  ? (small ? sample_kernel<__bf16, SHORT_ROW_THREADS> : sample_kernel<__bf16, ROW_THREADS>)
+                  : (small ? sample_kernel<float, SHORT_ROW_THREADS> : sample_kernel<float, ROW_THREADS>);
+    hipLaunchKernelGGL(k, dim3((unsigned)h->N), dim3(small ? SHORT_ROW_THREADS : ROW_THREADS), 0, h->last_stream, p);
+    return ops_launched(h);
+}
+
+extern "C" int lstm_dyn_sample_query(lstm_dyn_sample_t* h, int what, long long* value) {
+    return ops_query(h, what, value);
+}
+
+extern "C" int lstm_dyn_sample_destroy(lstm_dyn_sample_t* h) {
+    if (!h) return LSTM_DYN_OK;
+    const int rc = ops_free(h);
+    delete h;
+    return rc;
+}

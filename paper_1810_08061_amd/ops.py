@@ -58,6 +58,17 @@ def _lib():
         "beam_create": [PP, I, I, I, I], "beam_step": [P, P, P, P, I, P, P, P, P, P, I, P],
         "beam_query": [P, I, PLL], "beam_destroy": [P],
         "check_beam_args": [I] * 4 + [P] * 8 + [I],
+        "norm_create": [PP, I, I, I, I, F], "norm_forward": [P] * 7,
+        "norm_backward": [P] * 5 + [I, P, P, P, P], "norm_query": [P, I, PLL], "norm_destroy": [P],
+        "check_norm_args": [I] * 4 + [F] + [P] * 6 + [I, P, P, P],
+        "clip_create": [PP, P, I], "clip_norm": [P, P, I, DB, DB, P, P], "clip_apply": [P, P, I, P, P, P],
+        "clip_query": [P, I, PLL], "clip_destroy": [P], "check_clip_args": [P, I, P, I, P, P],
+        "adamw_step_clipped": [P, P, I, DB, DB, DB, DB, P, LL, P],
+        "sample_create": [PP, I, I, I], "sample_step": [P] * 7, "sample_query": [P, I, PLL], "sample_destroy": [P],
+        "check_sample_args": [I] * 3 + [P] * 5,
+        "attend_create": [PP, I, I, I, I, I, I, P], "attend_forward": [P] * 7, "attend_backward": [P] * 9,
+        "attend_step": [P, I] + [P] * 5, "attend_query": [P, I, PLL], "attend_destroy": [P],
+        "check_attend_args": [I] * 6 + [P] * 10,
     }.items():
         f = getattr(lib, "lstm_dyn_" + name)
         f.argtypes, f.restype = args, I
@@ -476,12 +487,14 @@ class AdamW(_Handle):
                     raise ValueError(f"a state must be {a.dtype} {tuple(a.shape)}, got {b.dtype} {tuple(b.shape)}")
                 a.copy_(b)
 
-    def step(self, grads, lr: float, grad_scale: float = 1.0, stream=None):
+    def step(self, grads, lr: float, grad_scale: float = 1.0, stream=None, clip=None):
         """One step from the gradients (all float32 or all bfloat16, in the parameters' shapes), each
-        times grad_scale.  The step's number is a value of the call: a captured call repeats it."""
+        times grad_scale.  The step's number is a value of the call: a captured call repeats it.
+        clip: a ``GradClip`` over the parameters; the gradients are clipped on their way, and what
+        ``clip.norm`` gives is returned."""
         if stream is not None:
             with _on(stream):
-                return self.step(grads, lr, grad_scale)
+                return self.step(grads, lr, grad_scale, None, clip)
         torch = _torch
         grads = list(grads)
         if len(grads) != len(self.params):
@@ -491,6 +504,14 @@ class AdamW(_Handle):
             raise TypeError("gradients must be float32 or bfloat16 device tensors")
         for g, p in zip(grads, self.params):
             self._check("a gradient", g, et, p.shape)
+        if clip is not None:
+            result = clip.norm(grads, grad_scale)
+            _ok(_ready.lstm_dyn_adamw_step_clipped(self.handle, self._pointers(*[g.data_ptr() for g in grads]),
+                                                   BF16 if et == torch.bfloat16 else F32, lr, self.betas[0],
+                                                   self.betas[1], self.eps, result.data_ptr(), self.steps_done + 1,
+                                                   _stream(grads[0].device)), "lstm_dyn_adamw_step_clipped")
+            self.steps_done += 1
+            return result
         _ok(_ready.lstm_dyn_adamw_step(self.handle, self._pointers(*[g.data_ptr() for g in grads]),
                                        BF16 if et == torch.bfloat16 else F32, lr, self.betas[0], self.betas[1],
                                        self.eps, grad_scale, self.steps_done + 1, _stream(grads[0].device)),
