@@ -60,7 +60,7 @@ struct AttendParams {
     int32_t* status;
     const float* powers;    // [heads][TABLE]
     const double* log2a;    // [heads]
-    int passes, T, heads, rows, shares, span, Dv, vec;   // rows = B heads; span: steps of a share
+    int passes, T, heads, rows, shares, span, Dv, mode;   // rows = B heads; span: steps of a share
 };
 
 template <class E>
@@ -73,60 +73,121 @@ constexpr int waves_of(int DP) { return DP == 32 ? 2 : 4; }
 
 __device__ inline double power(const double* log2a, int head, int n) { return n ? exp2(log2a[head] * n) : 1.0; }
 
+// The thread's number as one that the compiler does not know: what is formed from it inside the loop
+// over chunks is not kept in registers across it.
+__device__ inline int here() {
+    int t = threadIdx.x;
+    asm volatile("" : "+v"(t));
+    return t;
+}
+
 // x as the sum of bf16 parts
 __device__ inline void parts(float x, __bf16& hi, __bf16& lo) {
     hi = (__bf16)x;
     lo = (__bf16)(x - (float)hi);
 }
 
-// N elements at row t, column c of an operand; zeros where the row or the column is not there
-template <class E, int N>
-__device__ inline typename Vec<E, N>::type fetch(const E* p, bool on, int c, int width, bool vec) {
-    typename Vec<E, N>::type v;
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = (E)0.0f;
-    if (!on) return v;
-    if (vec) {
-        if (c < width) v = *reinterpret_cast<const typename Vec<E, N>::type*>(p + c);
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (c + i < width) v[i] = p[c + i];
-    }
-    return v;
-}
+// How rows lie in memory.  PIECES: every head's row is whole pieces of 16 bytes at multiples of 16.
+// SHIFTED: it starts at any element and has at least 16 bytes; its last piece is fetched from where the row
+// ends 16 bytes later, and moved.  ELEMENTS: any row.
+enum { PIECES, SHIFTED, ELEMENTS };
 
-// A chunk's x, y and z: fetched into registers while the chunk before is worked on, then put into LDS.
-template <class E, int DP, bool STATE>
+// A chunk's x, y and z: fetched into registers while the chunk before is worked on, then put into LDS.  The
+// fetches are under no condition (rows and columns that are not there fetch others): where ways
+// meet, the compiler waits for what is on its way.
+template <class E, int DP, bool STATE, int MODE>
 struct Stage {
     static constexpr int C = Chunk<E>::C, THREADS = 64 * waves_of(DP), N = 16 / (int)sizeof(E);
     static constexpr int COLS = DP / N, ROWS = C * COLS / THREADS;  // a thread's rows, one after another
     typedef typename Vec<E, N>::type piece_t;
+    struct __attribute__((packed, aligned(sizeof(E)))) Loose { piece_t v; };
     piece_t x[ROWS], y[ROWS], z[ROWS];
+    int n;   // steps of the chunk
 
-    __device__ void get(const E* px, const E* py, const E* pz, const Pass& a, int n, bool vec) {
-        const int c = ((int)threadIdx.x % COLS) * N, r0 = ((int)threadIdx.x / COLS) * ROWS;
+    static __device__ piece_t fetch(const E* p, int c, int width) {
+        if constexpr (MODE == PIECES) {
+            return *reinterpret_cast<const piece_t*>(p + (c < width ? c : 0));
+        } else if constexpr (MODE == SHIFTED) {
+            return reinterpret_cast<const Loose*>(p + min(c, width - N))->v;
+        } else {
+            piece_t v;
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = p[min(c + i, width - 1)];
+            return v;
+        }
+    }
+    // What was fetched, with zeros where nothing is.
+    static __device__ piece_t settle(piece_t v, bool on, int c, int width) {
+        typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+        if constexpr (MODE == ELEMENTS) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = on && c + i < width ? v[i] : (E)0.0f;
+            return v;
+        }
+        u32x4_t u = __builtin_bit_cast(u32x4_t, v);
+        if constexpr (MODE == SHIFTED) {
+            const int by = (int)sizeof(E) * max(0, min(c, width) - (width - N));   // bytes, 16: none of them is there
+            const unsigned __int128 w = __builtin_bit_cast(unsigned __int128, u);
+            u = __builtin_bit_cast(u32x4_t, by < 16 ? w >> (8 * by) : (unsigned __int128)0);
+        } else {
+            on = on && c < width;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) u[i] = on ? u[i] : 0u;
+        return __builtin_bit_cast(piece_t, u);
+    }
+    __device__ void get(const E* px, const E* py, const E* pz, const Pass& a, int steps) {
+        const unsigned id = here();
+        const int c = (int)(id % COLS) * N, r0 = (int)(id / COLS) * ROWS;
+        n = steps;
+#pragma unroll
+        for (int q = 0; q < ROWS; ++q) {
+            const long long r = min(r0 + q, n - 1);
+            if constexpr (!STATE) x[q] = fetch(px + r * a.ldx, c, a.P);
+            y[q] = fetch(py + r * a.ldy, c, a.P);
+            z[q] = fetch(pz + r * a.ldz, c, a.R);
+        }
+    }
+    __device__ void settle(const Pass& a) {
+        const unsigned id = here();
+        const int c = (int)(id % COLS) * N, r0 = (int)(id / COLS) * ROWS;
 #pragma unroll
         for (int q = 0; q < ROWS; ++q) {
             const bool on = r0 + q < n;
-            if constexpr (!STATE) x[q] = fetch<E, N>(px + (r0 + q) * a.ldx, on, c, a.P, vec);
-            y[q] = fetch<E, N>(py + (r0 + q) * a.ldy, on, c, a.P, vec);
-            z[q] = fetch<E, N>(pz + (r0 + q) * a.ldz, on, c, a.R, vec);
+            if constexpr (!STATE) x[q] = settle(x[q], on, c, a.P);
+            y[q] = settle(y[q], on, c, a.P);
+            z[q] = settle(z[q], on, c, a.R);
         }
     }
 };
 
+// Four elements of a row of out, from column c.
+template <class E, bool WHOLE>
+__device__ inline void put_four(E* p, int c, int width, f32x4_t v) {
+    if constexpr (WHOLE) {
+        if (c < width) {
+            typename Vec<E, 4>::type e;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) e[i] = (E)v[i];
+            *reinterpret_cast<typename Vec<E, 4>::type*>(p + c) = e;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (c + i < width) p[c + i] = (E)v[i];
+    }
+}
+
 // --- bf16 ------------------------------------------------------------------
 
-// LDS rows of 16-byte pieces, whose places are exchanged within a row by the row's number, so
-// that a column of pieces lies in different banks.
+// LDS rows are of 16-byte pieces, whose places are exchanged within a row by the row's number, so that
+// a column of pieces lies in different banks: piece k of a row lies at k ^ swap(row), where the swap
+// (0 to 7) of rows by steps is row & 7, of rows by columns (y and z transposed) (row ^ row / 8) & 7.
+// What a lane's numbers give (row, swap and piece together) is formed once and the rest are
+// constants, so that few addresses are kept.
 template <int PIECES>
-__device__ inline int swap_of(int row) {
-    return (row ^ (row >> 3)) & (PIECES < 8 ? PIECES - 1 : 7);
-}
-template <int PIECES>
-__device__ inline __bf16* at(__bf16* base, int row, int piece) {
-    return base + (row * PIECES + (piece ^ swap_of<PIECES>(row))) * 8;
+__device__ inline __bf16* at(__bf16* base, int row, int piece, int lane_swap) {
+    return base + row * PIECES * 8 + (piece & ~7) * 8 + ((piece & 7) ^ lane_swap) * 8;
 }
 
 template <int DP, bool STATE>
@@ -139,19 +200,23 @@ struct LdsBf16 {
     float powers[TABLE + 3];
 };
 
-template <int DP, bool STATE>
-__device__ inline void put_chunk(LdsBf16<DP, STATE>& s, const Stage<__bf16, DP, STATE>& g) {
-    typedef Stage<__bf16, DP, STATE> G;
+template <int DP, bool STATE, int MODE>
+__device__ inline void put_chunk(LdsBf16<DP, STATE>& s, const Stage<__bf16, DP, STATE, MODE>& g) {
+    typedef Stage<__bf16, DP, STATE, MODE> G;
     constexpr int ROWS = G::ROWS, COLS = G::COLS;
-    const int o = (int)threadIdx.x % COLS, r0 = ((int)threadIdx.x / COLS) * ROWS;
+    const unsigned id = here();
+    const int o = (int)(id % COLS), r0 = (int)(id / COLS) * ROWS;
     if constexpr (!STATE) {
+        constexpr int MASK = (COLS < 8 ? COLS : 8) - 1;
+        const int swap = (o & 7) ^ (r0 & MASK), o8 = (o & ~7) * 8;
 #pragma unroll
         for (int q = 0; q < ROWS; ++q) {
-            *reinterpret_cast<bf16x8_t*>(at<COLS>(s.x, r0 + q, o)) = g.x[q];
-            *reinterpret_cast<bf16x8_t*>(at<COLS>(s.y, r0 + q, o)) = g.y[q];
+            *reinterpret_cast<bf16x8_t*>(at<COLS>(s.x + o8, r0 + q, q, swap)) = g.x[q];
+            *reinterpret_cast<bf16x8_t*>(at<COLS>(s.y + o8, r0 + q, q, swap)) = g.y[q];
         }
     }
     typedef typename Vec<__bf16, ROWS>::type run_t;
+    const int swap = (r0 / 8) ^ (o & 7);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         run_t y, z;
@@ -160,8 +225,8 @@ __device__ inline void put_chunk(LdsBf16<DP, STATE>& s, const Stage<__bf16, DP, 
             y[q] = g.y[q][e];
             z[q] = g.z[q][e];
         }
-        *reinterpret_cast<run_t*>(at<8>(s.yt, 8 * o + e, r0 / 8) + r0 % 8) = y;
-        *reinterpret_cast<run_t*>(at<8>(s.zt, 8 * o + e, r0 / 8) + r0 % 8) = z;
+        *reinterpret_cast<run_t*>(at<8>(s.yt + r0 % 8, 8 * o + e, e, swap)) = y;
+        *reinterpret_cast<run_t*>(at<8>(s.zt + r0 % 8, 8 * o + e, e, swap)) = z;
     }
 }
 
@@ -171,12 +236,15 @@ __device__ inline f32x4_t mfma(bf16x8_t a, bf16x8_t b, f32x4_t c) {
 __device__ inline bf16x8_t join(bf16x4_t a, bf16x4_t b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 
 // One chunk: n steps, out at its first step.
-template <int DP, bool STATE>
+template <int DP, bool STATE, bool WHOLE>
 __device__ inline void work(LdsBf16<DP, STATE>& s, const Pass& a, f32x4_t (&M)[DP / 16][DP / 16 / waves_of(DP)], int n,
                             __bf16* out) {
     constexpr int W = waves_of(DP), RT = DP / 16 / W, PT = DP / 16, KB = DP / 32, IT = 4 / W, COLS = DP / 8;
-    const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4;
+    const int lane = here() & 63, l = lane & 15, g = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    constexpr int MASK = (COLS < 8 ? COLS : 8) - 1;
+    const int by_step = g ^ (l & MASK), by_half = (g >> 1) ^ (l & MASK), by_column = g ^ ((l ^ (l >> 3)) & 7);
+    const int in_a = g ^ (l & 7), half_in_a = (g >> 1) ^ (l & 7);
     if constexpr (!STATE) {
         // the products under the mask: this wave's steps i against all j, one column i a lane
         f32x4_t A[IT][4];
@@ -187,11 +255,11 @@ __device__ inline void work(LdsBf16<DP, STATE>& s, const Pass& a, f32x4_t (&M)[D
             for (int jt = 0; jt < 4; ++jt) A[q][jt] = f32x4_t{0, 0, 0, 0};
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
-                const bf16x8_t b = *reinterpret_cast<const bf16x8_t*>(at<COLS>(s.x, 16 * it + l, 4 * kb + g));
+                const bf16x8_t b = *reinterpret_cast<const bf16x8_t*>(at<COLS>(s.x, 16 * it + l, 4 * kb, by_step));
 #pragma unroll
                 for (int jt = 0; jt < 4; ++jt)
                     if (a.back ? jt >= it : jt <= it)
-                        A[q][jt] = mfma(*reinterpret_cast<const bf16x8_t*>(at<COLS>(s.y, 16 * jt + l, 4 * kb + g)), b, A[q][jt]);
+                        A[q][jt] = mfma(*reinterpret_cast<const bf16x8_t*>(at<COLS>(s.y, 16 * jt + l, 4 * kb, by_step)), b, A[q][jt]);
             }
 #pragma unroll
             for (int jt = 0; jt < 4; ++jt)
@@ -215,8 +283,8 @@ __device__ inline void work(LdsBf16<DP, STATE>& s, const Pass& a, f32x4_t (&M)[D
                     lo[r] = o;
                 }
                 const int i = 16 * (w * IT + q) + l;
-                *reinterpret_cast<bf16x4_t*>(at<8>(s.y, i, 2 * jt + g / 2) + 4 * (g & 1)) = hi;
-                *reinterpret_cast<bf16x4_t*>(at<8>(s.y + 64 * 64, i, 2 * jt + g / 2) + 4 * (g & 1)) = lo;
+                *reinterpret_cast<bf16x4_t*>(at<8>(s.y + 4 * (g & 1), i, 2 * jt, half_in_a)) = hi;
+                *reinterpret_cast<bf16x4_t*>(at<8>(s.y + 64 * 64 + 4 * (g & 1), i, 2 * jt, half_in_a)) = lo;
             }
         __syncthreads();
     }
@@ -225,7 +293,7 @@ __device__ inline void work(LdsBf16<DP, STATE>& s, const Pass& a, f32x4_t (&M)[D
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
-            z[kb][rt] = *reinterpret_cast<const bf16x8_t*>(at<8>(s.zt, 16 * (w * RT + rt) + l, 4 * kb + g));
+            z[kb][rt] = *reinterpret_cast<const bf16x8_t*>(at<8>(s.zt, 16 * (w * RT + rt) + l, 4 * kb ^ 2 * rt, by_column ^ (2 * RT * w & 7)));
     if constexpr (!STATE) {
         f32x4_t O[4][RT];
 #pragma unroll
@@ -247,38 +315,30 @@ __device__ inline void work(LdsBf16<DP, STATE>& s, const Pass& a, f32x4_t (&M)[D
 #pragma unroll
             for (int it = 0; it < 4; ++it) {
                 // rows of M in the order in which a lane holds them
-                const bf16x8_t x = join(*reinterpret_cast<const bf16x4_t*>(at<COLS>(s.x, 16 * it + l, 4 * kb + g / 2) + 4 * (g & 1)),
-                                        *reinterpret_cast<const bf16x4_t*>(at<COLS>(s.x, 16 * it + l, 4 * kb + 2 + g / 2) + 4 * (g & 1)));
+                const bf16x8_t x = join(*reinterpret_cast<const bf16x4_t*>(at<COLS>(s.x + 4 * (g & 1), 16 * it + l, 4 * kb, by_half)),
+                                        *reinterpret_cast<const bf16x4_t*>(at<COLS>(s.x + 4 * (g & 1), 16 * it + l, 4 * kb + 2, by_half)));
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) O[it][rt] = mfma(x, lo[rt], mfma(x, hi[rt], O[it][rt]));
+                for (int rt = 0; rt < RT; ++rt) O[it][rt] = mfma(lo[rt], x, mfma(hi[rt], x, O[it][rt]));
             }
         }
 #pragma unroll
         for (int it = 0; it < 4; ++it) {
+            const int i = 16 * it + l, e = a.back ? n - 1 - i : i + 1;
+            const float f = s.powers[e < 0 ? 0 : e];   // a row that is not there is all zeros
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = 16 * it + 4 * g + r, e = a.back ? n - 1 - i : i + 1;
-                const float f = s.powers[e < 0 ? 0 : e];   // a row that is not there is all zeros
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) O[it][rt][r] *= f;
-            }
+            for (int rt = 0; rt < RT; ++rt) O[it][rt] *= f;
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
                 if (a.back ? kb == 1 || it <= 1 : kb == 0 || it >= 2) {
-                    const bf16x8_t hi = *reinterpret_cast<const bf16x8_t*>(at<8>(s.y, 16 * it + l, 4 * kb + g));
-                    const bf16x8_t lo = *reinterpret_cast<const bf16x8_t*>(at<8>(s.y + 64 * 64, 16 * it + l, 4 * kb + g));
+                    const bf16x8_t hi = *reinterpret_cast<const bf16x8_t*>(at<8>(s.y, i, 4 * kb, in_a));
+                    const bf16x8_t lo = *reinterpret_cast<const bf16x8_t*>(at<8>(s.y + 64 * 64, i, 4 * kb, in_a));
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) O[it][rt] = mfma(lo, z[kb][rt], mfma(hi, z[kb][rt], O[it][rt]));
+                    for (int rt = 0; rt < RT; ++rt) O[it][rt] = mfma(z[kb][rt], lo, mfma(z[kb][rt], hi, O[it][rt]));
                 }
+            if (i < n)
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                const int c = 16 * (w * RT + rt) + l;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int i = 16 * it + 4 * g + r;
-                    if (i < n && c < a.R) out[i * a.ldo + c] = (__bf16)O[it][rt][r];
-                }
-            }
+                for (int rt = 0; rt < RT; ++rt)
+                    put_four<__bf16, WHOLE>(out + i * a.ldo, 16 * (w * RT + rt) + 4 * g, a.R, O[it][rt]);
         }
     }
     // the state
@@ -308,7 +368,7 @@ __device__ inline void work(LdsBf16<DP, STATE>& s, const Pass& a, f32x4_t (&M)[D
         }
 #pragma unroll
         for (int pt = 0; pt < PT; ++pt) {
-            const bf16x8_t y = *reinterpret_cast<const bf16x8_t*>(at<8>(s.yt, 16 * pt + l, 4 * kb + g));
+            const bf16x8_t y = *reinterpret_cast<const bf16x8_t*>(at<8>(s.yt, 16 * pt + l, 4 * kb ^ (2 * pt & 7), by_column));
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) M[pt][rt] = mfma(y, z1[rt], mfma(y, z2[rt], mfma(y, z3[rt], M[pt][rt])));
         }
@@ -327,9 +387,9 @@ struct LdsF32 {
     float powers[TABLE + 3];
 };
 
-template <int DP, bool STATE>
-__device__ inline void put_chunk(LdsF32<DP, STATE>& s, const Stage<float, DP, STATE>& g) {
-    typedef Stage<float, DP, STATE> G;
+template <int DP, bool STATE, int MODE>
+__device__ inline void put_chunk(LdsF32<DP, STATE>& s, const Stage<float, DP, STATE, MODE>& g) {
+    typedef Stage<float, DP, STATE, MODE> G;
     constexpr int LD = LdsF32<DP, STATE>::LD;
     const int c = ((int)threadIdx.x % G::COLS) * 4, r0 = ((int)threadIdx.x / G::COLS) * G::ROWS;
 #pragma unroll
@@ -342,11 +402,11 @@ __device__ inline void put_chunk(LdsF32<DP, STATE>& s, const Stage<float, DP, ST
 
 __device__ inline f32x4_t mfma(float a, float b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
-template <int DP, bool STATE>
+template <int DP, bool STATE, bool WHOLE>
 __device__ inline void work(LdsF32<DP, STATE>& s, const Pass& a, f32x4_t (&M)[DP / 16][DP / 16 / waves_of(DP)], int n,
                             float* out) {
     constexpr int W = waves_of(DP), RT = DP / 16 / W, PT = DP / 16, LD = LdsF32<DP, STATE>::LD;
-    const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4;
+    const int lane = here() & 63, l = lane & 15, g = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     if constexpr (!STATE) {
 #pragma unroll
@@ -390,33 +450,25 @@ __device__ inline void work(LdsF32<DP, STATE>& s, const Pass& a, f32x4_t (&M)[DP
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) O[rt] = mfma(x[r], M[pt][rt][r], O[rt]);
+                    for (int rt = 0; rt < RT; ++rt) O[rt] = mfma(M[pt][rt][r], x[r], O[rt]);
             }
+            const int i = 16 * it + l, e = a.back ? n - 1 - i : i + 1;
+            const float f = s.powers[e < 0 ? 0 : e];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = 16 * it + 4 * g + r, e = a.back ? n - 1 - i : i + 1;
-                const float f = s.powers[e < 0 ? 0 : e];
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) O[rt][r] *= f;
-            }
+            for (int rt = 0; rt < RT; ++rt) O[rt] *= f;
 #pragma unroll
             for (int jt = 0; jt < 2; ++jt)
                 if (a.back ? jt >= it : jt <= it) {
-                    const f32x4_t A = *reinterpret_cast<const f32x4_t*>(s.a + (16 * it + l) * 36 + 16 * jt + 4 * g);
+                    const f32x4_t A = *reinterpret_cast<const f32x4_t*>(s.a + i * 36 + 16 * jt + 4 * g);
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
 #pragma unroll
-                        for (int rt = 0; rt < RT; ++rt) O[rt] = mfma(A[r], z[jt][rt][r], O[rt]);
+                        for (int rt = 0; rt < RT; ++rt) O[rt] = mfma(z[jt][rt][r], A[r], O[rt]);
                 }
+            if (i < n)
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                const int c = 16 * (w * RT + rt) + l;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int i = 16 * it + 4 * g + r;
-                    if (i < n && c < a.R) out[i * a.ldo + c] = O[rt][r];
-                }
-            }
+                for (int rt = 0; rt < RT; ++rt)
+                    put_four<float, WHOLE>(out + i * a.ldo, 16 * (w * RT + rt) + 4 * g, a.R, O[rt]);
         }
     }
     const float keep = s.powers[n];
@@ -449,7 +501,7 @@ struct LdsOf<float, DP, STATE> { typedef LdsF32<DP, STATE> type; };
 // --- the passes ----------------------------------------------------------------
 
 // STATE: what each share adds to the state, alone.
-template <class E, int DP, bool STATE>
+template <class E, int DP, bool STATE, int MODE>
 __global__ void __launch_bounds__(64 * waves_of(DP), 2) attend_kernel(AttendParams p) {
     constexpr int C = Chunk<E>::C, W = waves_of(DP), RT = DP / 16 / W, PT = DP / 16;
     __shared__ typename LdsOf<E, DP, STATE>::type s;
@@ -488,20 +540,20 @@ __global__ void __launch_bounds__(64 * waves_of(DP), 2) attend_kernel(AttendPara
             }
 
     const int chunks = (len + C - 1) / C;
-    Stage<E, DP, STATE> stage;
+    Stage<E, DP, STATE, MODE> stage;
     auto chunk_of = [&](int c) { return a.back ? chunks - 1 - c : c; };
     auto fetch_chunk = [&](int c) {
         const int k = chunk_of(c) * C;
-        stage.get(px + (long long)k * a.ldx, py + (long long)k * a.ldy, pz + (long long)k * a.ldz, a, min(C, len - k),
-                  p.vec != 0);
+        stage.get(px + k * a.ldx, py + k * a.ldy, pz + k * a.ldz, a, min(C, len - k));
     };
     if (chunks) fetch_chunk(0);
     for (int c = 0; c < chunks; ++c) {
         const int k = chunk_of(c) * C;
+        stage.settle(a);
         put_chunk(s, stage);
         __syncthreads();
         if (c + 1 < chunks) fetch_chunk(c + 1);
-        work(s, a, M, min(C, len - k), out + (long long)k * a.ldo);
+        work<DP, STATE, MODE == PIECES>(s, a, M, min(C, len - k), out + k * a.ldo);
         __syncthreads();
     }
 
@@ -717,17 +769,23 @@ extern "C" int lstm_dyn_attend_create(lstm_dyn_attend_t** out, int B, int heads,
     return LSTM_DYN_OK;
 }
 
-template <class E, bool STATE>
-static int launch_pass(lstm_dyn_attend* h, const AttendParams& p) {
+template <class E, bool STATE, int MODE>
+static int launch_mode(lstm_dyn_attend* h, const AttendParams& p) {
     const int d = h->Dk > h->Dv ? h->Dk : h->Dv;
     const long long items = (long long)p.rows * p.shares, grid = (items + 7) / 8 * 8 * p.passes;
     if (d <= 32)
-        hipLaunchKernelGGL((attend_kernel<E, 32, STATE>), dim3((unsigned)grid), dim3(64 * waves_of(32)), 0, h->last_stream, p);
+        hipLaunchKernelGGL((attend_kernel<E, 32, STATE, MODE>), dim3((unsigned)grid), dim3(64 * waves_of(32)), 0, h->last_stream, p);
     else if (d <= 64)
-        hipLaunchKernelGGL((attend_kernel<E, 64, STATE>), dim3((unsigned)grid), dim3(64 * waves_of(64)), 0, h->last_stream, p);
+        hipLaunchKernelGGL((attend_kernel<E, 64, STATE, MODE>), dim3((unsigned)grid), dim3(64 * waves_of(64)), 0, h->last_stream, p);
     else
-        hipLaunchKernelGGL((attend_kernel<E, 128, STATE>), dim3((unsigned)grid), dim3(64 * waves_of(128)), 0, h->last_stream, p);
+        hipLaunchKernelGGL((attend_kernel<E, 128, STATE, MODE>), dim3((unsigned)grid), dim3(64 * waves_of(128)), 0, h->last_stream, p);
     return ops_launched(h);
+}
+template <class E, bool STATE>
+static int launch_pass(lstm_dyn_attend* h, const AttendParams& p) {
+    return p.mode == PIECES    ? launch_mode<E, STATE, PIECES>(h, p)
+           : p.mode == SHIFTED ? launch_mode<E, STATE, SHIFTED>(h, p)
+                               : launch_mode<E, STATE, ELEMENTS>(h, p);
 }
 
 // The shares' starts for passes `state`, then passes `p`.
@@ -771,11 +829,12 @@ static AttendParams attend_params(const lstm_dyn_attend* h, const int32_t* lengt
     return p;
 }
 
-// Whether every head's rows of these buffers start at 16 bytes and are whole pieces of 16.
-static bool by_pieces(const lstm_dyn_attend* h, const void* a, const void* b, const void* c) {
+// How every head's rows of these buffers lie.
+static int mode_of(const lstm_dyn_attend* h, const void* a, const void* b, const void* c) {
     const int n = 16 / dtype_bytes(h->dtype);
     const uintptr_t low = reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b) | reinterpret_cast<uintptr_t>(c);
-    return h->Dk % n == 0 && h->Dv % n == 0 && (low & 15) == 0;
+    if (h->Dk % n == 0 && h->Dv % n == 0 && (low & 15) == 0) return PIECES;
+    return h->Dk >= n && h->Dv >= n ? SHIFTED : ELEMENTS;
 }
 
 extern "C" int lstm_dyn_attend_forward(lstm_dyn_attend_t* h, const void* z, const int32_t* lengths, const float* S0,
@@ -787,7 +846,7 @@ extern "C" int lstm_dyn_attend_forward(lstm_dyn_attend_t* h, const void* z, cons
     const Parts in(h, z);
     AttendParams p = attend_params(h, lengths);
     p.passes = 1;
-    p.vec = by_pieces(h, z, out_y, nullptr);
+    p.mode = mode_of(h, z, out_y, nullptr);
     p.pass[0] = Pass{in.q, in.k, in.v, out_y, in.ld, in.ld, in.ld, (long long)h->heads * h->Dv, h->Dk, h->Dv, 0, 0, S0,
                      out_S, h->share};
     return run_passes(h, p, p);
@@ -803,7 +862,7 @@ extern "C" int lstm_dyn_attend_backward(lstm_dyn_attend_t* h, const void* z, con
     const long long ld = in.ld, ly = (long long)h->heads * h->Dv;
     float *fw = h->share, *bw = h->share + (h->shares > 1 ? h->share_floats() : 0);
     AttendParams p = attend_params(h, lengths);
-    p.vec = by_pieces(h, z, dy, dz);
+    p.mode = mode_of(h, z, dy, dz);
     AttendParams state = p;
     state.passes = 2;
     state.pass[0] = Pass{nullptr, in.k, in.v, nullptr, 0, ld, ld, 0, h->Dk, h->Dv, 0, 0, S0, nullptr, fw};
