@@ -169,7 +169,7 @@ int lstm_dyn_check_sample_args(int N, int V, int dtype, const void* logits, cons
 typedef struct lstm_dyn_attend lstm_dyn_attend_t;
 
 /* decay: [heads] host memory (copied), each in [0, 1].  B, heads, T_max >= 1, 1 <= Dk, Dv <= 128,
- * B * heads < 2^20, B * T_max < 2^31, T_max < 2^30. */
+ * heads <= 16384, B * heads < 2^20, B * T_max < 2^31, T_max < 2^30. */
 int lstm_dyn_attend_create(lstm_dyn_attend_t** out, int B, int heads, int Dk, int Dv, int T_max,
                            int dtype, const float* decay);
 int lstm_dyn_attend_forward(lstm_dyn_attend_t* h, const void* z, const int32_t* lengths,

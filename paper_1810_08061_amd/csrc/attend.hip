@@ -36,6 +36,7 @@ namespace ldyn {
 namespace {
 
 constexpr int MAX_D = 128;
+constexpr int MAX_HEADS = 16384; // a chunk of 64 rows of heads 3 x 128 elements stays below NOWHERE
 constexpr int TABLE = 65;        // powers of a head's decay
 constexpr int WANT_GROUPS = 512; // workgroups that a pass should have
 
@@ -56,11 +57,11 @@ struct Pass {
 
 struct AttendParams {
     Pass pass[3];
-    const int32_t* lengths;
+    const int32_t* lengths; // [B], or one for all rows
     int32_t* status;
     const float* powers;    // [heads][TABLE]
     const double* log2a;    // [heads]
-    int passes, T, heads, rows, shares, span, Dv, mode;   // rows = B heads; span: steps of a share
+    int passes, T, heads, rows, shares, span, Dv, mode, length_step;   // rows = B heads; span: steps of a share
 };
 
 template <class E>
@@ -81,11 +82,17 @@ __device__ inline int here() {
     return t;
 }
 
-// x as the sum of bf16 parts
-__device__ inline void parts(float x, __bf16& hi, __bf16& lo) {
-    hi = (__bf16)x;
-    lo = (__bf16)(x - (float)hi);
+// Pairs of numbers as sums of bf16 parts, each pair of parts in one register.
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+__device__ inline uint32_t pack(f32x2_t x) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2_t)); }
+__device__ inline f32x2_t unpack(uint32_t x) { return f32x2_t{__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)}; }
+__device__ inline void parts(f32x2_t x, uint32_t& hi, uint32_t& lo) {
+    hi = pack(x);
+    lo = pack(x - unpack(hi));
 }
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
 // How rows lie in memory.  PIECES: every head's row is whole pieces of 16 bytes at multiples of 16.
 // SHIFTED: it starts at any element and has at least 16 bytes; its last piece is fetched from where the row
@@ -93,8 +100,11 @@ __device__ inline void parts(float x, __bf16& hi, __bf16& lo) {
 enum { PIECES, SHIFTED, ELEMENTS };
 
 // A chunk's x, y and z: fetched into registers while the chunk before is worked on, then put into LDS.  The
-// fetches are under no condition (rows and columns that are not there fetch others): where ways
-// meet, the compiler waits for what is on its way.
+// fetches are under no condition: where ways meet, the compiler waits for what is on its way.
+// PIECES go through a descriptor of the chunk's rows, which gives zeros past them and in
+// columns that are not there (set beyond it); the others fetch rows and columns that
+// are there in place of ones that are not.
+constexpr uint32_t NOWHERE = 1u << 30;   // a chunk's rows have fewer bytes
 template <class E, int DP, bool STATE, int MODE>
 struct Stage {
     static constexpr int C = Chunk<E>::C, THREADS = 64 * waves_of(DP), N = 16 / (int)sizeof(E);
@@ -104,60 +114,57 @@ struct Stage {
     piece_t x[ROWS], y[ROWS], z[ROWS];
     int n;   // steps of the chunk
 
-    static __device__ piece_t fetch(const E* p, int c, int width) {
+    __device__ void fetch(piece_t (&v)[ROWS], const E* p, long long ld, int r0, int c, int width) const {
         if constexpr (MODE == PIECES) {
-            return *reinterpret_cast<const piece_t*>(p + (c < width ? c : 0));
-        } else if constexpr (MODE == SHIFTED) {
-            return reinterpret_cast<const Loose*>(p + min(c, width - N))->v;
-        } else {
-            piece_t v;
+            const uint32_t row = (uint32_t)ld * (uint32_t)sizeof(E);
+            const auto rows = __builtin_amdgcn_make_buffer_rsrc(const_cast<E*>(p), 0, (int)(n * row), 0x00027000);
+            const uint32_t at = c < width ? (uint32_t)r0 * row + (uint32_t)c * (uint32_t)sizeof(E) : NOWHERE;
 #pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = p[min(c + i, width - 1)];
-            return v;
+            for (int q = 0; q < ROWS; ++q)
+                v[q] = __builtin_bit_cast(piece_t, __builtin_amdgcn_raw_buffer_load_b128(rows, at + q * row, 0, 0));
+            return;
+        }
+#pragma unroll
+        for (int q = 0; q < ROWS; ++q) {
+            const E* r = p + min(r0 + q, n - 1) * ld;
+            if constexpr (MODE == SHIFTED) {
+                v[q] = reinterpret_cast<const Loose*>(r + min(c, width - N))->v;
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i) v[q][i] = r[min(c + i, width - 1)];
+            }
         }
     }
-    // What was fetched, with zeros where nothing is.
-    static __device__ piece_t settle(piece_t v, bool on, int c, int width) {
-        typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
-        if constexpr (MODE == ELEMENTS) {
+    // Zeros where nothing is.
+    __device__ void settle(piece_t (&v)[ROWS], int r0, int c, int width) const {
+        const int by = (int)sizeof(E) * max(0, min(c, width) - (width - N));   // bytes; 16: none of them is there
 #pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = on && c + i < width ? v[i] : (E)0.0f;
-            return v;
-        }
-        u32x4_t u = __builtin_bit_cast(u32x4_t, v);
-        if constexpr (MODE == SHIFTED) {
-            const int by = (int)sizeof(E) * max(0, min(c, width) - (width - N));   // bytes, 16: none of them is there
-            const unsigned __int128 w = __builtin_bit_cast(unsigned __int128, u);
-            u = __builtin_bit_cast(u32x4_t, by < 16 ? w >> (8 * by) : (unsigned __int128)0);
-        } else {
-            on = on && c < width;
-        }
+        for (int q = 0; q < ROWS; ++q) {
+            const bool on = r0 + q < n;
+            if constexpr (MODE == ELEMENTS) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) u[i] = on ? u[i] : 0u;
-        return __builtin_bit_cast(piece_t, u);
+                for (int i = 0; i < N; ++i) v[q][i] = on && c + i < width ? v[q][i] : (E)0.0f;
+            } else {
+                const unsigned __int128 w = __builtin_bit_cast(unsigned __int128, v[q]);
+                v[q] = __builtin_bit_cast(piece_t, on && by < 16 ? w >> (8 * by) : (unsigned __int128)0);
+            }
+        }
     }
     __device__ void get(const E* px, const E* py, const E* pz, const Pass& a, int steps) {
         const unsigned id = here();
         const int c = (int)(id % COLS) * N, r0 = (int)(id / COLS) * ROWS;
         n = steps;
-#pragma unroll
-        for (int q = 0; q < ROWS; ++q) {
-            const long long r = min(r0 + q, n - 1);
-            if constexpr (!STATE) x[q] = fetch(px + r * a.ldx, c, a.P);
-            y[q] = fetch(py + r * a.ldy, c, a.P);
-            z[q] = fetch(pz + r * a.ldz, c, a.R);
-        }
+        if constexpr (!STATE) fetch(x, px, a.ldx, r0, c, a.P);
+        fetch(y, py, a.ldy, r0, c, a.P);
+        fetch(z, pz, a.ldz, r0, c, a.R);
     }
     __device__ void settle(const Pass& a) {
+        if constexpr (MODE == PIECES) return;
         const unsigned id = here();
         const int c = (int)(id % COLS) * N, r0 = (int)(id / COLS) * ROWS;
-#pragma unroll
-        for (int q = 0; q < ROWS; ++q) {
-            const bool on = r0 + q < n;
-            if constexpr (!STATE) x[q] = settle(x[q], on, c, a.P);
-            y[q] = settle(y[q], on, c, a.P);
-            z[q] = settle(z[q], on, c, a.R);
-        }
+        if constexpr (!STATE) settle(x, r0, c, a.P);
+        settle(y, r0, c, a.P);
+        settle(z, r0, c, a.R);
     }
 };
 
@@ -166,10 +173,8 @@ template <class E, bool WHOLE>
 __device__ inline void put_four(E* p, int c, int width, f32x4_t v) {
     if constexpr (WHOLE) {
         if (c < width) {
-            typename Vec<E, 4>::type e;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) e[i] = (E)v[i];
-            *reinterpret_cast<typename Vec<E, 4>::type*>(p + c) = e;
+            typedef typename Vec<E, 4>::type four_t;
+            *reinterpret_cast<four_t*>(p + c) = __builtin_convertvector(v, four_t);
         }
     } else {
 #pragma unroll
@@ -274,17 +279,17 @@ __device__ inline void work(LdsBf16<DP, STATE>& s, const Pass& a, f32x4_t (&M)[D
         for (int q = 0; q < IT; ++q)
 #pragma unroll
             for (int jt = 0; jt < 4; ++jt) {
-                bf16x4_t hi, lo;
+                u32x2_t hi, lo;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    __bf16 h, o;
-                    parts(A[q][jt][r], h, o);
+                for (int r = 0; r < 2; ++r) {
+                    uint32_t h, o;
+                    parts(f32x2_t{A[q][jt][2 * r], A[q][jt][2 * r + 1]}, h, o);
                     hi[r] = h;
                     lo[r] = o;
                 }
                 const int i = 16 * (w * IT + q) + l;
-                *reinterpret_cast<bf16x4_t*>(at<8>(s.y + 4 * (g & 1), i, 2 * jt, half_in_a)) = hi;
-                *reinterpret_cast<bf16x4_t*>(at<8>(s.y + 64 * 64 + 4 * (g & 1), i, 2 * jt, half_in_a)) = lo;
+                *reinterpret_cast<u32x2_t*>(at<8>(s.y + 4 * (g & 1), i, 2 * jt, half_in_a)) = hi;
+                *reinterpret_cast<u32x2_t*>(at<8>(s.y + 64 * 64 + 4 * (g & 1), i, 2 * jt, half_in_a)) = lo;
             }
         __syncthreads();
     }
@@ -304,14 +309,18 @@ __device__ inline void work(LdsBf16<DP, STATE>& s, const Pass& a, f32x4_t (&M)[D
         for (int kb = 0; kb < KB; ++kb) {
             bf16x8_t hi[RT], lo[RT];
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
+            for (int rt = 0; rt < RT; ++rt) {
+                u32x4_t h4, l4;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    __bf16 h, o;
-                    parts(M[2 * kb + e / 4][rt][e % 4], h, o);
-                    hi[rt][e] = h;
-                    lo[rt][e] = o;
+                for (int e = 0; e < 4; ++e) {
+                    uint32_t h, o;
+                    parts(f32x2_t{M[2 * kb + e / 2][rt][2 * e % 4], M[2 * kb + e / 2][rt][2 * e % 4 + 1]}, h, o);
+                    h4[e] = h;
+                    l4[e] = o;
                 }
+                hi[rt] = __builtin_bit_cast(bf16x8_t, h4);
+                lo[rt] = __builtin_bit_cast(bf16x8_t, l4);
+            }
 #pragma unroll
             for (int it = 0; it < 4; ++it) {
                 // rows of M in the order in which a lane holds them
@@ -350,21 +359,29 @@ __device__ inline void work(LdsBf16<DP, STATE>& s, const Pass& a, f32x4_t (&M)[D
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
         bf16x8_t z1[RT], z2[RT], z3[RT];
+        float f[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int j = 32 * kb + 8 * g + e, d = a.back ? j + 1 : n - 1 - j;
-            const float f = s.powers[d < 0 ? 0 : d];
+            f[e] = s.powers[d < 0 ? 0 : d];
+        }
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                const float v = (float)z[kb][rt][e] * f;
-                const __bf16 hi = (__bf16)v;
-                const float left = v - (float)hi;
-                __bf16 mid, lo;
-                parts(left, mid, lo);
-                z1[rt][e] = hi;
-                z2[rt][e] = mid;
-                z3[rt][e] = lo;
+        for (int rt = 0; rt < RT; ++rt) {
+            const u32x4_t zz = __builtin_bit_cast(u32x4_t, z[kb][rt]);
+            u32x4_t p1, p2, p3;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const f32x2_t v = unpack(zz[e]) * f32x2_t{f[2 * e], f[2 * e + 1]};
+                const uint32_t hi = pack(v);
+                uint32_t mid, lo;
+                parts(v - unpack(hi), mid, lo);
+                p1[e] = hi;
+                p2[e] = mid;
+                p3[e] = lo;
             }
+            z1[rt] = __builtin_bit_cast(bf16x8_t, p1);
+            z2[rt] = __builtin_bit_cast(bf16x8_t, p2);
+            z3[rt] = __builtin_bit_cast(bf16x8_t, p3);
         }
 #pragma unroll
         for (int pt = 0; pt < PT; ++pt) {
@@ -506,13 +523,17 @@ __global__ void __launch_bounds__(64 * waves_of(DP), 2) attend_kernel(AttendPara
     constexpr int C = Chunk<E>::C, W = waves_of(DP), RT = DP / 16 / W, PT = DP / 16;
     __shared__ typename LdsOf<E, DP, STATE>::type s;
     // the passes of one share, which read the same rows, go to one chiplet (eight in turn) one after another
-    const unsigned item = blockIdx.x / (8u * p.passes) * 8u + blockIdx.x % 8u;
+    // (quotients are formed by the vector unit: made scalar again, so that what follows from them is)
+    auto scalar = [](unsigned x) { return (unsigned)__builtin_amdgcn_readfirstlane((int)x); };
+    const unsigned eight = blockIdx.x / 8u, turn = scalar(eight / (unsigned)p.passes);
+    const unsigned item = turn * 8u + blockIdx.x % 8u;
     if (item >= (unsigned)p.rows * (unsigned)p.shares) return;
-    const Pass& a = p.pass[blockIdx.x / 8u % (unsigned)p.passes];
-    const int row = (int)(item / (unsigned)p.shares), share = (int)(item % (unsigned)p.shares);
-    const int b = row / p.heads, head = row % p.heads;
-    const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4, w = threadIdx.x >> 6;
-    const int L = row_length(p.lengths, b, p.T, p.status, head == 0 && share == 0 && threadIdx.x == 0);
+    const Pass& a = p.pass[eight - turn * (unsigned)p.passes];
+    const int row = (int)scalar(item / (unsigned)p.shares), share = (int)(item - (unsigned)row * (unsigned)p.shares);
+    const int b = (int)scalar((unsigned)row / (unsigned)p.heads), head = row - b * p.heads;
+    const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4;
+    const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int given = p.lengths[b * p.length_step], L = max(0, min(given, p.T));
     const int t0 = share * p.span, span = min(p.span, p.T - t0);
     const int len = max(0, min(L - t0, span));
     // the last share has no successor going forward, the first none going back
@@ -532,12 +553,26 @@ __global__ void __launch_bounds__(64 * waves_of(DP), 2) attend_kernel(AttendPara
 #pragma unroll
     for (int pt = 0; pt < PT; ++pt)
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
+        for (int rt = 0; rt < RT; ++rt) M[pt][rt] = f32x4_t{0, 0, 0, 0};
+    const int step_i = a.transposed ? 1 : p.Dv, step_c = a.transposed ? p.Dv : 1;
+    if (!STATE && start) {   // (all fetched before the first is looked at, as in Stage)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = 16 * pt + 4 * g + r, c = 16 * (w * RT + rt) + l;
-                M[pt][rt][r] = !STATE && start && i < a.P && c < a.R ? start[a.transposed ? c * p.Dv + i : i * p.Dv + c] : 0.0f;
-            }
+        for (int pt = 0; pt < PT; ++pt)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int i = min(16 * pt + 4 * g + r, a.P - 1), c = min(16 * (w * RT + rt) + l, a.R - 1);
+                    M[pt][rt][r] = start[i * step_i + c * step_c];
+                }
+#pragma unroll
+        for (int pt = 0; pt < PT; ++pt)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (16 * pt + 4 * g + r >= a.P || 16 * (w * RT + rt) + l >= a.R) M[pt][rt][r] = 0.0f;
+    }
 
     const int chunks = (len + C - 1) / C;
     Stage<E, DP, STATE, MODE> stage;
@@ -567,10 +602,12 @@ __global__ void __launch_bounds__(64 * waves_of(DP), 2) attend_kernel(AttendPara
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int i = 16 * pt + 4 * g + r, c = 16 * (w * RT + rt) + l;
-                    if (i < a.P && c < a.R) end[a.transposed ? c * p.Dv + i : i * p.Dv + c] = M[pt][rt][r];
+                    if (i < a.P && c < a.R) end[i * step_i + c * step_c] = M[pt][rt][r];
                 }
     }
     if constexpr (!STATE) {
+        // (here and not above: in a branch of some lanes, what follows it would be taken for lanes' own)
+        if (given != L && head == 0 && share == 0 && threadIdx.x == 0) atomicOr(p.status, STATUS_BAD_LENGTHS);
         // rows past the length: zeros
         const int c = threadIdx.x % DP;
         if (c < a.R)
@@ -584,7 +621,7 @@ __global__ void __launch_bounds__(256) attend_join_kernel(AttendParams p) {
     const int row = blockIdx.y, PR = a.P * a.R, e = blockIdx.x * 256 + threadIdx.x;
     if (e >= PR) return;
     const int b = row / p.heads, head = row % p.heads;
-    const int L = row_length(p.lengths, b, p.T, p.status, false);
+    const int L = clamp_length(p.lengths[b * p.length_step], p.T, p.status, false);
     float* share = a.share + (long long)row * p.shares * PR + e;
     float state = a.start ? a.start[(long long)row * PR + e] : 0.0f;
     const float whole = (float)power(p.log2a, head, p.span);
@@ -656,7 +693,7 @@ __global__ void __launch_bounds__(256) attend_step_kernel(StepParams a) {
 
 int check_sizes(int B, int heads, int Dk, int Dv, int T, int dtype, const float* decay) {
     if (B < 1 || heads < 1 || Dk < 1 || Dv < 1 || T < 1 || !valid_dtype(dtype) || !decay) return LSTM_DYN_ERR_INVALID;
-    if (Dk > MAX_D || Dv > MAX_D || (long long)B * heads >= 1 << 20 || (long long)B * T >= 1LL << 31 || T >= 1 << 30)
+    if (Dk > MAX_D || Dv > MAX_D || heads > MAX_HEADS || (long long)B * heads >= 1 << 20 || (long long)B * T >= 1LL << 31 || T >= 1 << 30)
         return LSTM_DYN_ERR_UNSUPPORTED;
     for (int i = 0; i < heads; ++i)
         if (!(decay[i] >= 0.0f && decay[i] <= 1.0f)) return LSTM_DYN_ERR_INVALID;
@@ -694,6 +731,7 @@ using namespace ldyn;
 struct lstm_dyn_attend : OpsHandle {
     int B = 0, heads = 0, Dk = 0, Dv = 0, T = 0, dtype = 0;
     int shares = 1, span = 0;
+    const int32_t* whole = nullptr;   // T
     const float* powers = nullptr;
     const double* log2a = nullptr;
     float* share = nullptr;   // [2][B heads][shares][Dk][Dv]: going forward, going back
@@ -729,10 +767,12 @@ static int attend_make(lstm_dyn_attend* h, const float* decay) {
     const long long ns = h->shares > 1 ? 8 * h->share_floats() : 0;
     int rc = ops_device(h);
     if (rc != LSTM_DYN_OK || (rc = ops_init(h, 256 + np + nl + ns)) != LSTM_DYN_OK) return rc;
+    h->whole = reinterpret_cast<const int32_t*>(h->block + 64);
     h->powers = reinterpret_cast<const float*>(h->block + 256);
     h->log2a = reinterpret_cast<const double*>(h->block + 256 + np);
     h->share = reinterpret_cast<float*>(h->block + 256 + np + nl);
-    if (hipMemcpy(h->block + 256, powers.data(), 4 * powers.size(), hipMemcpyHostToDevice) != hipSuccess ||
+    if (hipMemcpy(h->block + 64, &h->T, 4, hipMemcpyHostToDevice) != hipSuccess ||
+        hipMemcpy(h->block + 256, powers.data(), 4 * powers.size(), hipMemcpyHostToDevice) != hipSuccess ||
         hipMemcpy(h->block + 256 + np, logs.data(), 8 * logs.size(), hipMemcpyHostToDevice) != hipSuccess) {
         (void)hipGetLastError();
         (void)ops_free(h);
@@ -816,7 +856,8 @@ struct Parts {
 
 static AttendParams attend_params(const lstm_dyn_attend* h, const int32_t* lengths) {
     AttendParams p{};
-    p.lengths = lengths;
+    p.lengths = lengths ? lengths : h->whole;
+    p.length_step = lengths ? 1 : 0;
     p.status = h->status();
     p.powers = h->powers;
     p.log2a = h->log2a;
