@@ -38,7 +38,6 @@ namespace {
 constexpr int MAX_D = 128;
 constexpr int MAX_HEADS = 16384; // a chunk of 64 rows of heads 3 x 128 elements stays below NOWHERE
 constexpr int TABLE = 65;        // powers of a head's decay
-constexpr int WANT_GROUPS = 512; // workgroups that a pass should have
 
 typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
 
@@ -67,10 +66,17 @@ struct AttendParams {
 template <class E>
 struct Chunk;
 template <>
-struct Chunk<__bf16> { static constexpr int C = 64; };
+struct Chunk<__bf16> {
+    static constexpr int C = 64;
+    static constexpr int waves(int DP) { return DP == 32 ? 2 : 4; }
+    static constexpr int per_unit(int DP) { return DP == 128 ? 2 : 3; }   // waves a SIMD unit holds: registers and LDS
+};
 template <>
-struct Chunk<float> { static constexpr int C = 32; };
-constexpr int waves_of(int DP) { return DP == 32 ? 2 : 4; }
+struct Chunk<float> {
+    static constexpr int C = 32;
+    static constexpr int waves(int DP) { return DP / 16; }
+    static constexpr int per_unit(int) { return 4; }
+};
 
 __device__ inline double power(const double* log2a, int head, int n) { return n ? exp2(log2a[head] * n) : 1.0; }
 
@@ -107,7 +113,7 @@ enum { PIECES, SHIFTED, ELEMENTS };
 constexpr uint32_t NOWHERE = 1u << 30;   // a chunk's rows have fewer bytes
 template <class E, int DP, bool STATE, int MODE>
 struct Stage {
-    static constexpr int C = Chunk<E>::C, THREADS = 64 * waves_of(DP), N = 16 / (int)sizeof(E);
+    static constexpr int C = Chunk<E>::C, THREADS = 64 * Chunk<E>::waves(DP), N = 16 / (int)sizeof(E);
     static constexpr int COLS = DP / N, ROWS = C * COLS / THREADS;  // a thread's rows, one after another
     typedef typename Vec<E, N>::type piece_t;
     struct __attribute__((packed, aligned(sizeof(E)))) Loose { piece_t v; };
@@ -242,9 +248,10 @@ __device__ inline bf16x8_t join(bf16x4_t a, bf16x4_t b) { return __builtin_shuff
 
 // One chunk: n steps, out at its first step.
 template <int DP, bool STATE, bool WHOLE>
-__device__ inline void work(LdsBf16<DP, STATE>& s, const Pass& a, f32x4_t (&M)[DP / 16][DP / 16 / waves_of(DP)], int n,
+__device__ inline void work(LdsBf16<DP, STATE>& s, const Pass& a, f32x4_t (&M)[DP / 16][DP / 16 / Chunk<__bf16>::waves(DP)], int n,
                             __bf16* out) {
-    constexpr int W = waves_of(DP), RT = DP / 16 / W, PT = DP / 16, KB = DP / 32, IT = 4 / W, COLS = DP / 8;
+    constexpr int W = Chunk<__bf16>::waves(DP), RT = DP / 16 / W, PT = DP / 16, KB = DP / 32, COLS = DP / 8;
+    constexpr int IT = 4 / W;   // a wave's rows of tiles of the masked products
     const int lane = here() & 63, l = lane & 15, g = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     constexpr int MASK = (COLS < 8 ? COLS : 8) - 1;
@@ -253,9 +260,10 @@ __device__ inline void work(LdsBf16<DP, STATE>& s, const Pass& a, f32x4_t (&M)[D
     if constexpr (!STATE) {
         // the products under the mask: this wave's steps i against all j, one column i a lane
         f32x4_t A[IT][4];
+        const int it0 = w * IT;
 #pragma unroll
         for (int q = 0; q < IT; ++q) {
-            const int it = w * IT + q;
+            const int it = it0 + q;
 #pragma unroll
             for (int jt = 0; jt < 4; ++jt) A[q][jt] = f32x4_t{0, 0, 0, 0};
 #pragma unroll
@@ -287,9 +295,10 @@ __device__ inline void work(LdsBf16<DP, STATE>& s, const Pass& a, f32x4_t (&M)[D
                     hi[r] = h;
                     lo[r] = o;
                 }
-                const int i = 16 * (w * IT + q) + l;
-                *reinterpret_cast<u32x2_t*>(at<8>(s.y + 4 * (g & 1), i, 2 * jt, half_in_a)) = hi;
-                *reinterpret_cast<u32x2_t*>(at<8>(s.y + 64 * 64 + 4 * (g & 1), i, 2 * jt, half_in_a)) = lo;
+                const int i = 16 * (it0 + q) + l;
+                __bf16* to = at<8>(s.y + 4 * (g & 1), i, 2 * jt, half_in_a);
+                *reinterpret_cast<u32x2_t*>(to) = hi;
+                *reinterpret_cast<u32x2_t*>(to + 64 * 64) = lo;
             }
         __syncthreads();
     }
@@ -420,9 +429,9 @@ __device__ inline void put_chunk(LdsF32<DP, STATE>& s, const Stage<float, DP, ST
 __device__ inline f32x4_t mfma(float a, float b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
 template <int DP, bool STATE, bool WHOLE>
-__device__ inline void work(LdsF32<DP, STATE>& s, const Pass& a, f32x4_t (&M)[DP / 16][DP / 16 / waves_of(DP)], int n,
+__device__ inline void work(LdsF32<DP, STATE>& s, const Pass& a, f32x4_t (&M)[DP / 16][DP / 16 / Chunk<float>::waves(DP)], int n,
                             float* out) {
-    constexpr int W = waves_of(DP), RT = DP / 16 / W, PT = DP / 16, LD = LdsF32<DP, STATE>::LD;
+    constexpr int W = Chunk<float>::waves(DP), RT = DP / 16 / W, PT = DP / 16, LD = LdsF32<DP, STATE>::LD;
     const int lane = here() & 63, l = lane & 15, g = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     if constexpr (!STATE) {
@@ -519,8 +528,8 @@ struct LdsOf<float, DP, STATE> { typedef LdsF32<DP, STATE> type; };
 
 // STATE: what each share adds to the state, alone.
 template <class E, int DP, bool STATE, int MODE>
-__global__ void __launch_bounds__(64 * waves_of(DP), 2) attend_kernel(AttendParams p) {
-    constexpr int C = Chunk<E>::C, W = waves_of(DP), RT = DP / 16 / W, PT = DP / 16;
+__global__ void __launch_bounds__(64 * Chunk<E>::waves(DP), Chunk<E>::per_unit(DP)) attend_kernel(AttendParams p) {
+    constexpr int C = Chunk<E>::C, W = Chunk<E>::waves(DP), RT = DP / 16 / W, PT = DP / 16;
     __shared__ typename LdsOf<E, DP, STATE>::type s;
     // the passes of one share, which read the same rows, go to one chiplet (eight in turn) one after another
     // (quotients are formed by the vector unit: made scalar again, so that what follows from them is)
@@ -625,11 +634,22 @@ __global__ void __launch_bounds__(256) attend_join_kernel(AttendParams p) {
     float* share = a.share + (long long)row * p.shares * PR + e;
     float state = a.start ? a.start[(long long)row * PR + e] : 0.0f;
     const float whole = (float)power(p.log2a, head, p.span);
-    for (int i = 0; i < p.shares; ++i) {
-        const int k = a.back ? p.shares - 1 - i : i, len = max(0, min(L - k * p.span, p.span));
-        const float add = len && i < p.shares - 1 ? share[(long long)k * PR] : 0.0f;
-        share[(long long)k * PR] = state;
-        if (len) state = (len == p.span ? whole : (float)power(p.log2a, head, len)) * state + add;
+    constexpr int AT_ONCE = 8;   // fetched before the first is used
+    for (int i0 = 0; i0 < p.shares; i0 += AT_ONCE) {
+        float add[AT_ONCE];
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+            const int i = min(i0 + j, p.shares - 1), k = a.back ? p.shares - 1 - i : i;
+            add[j] = share[(long long)k * PR];
+        }
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+            const int i = i0 + j, k = a.back ? p.shares - 1 - i : i, len = max(0, min(L - k * p.span, p.span));
+            if (i >= p.shares) break;
+            share[(long long)k * PR] = state;
+            // (a share without steps has left nothing there, nor has the last one)
+            if (len) state = (len == p.span ? whole : (float)power(p.log2a, head, len)) * state + (i < p.shares - 1 ? add[j] : 0.0f);
+        }
     }
 }
 
@@ -748,12 +768,18 @@ extern "C" int lstm_dyn_check_attend_args(int B, int heads, int Dk, int Dv, int 
 }
 
 static int attend_make(lstm_dyn_attend* h, const float* decay) {
-    // shares of four chunks and more, as many as bring WANT_GROUPS workgroups
+    // As many shares as bring 512 workgroups with bf16 data, 256 with fp32, since a share costs a second
+    // reading of two operands and its states.  From 256 rows and heads on, which fill the device
+    // by themselves, a share has to be 16 chunks: below, the states cost more than the even
+    // load gains (a training step, us, shares as these rules give them and with one number for all:
+    // 1 x 32768 x 16 heads, forward alone, 304 and 355 with 256; 32 x 512 x 8 heads of 64, 91 and 130;
+    // 5 x 301 x 3 heads in fp32 64 and with shares of four chunks and more 116; 4 x 1024 x 8 heads in fp32 212
+    // and 236 with 512).
     const int C = h->dtype == LSTM_DYN_BF16 ? Chunk<__bf16>::C : Chunk<float>::C;
-    const int rows = h->B * h->heads, chunks = (h->T + C - 1) / C;
-    const int want = rows >= WANT_GROUPS ? 1 : (WANT_GROUPS + rows - 1) / rows;
+    const int rows = h->B * h->heads, chunks = (h->T + C - 1) / C, groups = h->dtype == LSTM_DYN_BF16 ? 512 : 256;
+    const int want = rows >= groups ? 1 : (groups + rows - 1) / rows;
     int each = (chunks + want - 1) / want;
-    if (each < 4) each = 4;
+    if (rows >= 256 && each < 16) each = 16;
     h->shares = (chunks + each - 1) / each;
     h->span = each * C;
     std::vector<float> powers((size_t)h->heads * TABLE);
@@ -814,11 +840,11 @@ static int launch_mode(lstm_dyn_attend* h, const AttendParams& p) {
     const int d = h->Dk > h->Dv ? h->Dk : h->Dv;
     const long long items = (long long)p.rows * p.shares, grid = (items + 7) / 8 * 8 * p.passes;
     if (d <= 32)
-        hipLaunchKernelGGL((attend_kernel<E, 32, STATE, MODE>), dim3((unsigned)grid), dim3(64 * waves_of(32)), 0, h->last_stream, p);
+        hipLaunchKernelGGL((attend_kernel<E, 32, STATE, MODE>), dim3((unsigned)grid), dim3(64 * Chunk<E>::waves(32)), 0, h->last_stream, p);
     else if (d <= 64)
-        hipLaunchKernelGGL((attend_kernel<E, 64, STATE, MODE>), dim3((unsigned)grid), dim3(64 * waves_of(64)), 0, h->last_stream, p);
+        hipLaunchKernelGGL((attend_kernel<E, 64, STATE, MODE>), dim3((unsigned)grid), dim3(64 * Chunk<E>::waves(64)), 0, h->last_stream, p);
     else
-        hipLaunchKernelGGL((attend_kernel<E, 128, STATE, MODE>), dim3((unsigned)grid), dim3(64 * waves_of(128)), 0, h->last_stream, p);
+        hipLaunchKernelGGL((attend_kernel<E, 128, STATE, MODE>), dim3((unsigned)grid), dim3(64 * Chunk<E>::waves(128)), 0, h->last_stream, p);
     return ops_launched(h);
 }
 template <class E, bool STATE>
