@@ -11,7 +11,10 @@
 // (many equal logits), the range is cut again by key until they are not.  Then the kept weights of each
 // segment of the row are summed, and one wave walks the segment that u falls into.
 //
-// A workgroup holds a row: its two to six passes come from the L2 after the first.
+// A workgroup holds a row: its two to six passes come from the L2 after the first.  They are bound by the
+// vector unit of its CU, so where most tokens do not count a pass looks at them with as few instructions as
+// decide that (a difference, a product and a comparison), and forms keys and weights of the rest
+// alone; where most of them count it does the same for all, under no condition.
 #include "ops.h"
 #include "../../include/lstm_dyn_layer.h"
 
@@ -45,27 +48,38 @@ struct RowLds {
     int range, count, first;
 };
 
-// A larger logit, then a lower index, is a larger key.  x is no NaN and no -0.
+// A larger logit, then a lower index, is a larger key.  x is no NaN; -0 is 0.
 __device__ inline u64 key_of(float x, int i) {
-    const uint32_t b = __float_as_uint(x);
+    const uint32_t b = __float_as_uint(x + 0.0f);
     return (u64)(b & 0x80000000u ? ~b : b | 0x80000000u) << 32 | (uint32_t)~i;
 }
+__device__ inline float logit_of(u64 key) {
+    const uint32_t b = (uint32_t)(key >> 32);
+    return __uint_as_float(b & 0x80000000u ? b & 0x7fffffffu : ~b);
+}
 
-// NaN as -inf, -0 as 0.
-__device__ inline float clean(float x) { return x == x ? x + 0.0f : -__builtin_inff(); }
+// NaN as -inf.
+__device__ inline float clean(float x) { return fmaxf(x, -__builtin_inff()); }
 
 // exp((x - largest) / T): 1 / (T ln 2) is held in two parts, so its rounding does not
 // tilt the weights of tokens far from the largest.
 struct Weigh {
-    float largest, hi, lo, unit;
+    float largest, hi, lo, unit, none;
+    // How far below the largest x is, in ranges of the histogram.  From `none` on there is no weight, nearer
+    // p rounds to a multiple of 1 / unit that is not zero.  (-inf at an infinite T: the last range.)
+    __device__ float depth(float x) const { return fminf((x - largest) * hi * (-BINS / REACH), (float)(BINS - 1)); }
     __device__ float power(float x) const {
-        const float d = x == largest ? 0.0f : x - largest;
-        const float t = d * hi;
-        const float e = __builtin_amdgcn_exp2f(t);
-        if (!(t > -100.0f)) return 0.0f;
+        const float d = x - largest, t = d * hi, e = __builtin_amdgcn_exp2f(t);
         return e + e * ((__builtin_fmaf(d, hi, -t) + d * lo) * 0.69314718f);
     }
     __device__ u64 weight(float p) const { return (u64)rintf(p * unit); }
+};
+
+// The tokens of the order's start: all of some weight whose keys are `key` or more.
+struct Start {
+    u64 key = 0;
+    float logit = -__builtin_inff();   // of `key`: a smaller one is out
+    __device__ bool has(float x, int i) const { return x > logit || (x == logit && key_of(x, i) >= key); }
 };
 
 // A row in pieces of 16 bytes, the first and the last perhaps in part.
@@ -152,44 +166,54 @@ __device__ inline void crossing(RowLds& s, int n, u64 target, G value) {
     __syncthreads();
 }
 
-// The least key of the shortest start of the tokens in order whose measure (their number, or with
-// MASS their weight) reaches the target, among the tokens of some weight with keys of `least` or more.
-// aim(all): the target, given the sum of all measures; if it is no less than all there is, `least` is returned.
-template <int THREADS, bool MASS, class E, class A>
-__device__ inline u64 find_cut(RowLds& s, const Row<E>& row, const Weigh& weigh, u64 least, A aim) {
+// The shortest start, within `within` (ALL: it is all tokens), whose measure (the tokens' number, or with MASS
+// their weight) reaches the target.  aim(all): the target, given the sum of all measures; if it is no less than
+// all there is, `within` itself.
+template <int THREADS, bool MASS, bool ALL, class E, class A>
+__device__ inline Start find_start(RowLds& s, const Row<E>& row, const Weigh& weigh, const Start within, A aim) {
     const int tid = threadIdx.x;
-    // the largest key is in range 0
-    auto range_of = [&](float x) {
-        const float d = x == weigh.largest ? 0.0f : weigh.largest - x;
-        return (int)fminf(d * weigh.hi * (BINS / REACH), (float)(BINS - 1));
+    auto clear = [&] {
+        for (int i = tid; i < BINS; i += THREADS) s.hist[i] = 0;
+        __syncthreads();
     };
-    for (int i = tid; i < BINS; i += THREADS) s.hist[i] = 0;
-    __syncthreads();
+    auto measure = [&](float x) { return MASS ? weigh.weight(weigh.power(x)) : 1ull; };
+    clear();
     row.each(tid, row.pieces, THREADS, [&](float x, int i) {
-        if (key_of(x, i) < least) return;
-        const u64 w = weigh.weight(weigh.power(x));
-        if (w) atomicAdd(&s.hist[range_of(x)], MASS ? w : 1ull);
+        const float q = weigh.depth(x);
+        const bool on = q < weigh.none;
+        if constexpr (ALL) {
+            // (the weight of -inf at an infinite T is that of no number: not taken)
+            const u64 m = measure(x);
+            if constexpr (MASS) atomicAdd(&s.hist[(int)q], on ? m : 0ull);
+            else atomicAdd(reinterpret_cast<uint32_t*>(&s.hist[(int)q]), on ? 1u : 0u);
+        } else {
+            if (on && x >= within.logit && within.has(x, i)) atomicAdd(&s.hist[(int)q], measure(x));
+        }
     });
     __syncthreads();
     crossing<THREADS>(s, BINS, 0, [&](int i) { return s.hist[i]; });  // the sum alone
     const u64 all = s.total, target = aim(all);
-    if (target >= all) return least;
+    if (target >= all) return within;
     crossing<THREADS>(s, BINS, target, [&](int i) { return s.hist[i]; });
-    const int range = s.range;
-    u64 rest = s.rest, lo = least, hi = ~0ull;
+    const int at = s.range;
+    // f(x, key) of the range's tokens
+    auto each = [&](auto f) {
+        row.each(tid, row.pieces, THREADS, [&](float x, int i) {
+            const float q = weigh.depth(x);
+            if ((int)q == at && q < weigh.none && (ALL || within.has(x, i))) f(x, key_of(x, i));
+        });
+    };
+    u64 rest = s.rest, lo = 0, hi = ~0ull;
     for (bool by_key = false;; by_key = true) {
         // the tokens of the range, if they are few
         if (tid == 0) s.count = 0;
         __syncthreads();
-        row.each(tid, row.pieces, THREADS, [&](float x, int i) {
-            const u64 key = key_of(x, i);
-            if (key < lo || key > hi || range_of(x) != range) return;
-            const u64 w = weigh.weight(weigh.power(x));
-            if (!w) return;
-            const int at = atomicAdd(&s.count, 1);
-            if (at < LIST) {
-                s.key[at] = key;
-                s.weight[at] = MASS ? w : 1ull;
+        each([&](float x, u64 key) {
+            if (key < lo || key > hi) return;
+            const int to = atomicAdd(&s.count, 1);
+            if (to < LIST) {
+                s.key[to] = key;
+                s.weight[to] = measure(x);
             }
         });
         __syncthreads();
@@ -198,18 +222,18 @@ __device__ inline u64 find_cut(RowLds& s, const Row<E>& row, const Weigh& weigh,
             for (int e = tid; e < n; e += THREADS) {
                 const u64 key = s.key[e];
                 u64 before = 0;
+#pragma unroll 4
                 for (int f = 0; f < n; ++f) before += s.key[f] > key ? s.weight[f] : 0ull;
                 if (before < rest && before + s.weight[e] >= rest) s.found = key;
             }
             __syncthreads();
-            return s.found;
+            const u64 key = s.found;
+            return Start{key, logit_of(key)};
         }
         // cut [lo, hi] again: at first by the keys that are in it
         if (!by_key) {
             u64 a = ~0ull, b = 0;
-            row.each(tid, row.pieces, THREADS, [&](float x, int i) {
-                const u64 key = key_of(x, i);
-                if (key < lo || range_of(x) != range || !weigh.weight(weigh.power(x))) return;
+            each([&](float x, u64 key) {
                 a = key < a ? key : a;
                 b = key > b ? key : b;
             });
@@ -230,17 +254,13 @@ __device__ inline u64 find_cut(RowLds& s, const Row<E>& row, const Weigh& weigh,
             }
             lo = a;
             hi = b;
+            __syncthreads();
         }
         int shift = 0;
         while ((hi - lo) >> shift >= BINS) ++shift;
-        __syncthreads();
-        for (int i = tid; i < BINS; i += THREADS) s.hist[i] = 0;
-        __syncthreads();
-        row.each(tid, row.pieces, THREADS, [&](float x, int i) {
-            const u64 key = key_of(x, i);
-            if (key < lo || key > hi || range_of(x) != range) return;
-            const u64 w = weigh.weight(weigh.power(x));
-            if (w) atomicAdd(&s.hist[(hi - key) >> shift], MASS ? w : 1ull);
+        clear();
+        each([&](float x, u64 key) {
+            if (key >= lo && key <= hi) atomicAdd(&s.hist[(hi - key) >> shift], measure(x));
         });
         __syncthreads();
         crossing<THREADS>(s, BINS, rest, [&](int i) { return s.hist[i]; });
@@ -249,6 +269,72 @@ __device__ inline u64 find_cut(RowLds& s, const Row<E>& row, const Weigh& weigh,
         lo = top - lo > width ? top - width : lo;
         hi = top;
     }
+}
+
+// weight(x, index) of all tokens is summed by index; found(x, index, all) is called by one thread, for the first token at which
+// the running sum reaches aim(all).
+template <int THREADS, class E, class W, class A, class F>
+__device__ inline void walk(RowLds& s, const Row<E>& row, W weight, A aim, F found) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    // segments of 64 `rounds` pieces, each the work of one wave
+    const int rounds = (row.pieces + 64 * SEGMENTS - 1) / (64 * SEGMENTS);
+    __syncthreads();
+    for (int i = tid; i < SEGMENTS; i += THREADS) s.segment[i] = 0;
+    __syncthreads();
+    const int segments = (row.pieces + 64 * rounds - 1) / (64 * rounds);
+    for (int g = wave; g < segments; g += THREADS / 64) {
+        u64 sum = 0;
+        const int k0 = g * 64 * rounds;
+        row.each(k0 + lane, min(row.pieces, k0 + 64 * rounds), 64, [&](float x, int i) { sum += weight(x, i); });
+        sum = wave_sum(sum);
+        if (lane == 0) s.segment[g] = sum;
+    }
+    __syncthreads();
+    crossing<THREADS>(s, SEGMENTS, 0, [&](int i) { return s.segment[i]; });
+    const u64 all = s.total;
+    crossing<THREADS>(s, SEGMENTS, aim(all), [&](int i) { return s.segment[i]; });
+    if (wave != 0) return;
+    u64 rest = s.rest;
+    const int k0 = s.range * 64 * rounds;
+    for (int r = 0; r < rounds; ++r) {
+        const int k = k0 + r * 64 + lane;
+        constexpr int M = Row<E>::N;
+        float x[M];
+        u64 w[M], sum = 0;
+        if (k < row.pieces) {
+            const auto raw = row.piece(k);
+#pragma unroll
+            for (int j = 0; j < M; ++j) x[j] = clean((float)raw[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < M; ++j) {
+            w[j] = k < row.pieces ? weight(x[j], k * M - row.off + j) : 0;
+            sum += w[j];
+        }
+        const u64 up = wave_scan(sum);
+        if (up >= rest && up - sum < rest) {
+            u64 before = up - sum;
+#pragma unroll
+            for (int j = 0; j < M; ++j) {
+                if (before < rest && before + w[j] >= rest) found(x[j], k * M - row.off + j, all);
+                before += w[j];
+            }
+        }
+        const u64 whole = __shfl(up, 63);
+        if (whole >= rest) break;
+        rest -= whole;
+    }
+}
+
+// The first running sum above u of all.
+__device__ inline u64 above(float u, u64 all) {
+    u = fminf(fmaxf(u, 0.0f), 1.0f);   // (a NaN is 0)
+    const u64 t = (u64)((double)u * (double)all) + 1;
+    return t < all ? t : all;
+}
+__device__ inline u64 top_p_of(float top_p, u64 all) {
+    const u64 t = (u64)ceil((double)top_p * (double)all);
+    return t ? t : 1ull;
 }
 
 template <class E, int THREADS>
@@ -296,79 +382,60 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(SampleParams a) {
         return;
     }
 
+    const float u = a.u[n];
+    if (mx == __builtin_inff()) {
+        // such tokens are alike: their number is cut, not their sum
+        walk<THREADS>(
+            s, row, [&](float x, int) { return x == mx ? 1ull : 0ull; },
+            [&](u64 all) {
+                u64 kept = top_k && (u64)top_k < all ? (u64)top_k : all;
+                if (top_p < 1.0f) kept = top_p_of(top_p, kept);
+                if (tid == 0) s.found = kept;
+                return above(u, kept);
+            },
+            [&](float, int i, u64) {
+                a.token[n] = i;
+                a.logp[n] = (float)-log((double)s.found);
+            });
+        return;
+    }
+
     Weigh weigh;
     weigh.largest = mx;
     weigh.hi = (float)per;
     weigh.lo = (float)(per - (double)weigh.hi);
     weigh.unit = __uint_as_float((uint32_t)(a.bits + 127) << 23);
-    u64 cut = 0;
-    if (top_k) cut = find_cut<THREADS, false>(s, row, weigh, cut, [&](u64) { return (u64)top_k; });
-    if (top_p < 1.0f)
-        cut = find_cut<THREADS, true>(s, row, weigh, cut, [&](u64 all) {
-            const u64 t = (u64)ceil((double)top_p * (double)all);
-            return t ? t : 1ull;
-        });
-
-    // a kept token's weight, or zero
-    auto kept = [&](float x, int i) -> u64 {
-        if (key_of(x, i) < cut) return 0;
-        const float p = weigh.power(x);
-        return least_p && p < min_p ? 0 : weigh.weight(p);
+    weigh.none = ((float)a.bits + 0.5f) * (BINS / REACH);
+    auto token = [&](float x, int i, u64 all) {
+        a.token[n] = i;
+        a.logp[n] = (float)(((double)x - (double)mx) / (double)T - log((double)all * exp2(-(double)a.bits)));
     };
-    // segments of 64 `rounds` pieces, each the work of one wave
-    const int rounds = (row.pieces + 64 * SEGMENTS - 1) / (64 * SEGMENTS);
-    for (int i = tid; i < SEGMENTS; i += THREADS) s.segment[i] = 0;
-    __syncthreads();
-    const int segments = (row.pieces + 64 * rounds - 1) / (64 * rounds);
-    for (int g = wave; g < segments; g += THREADS / 64) {
-        u64 sum = 0;
-        const int k0 = g * 64 * rounds;
-        row.each(k0 + lane, min(row.pieces, k0 + 64 * rounds), 64, [&](float x, int i) { sum += kept(x, i); });
-        sum = wave_sum(sum);
-        if (lane == 0) s.segment[g] = sum;
+    auto aim = [&](u64 all) { return above(u, all); };
+    Start start;
+    if (top_k) {
+        start = find_start<THREADS, false, true>(s, row, weigh, start, [&](u64) { return (u64)top_k; });
+        if (top_p < 1.0f)
+            start = find_start<THREADS, true, false>(s, row, weigh, start, [&](u64 all) { return top_p_of(top_p, all); });
+    } else if (top_p < 1.0f) {
+        start = find_start<THREADS, true, true>(s, row, weigh, start, [&](u64 all) { return top_p_of(top_p, all); });
+    } else if (!least_p) {
+        walk<THREADS>(
+            s, row,
+            [&](float x, int) {
+                const u64 w = weigh.weight(weigh.power(x));
+                return weigh.depth(x) < weigh.none ? w : 0ull;
+            },
+            aim, token);
+        return;
     }
-    __syncthreads();
-    crossing<THREADS>(s, SEGMENTS, 0, [&](int i) { return s.segment[i]; });
-    const u64 all = s.total;
-    const float u = fminf(fmaxf(a.u[n], 0.0f), 1.0f);   // (a NaN is 0)
-    u64 target = (u64)((double)u * (double)all) + 1;    // the first running sum above u of all
-    if (target > all) target = all;
-    crossing<THREADS>(s, SEGMENTS, target, [&](int i) { return s.segment[i]; });
-    if (wave != 0) return;
-    u64 rest = s.rest;
-    const int k0 = s.range * 64 * rounds;
-    for (int r = 0; r < rounds; ++r) {
-        const int k = k0 + r * 64 + lane;
-        constexpr int M = Row<E>::N;
-        float x[M];
-        u64 w[M], sum = 0;
-        if (k < row.pieces) {
-            const auto raw = row.piece(k);
-#pragma unroll
-            for (int j = 0; j < M; ++j) x[j] = clean((float)raw[j]);
-        }
-#pragma unroll
-        for (int j = 0; j < M; ++j) {
-            w[j] = k < row.pieces ? kept(x[j], k * M - row.off + j) : 0;
-            sum += w[j];
-        }
-        const u64 up = wave_scan(sum);
-        if (up >= rest && up - sum < rest) {
-            u64 before = up - sum;
-#pragma unroll
-            for (int j = 0; j < M; ++j) {
-                if (before < rest && before + w[j] >= rest) {
-                    const double d = x[j] == mx ? 0.0 : (double)x[j] - (double)mx;
-                    a.token[n] = k * M - row.off + j;
-                    a.logp[n] = (float)(d / (double)T - log((double)all * exp2(-(double)a.bits)));
-                }
-                before += w[j];
-            }
-        }
-        const u64 whole = __shfl(up, 63);
-        if (whole >= rest) break;
-        rest -= whole;
-    }
+    walk<THREADS>(
+        s, row,
+        [&](float x, int i) -> u64 {
+            if (!(x >= start.logit && weigh.depth(x) < weigh.none && start.has(x, i))) return 0;
+            const float p = weigh.power(x);
+            return least_p && p < min_p ? 0 : weigh.weight(p);
+        },
+        aim, token);
 }
 
 int check_sizes(int N, int V, int dtype) {
