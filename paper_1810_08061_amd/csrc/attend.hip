@@ -174,40 +174,57 @@ struct Stage {
     }
 };
 
-// Four elements of a row of out, from column c.
-template <class E, bool WHOLE>
-__device__ inline void put_four(E* p, int c, int width, f32x4_t v) {
-    if constexpr (WHOLE) {
-        if (c < width) {
-            typedef typename Vec<E, 4>::type four_t;
-            *reinterpret_cast<four_t*>(p + c) = __builtin_convertvector(v, four_t);
-        }
-    } else {
+// out's rows 16 it + l from tiles whose lanes hold four columns of a row, from column c on.  WHOLE: through a
+// descriptor, as Stage fetches.
+template <class E, int TI, int RT, bool WHOLE>
+__device__ inline void put_rows(E* out, const Pass& a, int n, int c, int l, const f32x4_t (&O)[TI][RT]) {
+    typedef typename Vec<E, 4>::type four_t;
+    const uint32_t row = (uint32_t)a.ldo * (uint32_t)sizeof(E);
+    const auto rows = __builtin_amdgcn_make_buffer_rsrc(out, 0, (int)(n * row), 0x00027000);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (c + i < width) p[c + i] = (E)v[i];
+    for (int rt = 0; rt < RT; ++rt) {
+        const int cc = c + 16 * rt;
+        const uint32_t to = WHOLE && cc >= a.R ? NOWHERE : (uint32_t)l * row + (uint32_t)cc * (uint32_t)sizeof(E);
+#pragma unroll
+        for (int it = 0; it < TI; ++it) {
+            if constexpr (WHOLE) {
+                const four_t e = __builtin_convertvector(O[it][rt], four_t);
+                if constexpr (sizeof(E) == 2)
+                    __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2_t, e), rows, to + it * 16 * row, 0, 0);
+                else
+                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, e), rows, to + it * 16 * row, 0, 0);
+            } else if (16 * it + l < n) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (cc + i < a.R) out[(16 * it + l) * a.ldo + cc + i] = (E)O[it][rt][i];
+            }
+        }
     }
 }
 
 // --- bf16 ------------------------------------------------------------------
 
-// LDS rows are of 16-byte pieces, whose places are exchanged within a row by the row's number, so that
-// a column of pieces lies in different banks: piece k of a row lies at k ^ swap(row), where the swap
-// (0 to 7) of rows by steps is row & 7, of rows by columns (y and z transposed) (row ^ row / 8) & 7.
-// What a lane's numbers give (row, swap and piece together) is formed once and the rest are
-// constants, so that few addresses are kept.
-template <int PIECES>
+// LDS holds the chunk's rows by steps, each in 16-byte pieces whose places are exchanged within the row: piece k
+// of row r lies at k ^ swap_of(r), so that neither a column of pieces over eight rows nor one of pairs of
+// pieces over four rows (what the transposing read takes) lies in few banks.  The parts of a row's number
+// may be exchanged one by one (swap_of(a ^ b) = swap_of(a) ^ swap_of(b)).  What a lane's numbers
+// give (row, exchange and piece together) is formed once and the rest are constants, so that few addresses are kept.
+template <int COLS>
+__device__ constexpr int swap_of(int row) {
+    return COLS >= 8 ? (row & 3) << 1 | (row >> 2 & 1) : (row >> 3 & 1) << 1 | (row >> 2 & 1);
+}
+template <int COLS>
 __device__ inline __bf16* at(__bf16* base, int row, int piece, int lane_swap) {
-    return base + row * PIECES * 8 + (piece & ~7) * 8 + ((piece & 7) ^ lane_swap) * 8;
+    return base + row * COLS * 8 + (piece & ~7) * 8 + ((piece & 7) ^ lane_swap) * 8;
 }
 
 template <int DP, bool STATE>
 struct LdsBf16 {
-    // y by steps makes room for the masked products, two parts of 64 x 64, once they are formed
-    __bf16 x[STATE ? 8 : 64 * DP];
-    __bf16 y[STATE ? 8 : (DP > 64 ? 64 * DP : 64 * 128)];
-    __bf16 yt[DP * 64];
-    __bf16 zt[DP * 64];
+    // x makes room for the masked products, two parts of 64 x 64, once it has been read
+    __bf16 x[STATE ? 8 : (DP > 64 ? 64 * DP : 64 * 128)];
+    __bf16 y[64 * DP];
+    __bf16 z[64 * DP];
+    __bf16 out[STATE ? 8 : 64 * DP];
     float powers[TABLE + 3];
 };
 
@@ -216,28 +233,12 @@ __device__ inline void put_chunk(LdsBf16<DP, STATE>& s, const Stage<__bf16, DP, 
     typedef Stage<__bf16, DP, STATE, MODE> G;
     constexpr int ROWS = G::ROWS, COLS = G::COLS;
     const unsigned id = here();
-    const int o = (int)(id % COLS), r0 = (int)(id / COLS) * ROWS;
-    if constexpr (!STATE) {
-        constexpr int MASK = (COLS < 8 ? COLS : 8) - 1;
-        const int swap = (o & 7) ^ (r0 & MASK), o8 = (o & ~7) * 8;
+    const int o = (int)(id % COLS), r0 = (int)(id / COLS) * ROWS, swap = (o & 7) ^ swap_of<COLS>(r0), o8 = (o & ~7) * 8;
 #pragma unroll
-        for (int q = 0; q < ROWS; ++q) {
-            *reinterpret_cast<bf16x8_t*>(at<COLS>(s.x + o8, r0 + q, q, swap)) = g.x[q];
-            *reinterpret_cast<bf16x8_t*>(at<COLS>(s.y + o8, r0 + q, q, swap)) = g.y[q];
-        }
-    }
-    typedef typename Vec<__bf16, ROWS>::type run_t;
-    const int swap = (r0 / 8) ^ (o & 7);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        run_t y, z;
-#pragma unroll
-        for (int q = 0; q < ROWS; ++q) {
-            y[q] = g.y[q][e];
-            z[q] = g.z[q][e];
-        }
-        *reinterpret_cast<run_t*>(at<8>(s.yt + r0 % 8, 8 * o + e, e, swap)) = y;
-        *reinterpret_cast<run_t*>(at<8>(s.zt + r0 % 8, 8 * o + e, e, swap)) = z;
+    for (int q = 0; q < ROWS; ++q) {
+        if constexpr (!STATE) *reinterpret_cast<bf16x8_t*>(at<COLS>(s.x + o8, r0 + q, swap_of<COLS>(q), swap)) = g.x[q];
+        *reinterpret_cast<bf16x8_t*>(at<COLS>(s.y + o8, r0 + q, swap_of<COLS>(q), swap)) = g.y[q];
+        *reinterpret_cast<bf16x8_t*>(at<COLS>(s.z + o8, r0 + q, swap_of<COLS>(q), swap)) = g.z[q];
     }
 }
 
@@ -246,120 +247,181 @@ __device__ inline f32x4_t mfma(bf16x8_t a, bf16x8_t b, f32x4_t c) {
 }
 __device__ inline bf16x8_t join(bf16x4_t a, bf16x4_t b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 
-// One chunk: n steps, out at its first step.
-template <int DP, bool STATE, bool WHOLE>
-__device__ inline void work(LdsBf16<DP, STATE>& s, const Pass& a, f32x4_t (&M)[DP / 16][DP / 16 / Chunk<__bf16>::waves(DP)], int n,
-                            __bf16* out) {
-    constexpr int W = Chunk<__bf16>::waves(DP), RT = DP / 16 / W, PT = DP / 16, KB = DP / 32, COLS = DP / 8;
+// Where a lane reads columns: sixteen lanes read four rows of sixteen columns, and each is given the four
+// elements of its column (an LDS read that transposes).  Rows 8 g to 8 g + 7 in two such reads.
+// A piece of the masked products [64][64]: piece k of row r at k ^ (r & 7).
+__device__ inline __bf16* in_square(__bf16* base, int row, int piece, int lane_swap) {
+    return base + row * 64 + (piece ^ lane_swap) * 8;
+}
+struct Columns {
+    int row, swap, half;
+    template <int COLS>
+    __device__ void init(int l, int g) {
+        row = 8 * g + (l >> 2);
+        swap = ((l & 3) >> 1) ^ swap_of<COLS>(row);
+        half = 4 * (l & 1);
+    }
+};
+// Column l of tile ct (16 columns), rows 32 kb + 8 g + 0 .. 7: an operand's part of a lane.
+template <int COLS>
+__device__ inline bf16x8_t columns(__bf16* base, const Columns& c, int ct, int kb) {
+    typedef short s16x4_t __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4_t* lds_t;
+    __bf16* lo = at<COLS>(base + c.half, 32 * kb + c.row, 2 * ct, c.swap);
+    __bf16* hi = at<COLS>(base + c.half, 32 * kb + 4 + c.row, (2 * ct) ^ swap_of<COLS>(4), c.swap);
+    return join(__builtin_bit_cast(bf16x4_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)lo)),
+                __builtin_bit_cast(bf16x4_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)hi)));
+}
+
+// One chunk of n steps, out at its first step: what it gives.
+template <int DP, bool WHOLE>
+__device__ inline void give(LdsBf16<DP, false>& s, const Pass& a, const f32x4_t (&M)[DP / 16][DP / 16 / Chunk<__bf16>::waves(DP)],
+                            int n, __bf16* out) {
+    constexpr int W = Chunk<__bf16>::waves(DP), RT = DP / 16 / W, KB = DP / 32, COLS = DP / 8;
     constexpr int IT = 4 / W;   // a wave's rows of tiles of the masked products
     const int lane = here() & 63, l = lane & 15, g = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    constexpr int MASK = (COLS < 8 ? COLS : 8) - 1;
-    const int by_step = g ^ (l & MASK), by_half = (g >> 1) ^ (l & MASK), by_column = g ^ ((l ^ (l >> 3)) & 7);
+    const int by_step = g ^ swap_of<COLS>(l), by_half = (g >> 1) ^ swap_of<COLS>(l);
     const int in_a = g ^ (l & 7), half_in_a = (g >> 1) ^ (l & 7);
-    if constexpr (!STATE) {
-        // the products under the mask: this wave's steps i against all j, one column i a lane
-        f32x4_t A[IT][4];
-        const int it0 = w * IT;
+    // the products under the mask: this wave's steps i against all j, one column i a lane
+    f32x4_t A[IT][4];
+    const int it0 = w * IT;
 #pragma unroll
-        for (int q = 0; q < IT; ++q) {
-            const int it = it0 + q;
+    for (int q = 0; q < IT; ++q) {
+        const int it = it0 + q;
 #pragma unroll
-            for (int jt = 0; jt < 4; ++jt) A[q][jt] = f32x4_t{0, 0, 0, 0};
+        for (int jt = 0; jt < 4; ++jt) A[q][jt] = f32x4_t{0, 0, 0, 0};
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
-                const bf16x8_t b = *reinterpret_cast<const bf16x8_t*>(at<COLS>(s.x, 16 * it + l, 4 * kb, by_step));
+        for (int kb = 0; kb < KB; ++kb) {
+            const bf16x8_t b = *reinterpret_cast<const bf16x8_t*>(at<COLS>(s.x, 16 * it + l, 4 * kb, by_step));
 #pragma unroll
-                for (int jt = 0; jt < 4; ++jt)
-                    if (a.back ? jt >= it : jt <= it)
-                        A[q][jt] = mfma(*reinterpret_cast<const bf16x8_t*>(at<COLS>(s.y, 16 * jt + l, 4 * kb, by_step)), b, A[q][jt]);
-            }
-#pragma unroll
-            for (int jt = 0; jt < 4; ++jt)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int d = (16 * it + l) - (16 * jt + 4 * g + r), dist = a.back ? -d : d;
-                    A[q][jt][r] = dist >= 0 ? A[q][jt][r] * s.powers[dist] : 0.0f;
-                }
+            for (int jt = 0; jt < 4; ++jt)   // all of them: branches would cost more than the masked tiles
+                A[q][jt] = mfma(*reinterpret_cast<const bf16x8_t*>(at<COLS>(s.y, 16 * jt + l, 4 * kb, by_step)), b, A[q][jt]);
         }
-        __syncthreads();   // y by steps has been read
 #pragma unroll
-        for (int q = 0; q < IT; ++q)
+        for (int jt = 0; jt < 4; ++jt)
 #pragma unroll
-            for (int jt = 0; jt < 4; ++jt) {
-                u32x2_t hi, lo;
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    uint32_t h, o;
-                    parts(f32x2_t{A[q][jt][2 * r], A[q][jt][2 * r + 1]}, h, o);
-                    hi[r] = h;
-                    lo[r] = o;
-                }
-                const int i = 16 * (it0 + q) + l;
-                __bf16* to = at<8>(s.y + 4 * (g & 1), i, 2 * jt, half_in_a);
-                *reinterpret_cast<u32x2_t*>(to) = hi;
-                *reinterpret_cast<u32x2_t*>(to + 64 * 64) = lo;
+            for (int r = 0; r < 4; ++r) {
+                const int d = (16 * it + l) - (16 * jt + 4 * g + r), dist = a.back ? -d : d;
+                const float f = s.powers[max(dist, 0)];
+                A[q][jt][r] *= dist >= 0 ? f : 0.0f;
             }
-        __syncthreads();
     }
+    // through the state
+    f32x4_t O[4][RT];
+#pragma unroll
+    for (int it = 0; it < 4; ++it)
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) O[it][rt] = f32x4_t{0, 0, 0, 0};
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+        bf16x8_t hi[RT], lo[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            u32x4_t h4, l4;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                uint32_t h, o;
+                parts(f32x2_t{M[2 * kb + e / 2][rt][2 * e % 4], M[2 * kb + e / 2][rt][2 * e % 4 + 1]}, h, o);
+                h4[e] = h;
+                l4[e] = o;
+            }
+            hi[rt] = __builtin_bit_cast(bf16x8_t, h4);
+            lo[rt] = __builtin_bit_cast(bf16x8_t, l4);
+        }
+        bf16x8_t x[4];
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+            // rows of M in the order in which a lane holds them
+            x[it] = join(*reinterpret_cast<const bf16x4_t*>(at<COLS>(s.x + 4 * (g & 1), 16 * it + l, 4 * kb, by_half)),
+                                    *reinterpret_cast<const bf16x4_t*>(at<COLS>(s.x + 4 * (g & 1), 16 * it + l, 4 * kb + 2, by_half)));
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) O[it][rt] = mfma(lo[rt], x[it], O[it][rt]);
+        }
+#pragma unroll
+        for (int it = 0; it < 4; ++it)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) O[it][rt] = mfma(hi[rt], x[it], O[it][rt]);
+    }
+    __syncthreads();   // x has been read
+#pragma unroll
+    for (int q = 0; q < IT; ++q)
+#pragma unroll
+        for (int jt = 0; jt < 4; ++jt) {
+            u32x2_t hi, lo;
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                uint32_t h, o;
+                parts(f32x2_t{A[q][jt][2 * r], A[q][jt][2 * r + 1]}, h, o);
+                hi[r] = h;
+                lo[r] = o;
+            }
+            __bf16* to = in_square(s.x + 4 * (g & 1), 16 * (it0 + q) + l, 2 * jt, half_in_a);
+            *reinterpret_cast<u32x2_t*>(to) = hi;
+            *reinterpret_cast<u32x2_t*>(to + 64 * 64) = lo;
+        }
+    __syncthreads();
+    Columns c;
+    c.init<COLS>(l, g);
     bf16x8_t z[2][RT];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-            z[kb][rt] = *reinterpret_cast<const bf16x8_t*>(at<8>(s.zt, 16 * (w * RT + rt) + l, 4 * kb ^ 2 * rt, by_column ^ (2 * RT * w & 7)));
-    if constexpr (!STATE) {
-        f32x4_t O[4][RT];
+        for (int rt = 0; rt < RT; ++rt) z[kb][rt] = columns<COLS>(s.z, c, w * RT + rt, kb);
 #pragma unroll
-        for (int it = 0; it < 4; ++it)
+    for (int it = 0; it < 4; ++it) {
+        const int e = a.back ? n - 1 - (16 * it + l) : 16 * it + l + 1;
+        const float f = s.powers[e < 0 ? 0 : e];   // a row that is not there is all zeros
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) O[it][rt] = f32x4_t{0, 0, 0, 0};
+        for (int rt = 0; rt < RT; ++rt) O[it][rt] *= f;
+    }
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
-            bf16x8_t hi[RT], lo[RT];
+    for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                u32x4_t h4, l4;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    uint32_t h, o;
-                    parts(f32x2_t{M[2 * kb + e / 2][rt][2 * e % 4], M[2 * kb + e / 2][rt][2 * e % 4 + 1]}, h, o);
-                    h4[e] = h;
-                    l4[e] = o;
-                }
-                hi[rt] = __builtin_bit_cast(bf16x8_t, h4);
-                lo[rt] = __builtin_bit_cast(bf16x8_t, l4);
-            }
+        for (int part = 1; part >= 0; --part)
 #pragma unroll
             for (int it = 0; it < 4; ++it) {
-                // rows of M in the order in which a lane holds them
-                const bf16x8_t x = join(*reinterpret_cast<const bf16x4_t*>(at<COLS>(s.x + 4 * (g & 1), 16 * it + l, 4 * kb, by_half)),
-                                        *reinterpret_cast<const bf16x4_t*>(at<COLS>(s.x + 4 * (g & 1), 16 * it + l, 4 * kb + 2, by_half)));
+                const bf16x8_t A8 = *reinterpret_cast<const bf16x8_t*>(in_square(s.x + part * 64 * 64, 16 * it + l, 4 * kb, in_a));
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) O[it][rt] = mfma(lo[rt], x, mfma(hi[rt], x, O[it][rt]));
+                for (int rt = 0; rt < RT; ++rt) O[it][rt] = mfma(z[kb][rt], A8, O[it][rt]);
             }
-        }
-#pragma unroll
-        for (int it = 0; it < 4; ++it) {
-            const int i = 16 * it + l, e = a.back ? n - 1 - i : i + 1;
-            const float f = s.powers[e < 0 ? 0 : e];   // a row that is not there is all zeros
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) O[it][rt] *= f;
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-                if (a.back ? kb == 1 || it <= 1 : kb == 0 || it >= 2) {
-                    const bf16x8_t hi = *reinterpret_cast<const bf16x8_t*>(at<8>(s.y, i, 4 * kb, in_a));
-                    const bf16x8_t lo = *reinterpret_cast<const bf16x8_t*>(at<8>(s.y + 64 * 64, i, 4 * kb, in_a));
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) O[it][rt] = mfma(z[kb][rt], lo, mfma(z[kb][rt], hi, O[it][rt]));
-                }
-            if (i < n)
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
-                    put_four<__bf16, WHOLE>(out + i * a.ldo, 16 * (w * RT + rt) + 4 * g, a.R, O[it][rt]);
-        }
+    if constexpr (!WHOLE) {
+        put_rows<__bf16, 4, RT, false>(out, a, n, 16 * w * RT + 4 * g, l, O);
+        return;
     }
-    // the state
+    // a wave's columns go through LDS into pieces of 16 bytes: stores of 8 bytes, 32 of a row, took a third of
+    // the whole pass (1 x 32768 x 16 heads of 128: XXX)
+    __bf16* mine = s.out + w * 64 * 16 * RT;
+#pragma unroll
+    for (int it = 0; it < 4; ++it)
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            const f32x4_t v = O[it][rt];
+            const u32x2_t e = {pack(f32x2_t{v[0], v[1]}), pack(f32x2_t{v[2], v[3]})};
+            const int row = 16 * it + l, piece = (2 * rt + (g >> 1)) ^ ((l >> 2) & (2 * RT - 1));
+            *reinterpret_cast<u32x2_t*>(mine + (row * 2 * RT + piece) * 8 + 4 * (g & 1)) = e;
+        }
+    constexpr int PER = 2 * RT;   // pieces of a row
+    const uint32_t row_bytes = (uint32_t)a.ldo * 2u;
+    const auto rows = __builtin_amdgcn_make_buffer_rsrc(out, 0, (int)(n * row_bytes), 0x00027000);
+    const int k = lane & (PER - 1), r0 = lane / PER, cc = 16 * w * RT + 8 * k;
+    const uint32_t to = cc < a.R ? (uint32_t)r0 * row_bytes + (uint32_t)cc * 2u : NOWHERE;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        const int row = r0 + j * (64 / PER);
+        const u32x4_t v = *reinterpret_cast<const u32x4_t*>(mine + (row * PER + (k ^ ((row >> 2) & (PER - 1)))) * 8);
+        __builtin_amdgcn_raw_buffer_store_b128(v, rows, to + (uint32_t)(j * (64 / PER)) * row_bytes, 0, 0);
+    }
+}
+
+// The same chunk: the state after it.
+template <int DP, bool STATE>
+__device__ inline void carry(LdsBf16<DP, STATE>& s, const Pass& a, f32x4_t (&M)[DP / 16][DP / 16 / Chunk<__bf16>::waves(DP)], int n) {
+    constexpr int W = Chunk<__bf16>::waves(DP), RT = DP / 16 / W, PT = DP / 16, COLS = DP / 8;
+    const int lane = here() & 63, l = lane & 15, g = lane >> 4;
+    const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    Columns c;
+    c.init<COLS>(l, g);
     const float keep = s.powers[n];
 #pragma unroll
     for (int pt = 0; pt < PT; ++pt)
@@ -376,7 +438,7 @@ __device__ inline void work(LdsBf16<DP, STATE>& s, const Pass& a, f32x4_t (&M)[D
         }
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            const u32x4_t zz = __builtin_bit_cast(u32x4_t, z[kb][rt]);
+            const u32x4_t zz = __builtin_bit_cast(u32x4_t, columns<COLS>(s.z, c, w * RT + rt, kb));
             u32x4_t p1, p2, p3;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -392,12 +454,22 @@ __device__ inline void work(LdsBf16<DP, STATE>& s, const Pass& a, f32x4_t (&M)[D
             z2[rt] = __builtin_bit_cast(bf16x8_t, p2);
             z3[rt] = __builtin_bit_cast(bf16x8_t, p3);
         }
+        // the three parts one after another: a product waits for the one before in its sum
+        bf16x8_t y[PT];
 #pragma unroll
         for (int pt = 0; pt < PT; ++pt) {
-            const bf16x8_t y = *reinterpret_cast<const bf16x8_t*>(at<8>(s.yt, 16 * pt + l, 4 * kb ^ (2 * pt & 7), by_column));
+            y[pt] = columns<COLS>(s.y, c, pt, kb);
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) M[pt][rt] = mfma(y, z1[rt], mfma(y, z2[rt], mfma(y, z3[rt], M[pt][rt])));
+            for (int rt = 0; rt < RT; ++rt) M[pt][rt] = mfma(y[pt], z3[rt], M[pt][rt]);
         }
+#pragma unroll
+        for (int pt = 0; pt < PT; ++pt)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) M[pt][rt] = mfma(y[pt], z2[rt], M[pt][rt]);
+#pragma unroll
+        for (int pt = 0; pt < PT; ++pt)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) M[pt][rt] = mfma(y[pt], z1[rt], M[pt][rt]);
     }
 }
 
@@ -428,35 +500,37 @@ __device__ inline void put_chunk(LdsF32<DP, STATE>& s, const Stage<float, DP, ST
 
 __device__ inline f32x4_t mfma(float a, float b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
-template <int DP, bool STATE, bool WHOLE>
-__device__ inline void work(LdsF32<DP, STATE>& s, const Pass& a, f32x4_t (&M)[DP / 16][DP / 16 / Chunk<float>::waves(DP)], int n,
+template <int DP, bool WHOLE>
+__device__ inline void give(LdsF32<DP, false>& s, const Pass& a, const f32x4_t (&M)[DP / 16][DP / 16 / Chunk<float>::waves(DP)], int n,
                             float* out) {
-    constexpr int W = Chunk<float>::waves(DP), RT = DP / 16 / W, PT = DP / 16, LD = LdsF32<DP, STATE>::LD;
+    constexpr int W = Chunk<float>::waves(DP), RT = DP / 16 / W, PT = DP / 16, LD = LdsF32<DP, false>::LD;
     const int lane = here() & 63, l = lane & 15, g = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    if constexpr (!STATE) {
 #pragma unroll
-        for (int pair = 0; pair < 4; ++pair) {
-            if (pair % W != w) continue;
-            const int it = pair >> 1, jt = pair & 1;
-            f32x4_t A = {0, 0, 0, 0};
-            if (a.back ? jt >= it : jt <= it)
+    for (int pair = 0; pair < 4; ++pair) {
+        if (pair % W != w) continue;
+        const int it = pair >> 1, jt = pair & 1;
+        f32x4_t A = {0, 0, 0, 0}, A2 = {0, 0, 0, 0};   // two, since a product waits for the one before in its sum
 #pragma unroll
-                for (int pt = 0; pt < PT; ++pt) {
-                    const f32x4_t y = *reinterpret_cast<const f32x4_t*>(s.y + (16 * jt + l) * LD + 16 * pt + 4 * g);
-                    const f32x4_t x = *reinterpret_cast<const f32x4_t*>(s.x + (16 * it + l) * LD + 16 * pt + 4 * g);
+        for (int pt = 0; pt < PT; ++pt) {
+            const f32x4_t y = *reinterpret_cast<const f32x4_t*>(s.y + (16 * jt + l) * LD + 16 * pt + 4 * g);
+            const f32x4_t x = *reinterpret_cast<const f32x4_t*>(s.x + (16 * it + l) * LD + 16 * pt + 4 * g);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) A = mfma(y[r], x[r], A);
-                }
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int d = (16 * it + l) - (16 * jt + 4 * g + r), dist = a.back ? -d : d;
-                A[r] = dist >= 0 ? A[r] * s.powers[dist] : 0.0f;
+            for (int r = 0; r < 4; r += 2) {
+                A = mfma(y[r], x[r], A);
+                A2 = mfma(y[r + 1], x[r + 1], A2);
             }
-            *reinterpret_cast<f32x4_t*>(s.a + (16 * it + l) * 36 + 16 * jt + 4 * g) = A;
         }
-        __syncthreads();
+        A += A2;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int d = (16 * it + l) - (16 * jt + 4 * g + r), dist = a.back ? -d : d;
+            const float f = s.powers[max(dist, 0)];
+            A[r] *= dist >= 0 ? f : 0.0f;
+        }
+        *reinterpret_cast<f32x4_t*>(s.a + (16 * it + l) * 36 + 16 * jt + 4 * g) = A;
     }
+    __syncthreads();
     float z[2][RT][4];
 #pragma unroll
     for (int jt = 0; jt < 2; ++jt)
@@ -464,39 +538,56 @@ __device__ inline void work(LdsF32<DP, STATE>& s, const Pass& a, f32x4_t (&M)[DP
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
             for (int r = 0; r < 4; ++r) z[jt][rt][r] = s.z[(16 * jt + 4 * g + r) * LD + 16 * (w * RT + rt) + l];
-    if constexpr (!STATE) {
+    f32x4_t O[2][RT];
 #pragma unroll
-        for (int it = 0; it < 2; ++it) {
-            f32x4_t O[RT];
+    for (int it = 0; it < 2; ++it)
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) O[rt] = f32x4_t{0, 0, 0, 0};
+        for (int rt = 0; rt < RT; ++rt) O[it][rt] = f32x4_t{0, 0, 0, 0};
 #pragma unroll
-            for (int pt = 0; pt < PT; ++pt) {
-                const f32x4_t x = *reinterpret_cast<const f32x4_t*>(s.x + (16 * it + l) * LD + 16 * pt + 4 * g);
+    for (int pt = 0; pt < PT; ++pt) {
+        f32x4_t x[2];
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
+        for (int it = 0; it < 2; ++it) x[it] = *reinterpret_cast<const f32x4_t*>(s.x + (16 * it + l) * LD + 16 * pt + 4 * g);
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) O[rt] = mfma(M[pt][rt][r], x[r], O[rt]);
-            }
-            const int i = 16 * it + l, e = a.back ? n - 1 - i : i + 1;
-            const float f = s.powers[e < 0 ? 0 : e];
+        for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) O[rt] *= f;
+            for (int it = 0; it < 2; ++it)
 #pragma unroll
-            for (int jt = 0; jt < 2; ++jt)
-                if (a.back ? jt >= it : jt <= it) {
-                    const f32x4_t A = *reinterpret_cast<const f32x4_t*>(s.a + i * 36 + 16 * jt + 4 * g);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-#pragma unroll
-                        for (int rt = 0; rt < RT; ++rt) O[rt] = mfma(z[jt][rt][r], A[r], O[rt]);
-                }
-            if (i < n)
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
-                    put_four<float, WHOLE>(out + i * a.ldo, 16 * (w * RT + rt) + 4 * g, a.R, O[rt]);
-        }
+                for (int rt = 0; rt < RT; ++rt) O[it][rt] = mfma(M[pt][rt][r], x[it][r], O[it][rt]);
     }
+    f32x4_t A[2][2];
+#pragma unroll
+    for (int it = 0; it < 2; ++it) {
+        const int i = 16 * it + l, e = a.back ? n - 1 - i : i + 1;
+        const float f = s.powers[e < 0 ? 0 : e];   // a row that is not there is all zeros
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) O[it][rt] *= f;
+#pragma unroll
+        for (int jt = 0; jt < 2; ++jt) A[it][jt] = *reinterpret_cast<const f32x4_t*>(s.a + i * 36 + 16 * jt + 4 * g);
+    }
+#pragma unroll
+    for (int jt = 0; jt < 2; ++jt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int it = 0; it < 2; ++it)
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) O[it][rt] = mfma(z[jt][rt][r], A[it][jt][r], O[it][rt]);
+    put_rows<float, 2, RT, WHOLE>(out, a, n, 16 * w * RT + 4 * g, l, O);
+}
+
+template <int DP, bool STATE>
+__device__ inline void carry(LdsF32<DP, STATE>& s, const Pass& a, f32x4_t (&M)[DP / 16][DP / 16 / Chunk<float>::waves(DP)], int n) {
+    constexpr int W = Chunk<float>::waves(DP), RT = DP / 16 / W, PT = DP / 16, LD = LdsF32<DP, STATE>::LD;
+    const int lane = here() & 63, l = lane & 15, g = lane >> 4;
+    const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    float z[2][RT][4];
+#pragma unroll
+    for (int jt = 0; jt < 2; ++jt)
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) z[jt][rt][r] = s.z[(16 * jt + 4 * g + r) * LD + 16 * (w * RT + rt) + l];
     const float keep = s.powers[n];
 #pragma unroll
     for (int pt = 0; pt < PT; ++pt)
@@ -596,8 +687,10 @@ __global__ void __launch_bounds__(64 * Chunk<E>::waves(DP), Chunk<E>::per_unit(D
         stage.settle(a);
         put_chunk(s, stage);
         __syncthreads();
-        if (c + 1 < chunks) fetch_chunk(c + 1);
-        work<DP, STATE, MODE == PIECES>(s, a, M, min(C, len - k), out + k * a.ldo);
+        const int n = min(C, len - k);
+        if constexpr (!STATE) give<DP, MODE == PIECES>(s, a, M, n, out + k * a.ldo);
+        if (c + 1 < chunks) fetch_chunk(c + 1);   // (here, where few registers are in use)
+        carry<DP, STATE>(s, a, M, n);
         __syncthreads();
     }
 
