@@ -202,6 +202,30 @@ __device__ inline void put_rows(E* out, const Pass& a, int n, int c, int l, cons
     }
 }
 
+// A lane's decays under the mask, of its wave's tiles of the masked products (one column i a lane,
+// four rows j in a register each): a^|i-j| where j is not later than i in the pass's direction, else 0.
+template <class E, int DP>
+struct Mask {
+    static constexpr int W = Chunk<E>::waves(DP), C = Chunk<E>::C;
+    static constexpr int IT = C == 64 ? 4 / W : (4 + W - 1) / W, JT = C == 64 ? 4 : 1;
+    f32x4_t f[IT][JT];
+    __device__ void init(const float* powers, bool back, int w, int l, int g) {
+#pragma unroll
+        for (int q = 0; q < IT; ++q)
+#pragma unroll
+            for (int j = 0; j < JT; ++j) {
+                // fp32: tile (pair / 2, pair % 2) of pairs w, w + W, ...
+                const int pair = (w + q * W) & 3, it = C == 64 ? w * IT + q : pair >> 1, jt = C == 64 ? j : pair & 1;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int d = (16 * it + l) - (16 * jt + 4 * g + r), dist = back ? -d : d;
+                    const float x = powers[max(dist, 0)];
+                    f[q][j][r] = dist >= 0 ? x : 0.0f;
+                }
+            }
+    }
+};
+
 // --- bf16 ------------------------------------------------------------------
 
 // LDS holds the chunk's rows by steps, each in 16-byte pieces whose places are exchanged within the row: piece k
@@ -225,7 +249,7 @@ struct LdsBf16 {
     __bf16 y[64 * DP];
     __bf16 z[64 * DP];
     __bf16 out[STATE ? 8 : 64 * DP];
-    float powers[TABLE + 3];
+    float of_x[64], of_z[64];   // what a step's product with the state, and what it adds to the state, decay by
 };
 
 template <int DP, bool STATE, int MODE>
@@ -276,7 +300,7 @@ __device__ inline bf16x8_t columns(__bf16* base, const Columns& c, int ct, int k
 // One chunk of n steps, out at its first step: what it gives.
 template <int DP, bool WHOLE>
 __device__ inline void give(LdsBf16<DP, false>& s, const Pass& a, const f32x4_t (&M)[DP / 16][DP / 16 / Chunk<__bf16>::waves(DP)],
-                            int n, __bf16* out) {
+                            const Mask<__bf16, DP>& mask, int n, __bf16* out) {
     constexpr int W = Chunk<__bf16>::waves(DP), RT = DP / 16 / W, KB = DP / 32, COLS = DP / 8;
     constexpr int IT = 4 / W;   // a wave's rows of tiles of the masked products
     const int lane = here() & 63, l = lane & 15, g = lane >> 4;
@@ -299,14 +323,9 @@ __device__ inline void give(LdsBf16<DP, false>& s, const Pass& a, const f32x4_t 
                 A[q][jt] = mfma(*reinterpret_cast<const bf16x8_t*>(at<COLS>(s.y, 16 * jt + l, 4 * kb, by_step)), b, A[q][jt]);
         }
 #pragma unroll
-        for (int jt = 0; jt < 4; ++jt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int d = (16 * it + l) - (16 * jt + 4 * g + r), dist = a.back ? -d : d;
-                const float f = s.powers[max(dist, 0)];
-                A[q][jt][r] *= dist >= 0 ? f : 0.0f;
-            }
+        for (int jt = 0; jt < 4; ++jt) A[q][jt] *= mask.f[q][jt];
     }
+    __builtin_amdgcn_sched_barrier(0);
     // through the state
     f32x4_t O[4][RT];
 #pragma unroll
@@ -342,6 +361,7 @@ __device__ inline void give(LdsBf16<DP, false>& s, const Pass& a, const f32x4_t 
         for (int it = 0; it < 4; ++it)
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) O[it][rt] = mfma(hi[rt], x[it], O[it][rt]);
+        __builtin_amdgcn_sched_barrier(0);   // (what is fetched early takes registers that are short)
     }
     __syncthreads();   // x has been read
 #pragma unroll
@@ -370,8 +390,7 @@ __device__ inline void give(LdsBf16<DP, false>& s, const Pass& a, const f32x4_t 
         for (int rt = 0; rt < RT; ++rt) z[kb][rt] = columns<COLS>(s.z, c, w * RT + rt, kb);
 #pragma unroll
     for (int it = 0; it < 4; ++it) {
-        const int e = a.back ? n - 1 - (16 * it + l) : 16 * it + l + 1;
-        const float f = s.powers[e < 0 ? 0 : e];   // a row that is not there is all zeros
+        const float f = s.of_x[16 * it + l];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) O[it][rt] *= f;
     }
@@ -416,13 +435,12 @@ __device__ inline void give(LdsBf16<DP, false>& s, const Pass& a, const f32x4_t 
 
 // The same chunk: the state after it.
 template <int DP, bool STATE>
-__device__ inline void carry(LdsBf16<DP, STATE>& s, const Pass& a, f32x4_t (&M)[DP / 16][DP / 16 / Chunk<__bf16>::waves(DP)], int n) {
+__device__ inline void carry(LdsBf16<DP, STATE>& s, const Pass& a, f32x4_t (&M)[DP / 16][DP / 16 / Chunk<__bf16>::waves(DP)], float keep) {
     constexpr int W = Chunk<__bf16>::waves(DP), RT = DP / 16 / W, PT = DP / 16, COLS = DP / 8;
     const int lane = here() & 63, l = lane & 15, g = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     Columns c;
     c.init<COLS>(l, g);
-    const float keep = s.powers[n];
 #pragma unroll
     for (int pt = 0; pt < PT; ++pt)
 #pragma unroll
@@ -430,12 +448,9 @@ __device__ inline void carry(LdsBf16<DP, STATE>& s, const Pass& a, f32x4_t (&M)[
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
         bf16x8_t z1[RT], z2[RT], z3[RT];
-        float f[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int j = 32 * kb + 8 * g + e, d = a.back ? j + 1 : n - 1 - j;
-            f[e] = s.powers[d < 0 ? 0 : d];
-        }
+        const f32x4_t f0 = *reinterpret_cast<const f32x4_t*>(s.of_z + 32 * kb + 8 * g);
+        const f32x4_t f1 = *reinterpret_cast<const f32x4_t*>(s.of_z + 32 * kb + 8 * g + 4);
+        const float f[8] = {f0[0], f0[1], f0[2], f0[3], f1[0], f1[1], f1[2], f1[3]};
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             const u32x4_t zz = __builtin_bit_cast(u32x4_t, columns<COLS>(s.z, c, w * RT + rt, kb));
@@ -482,7 +497,7 @@ struct LdsF32 {
     float y[32 * LD];
     float z[32 * LD];
     float a[STATE ? 4 : 32 * 36];
-    float powers[TABLE + 3];
+    float of_x[32], of_z[32];
 };
 
 template <int DP, bool STATE, int MODE>
@@ -501,8 +516,8 @@ __device__ inline void put_chunk(LdsF32<DP, STATE>& s, const Stage<float, DP, ST
 __device__ inline f32x4_t mfma(float a, float b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
 template <int DP, bool WHOLE>
-__device__ inline void give(LdsF32<DP, false>& s, const Pass& a, const f32x4_t (&M)[DP / 16][DP / 16 / Chunk<float>::waves(DP)], int n,
-                            float* out) {
+__device__ inline void give(LdsF32<DP, false>& s, const Pass& a, const f32x4_t (&M)[DP / 16][DP / 16 / Chunk<float>::waves(DP)],
+                            const Mask<float, DP>& mask, int n, float* out) {
     constexpr int W = Chunk<float>::waves(DP), RT = DP / 16 / W, PT = DP / 16, LD = LdsF32<DP, false>::LD;
     const int lane = here() & 63, l = lane & 15, g = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -522,12 +537,7 @@ __device__ inline void give(LdsF32<DP, false>& s, const Pass& a, const f32x4_t (
             }
         }
         A += A2;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int d = (16 * it + l) - (16 * jt + 4 * g + r), dist = a.back ? -d : d;
-            const float f = s.powers[max(dist, 0)];
-            A[r] *= dist >= 0 ? f : 0.0f;
-        }
+        A *= mask.f[pair / W][0];
         *reinterpret_cast<f32x4_t*>(s.a + (16 * it + l) * 36 + 16 * jt + 4 * g) = A;
     }
     __syncthreads();
@@ -558,8 +568,8 @@ __device__ inline void give(LdsF32<DP, false>& s, const Pass& a, const f32x4_t (
     f32x4_t A[2][2];
 #pragma unroll
     for (int it = 0; it < 2; ++it) {
-        const int i = 16 * it + l, e = a.back ? n - 1 - i : i + 1;
-        const float f = s.powers[e < 0 ? 0 : e];   // a row that is not there is all zeros
+        const int i = 16 * it + l;
+        const float f = s.of_x[i];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) O[it][rt] *= f;
 #pragma unroll
@@ -577,7 +587,7 @@ __device__ inline void give(LdsF32<DP, false>& s, const Pass& a, const f32x4_t (
 }
 
 template <int DP, bool STATE>
-__device__ inline void carry(LdsF32<DP, STATE>& s, const Pass& a, f32x4_t (&M)[DP / 16][DP / 16 / Chunk<float>::waves(DP)], int n) {
+__device__ inline void carry(LdsF32<DP, STATE>& s, const Pass& a, f32x4_t (&M)[DP / 16][DP / 16 / Chunk<float>::waves(DP)], float keep) {
     constexpr int W = Chunk<float>::waves(DP), RT = DP / 16 / W, PT = DP / 16, LD = LdsF32<DP, STATE>::LD;
     const int lane = here() & 63, l = lane & 15, g = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -588,7 +598,6 @@ __device__ inline void carry(LdsF32<DP, STATE>& s, const Pass& a, f32x4_t (&M)[D
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
             for (int r = 0; r < 4; ++r) z[jt][rt][r] = s.z[(16 * jt + 4 * g + r) * LD + 16 * (w * RT + rt) + l];
-    const float keep = s.powers[n];
 #pragma unroll
     for (int pt = 0; pt < PT; ++pt)
 #pragma unroll
@@ -597,8 +606,8 @@ __device__ inline void carry(LdsF32<DP, STATE>& s, const Pass& a, f32x4_t (&M)[D
     for (int jt = 0; jt < 2; ++jt)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int j = 16 * jt + 4 * g + r, d = a.back ? j + 1 : n - 1 - j;
-            const float f = s.powers[d < 0 ? 0 : d];
+            const int j = 16 * jt + 4 * g + r;
+            const float f = s.of_z[j];
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) z[jt][rt][r] *= f;
 #pragma unroll
@@ -639,7 +648,14 @@ __global__ void __launch_bounds__(64 * Chunk<E>::waves(DP), Chunk<E>::per_unit(D
     // the last share has no successor going forward, the first none going back
     if (STATE && (len == 0 || share == (a.back ? 0 : p.shares - 1))) return;
 
-    for (int i = threadIdx.x; i <= C; i += 64 * W) s.powers[i] = p.powers[head * TABLE + i];
+    const float* powers = p.powers + head * TABLE;
+    // (a chunk of n steps: rows that are not there are zeros, whatever they decay by)
+    auto decays = [&](int n) {
+        for (int i = threadIdx.x; i < C; i += 64 * W) {
+            s.of_x[i] = powers[a.back ? max(n - 1 - i, 0) : i + 1];
+            s.of_z[i] = powers[a.back ? i + 1 : max(n - 1 - i, 0)];
+        }
+    };
     const long long step0 = (long long)b * p.T + t0;
     const E* px = static_cast<const E*>(a.x) + step0 * a.ldx + head * a.P;
     const E* py = static_cast<const E*>(a.y) + step0 * a.ldy + head * a.P;
@@ -682,15 +698,21 @@ __global__ void __launch_bounds__(64 * Chunk<E>::waves(DP), Chunk<E>::per_unit(D
         stage.get(px + k * a.ldx, py + k * a.ldy, pz + k * a.ldz, a, min(C, len - k));
     };
     if (chunks) fetch_chunk(0);
+    Mask<E, DP> mask;
+    if constexpr (!STATE) mask.init(powers, a.back, w, l, g);
+    const float keep = powers[C];
+    decays(C);
     for (int c = 0; c < chunks; ++c) {
         const int k = chunk_of(c) * C;
+        const int n = min(C, len - k);
+        // only the last chunk of a row may be shorter: the first that is gone through, or the last
+        if (n < C || (a.back && c == 1)) decays(n);
         stage.settle(a);
         put_chunk(s, stage);
         __syncthreads();
-        const int n = min(C, len - k);
-        if constexpr (!STATE) give<DP, MODE == PIECES>(s, a, M, n, out + k * a.ldo);
+        if constexpr (!STATE) give<DP, MODE == PIECES>(s, a, M, mask, n, out + k * a.ldo);
         if (c + 1 < chunks) fetch_chunk(c + 1);   // (here, where few registers are in use)
-        carry<DP, STATE>(s, a, M, n);
+        carry<DP, STATE>(s, a, M, n == C ? keep : powers[n]);
         __syncthreads();
     }
 
