@@ -73,11 +73,11 @@ __device__ inline void load_row(const E* p, int col, int step, int D, float* out
         }
     }
 }
-template <class E, int V, int NV>
+template <bool FAR, class E, int V, int NV>
 __device__ inline void store_row(E* p, int col, int step, int D, const float* in) {
 #pragma unroll
     for (int i = 0; i < NV; ++i)
-        if (col + i * step < D) store_vec<E, V>(p + col + i * step, in + i * V);
+        if (col + i * step < D) put<FAR, E, V>(p + col + i * step, in + i * V);
 }
 // Weight or bias; a missing one is `fill`.
 template <int V, int NV>
@@ -115,6 +115,8 @@ __device__ inline float normalise(float* x, int col, int step, int D, float eps,
     return r;
 }
 
+// FAR: the output goes past the caches.
+
 // Whether row r is one of a sequence's steps.
 __device__ inline bool row_on(const NormParams& a, int r, bool report) {
     if (!a.lengths) return true;
@@ -124,7 +126,7 @@ __device__ inline bool row_on(const NormParams& a, int r, bool report) {
 
 constexpr int threads_of(int W) { return W > 4 ? 64 * W : 256; }
 
-template <class E, int V, int NV, int W>
+template <class E, int V, int NV, int W, bool FAR>
 __global__ void __launch_bounds__(threads_of(W)) norm_kernel(NormParams a) {
     __shared__ float lds[1][16];
     constexpr int PER = threads_of(W) / 64 / W;  // rows of a workgroup at once
@@ -146,11 +148,11 @@ __global__ void __launch_bounds__(threads_of(W)) norm_kernel(NormParams a) {
 #pragma unroll
             for (int i = 0; i < V * NV; ++i) x[i] = x[i] * w[i] + b[i];
         }
-        store_row<E, V, NV>(out, col, step, a.D, x);
+        store_row<FAR, E, V, NV>(out, col, step, a.D, x);
     }
 }
 
-template <class E, class G, int V, int NV, int W>
+template <class E, class G, int V, int NV, int W, bool FAR>
 __global__ void __launch_bounds__(threads_of(W)) norm_back_kernel(NormParams a) {
     __shared__ float lds[2][16];
     constexpr int WAVES = threads_of(W) / 64, PER = WAVES / W;
@@ -186,7 +188,7 @@ __global__ void __launch_bounds__(threads_of(W)) norm_back_kernel(NormParams a) 
 #pragma unroll
             for (int i = 0; i < V * NV; ++i) g[i] = rs * (g[i] - m0 - x[i] * m1);
         }
-        store_row<G, V, NV>(out, col, step, a.D, g);
+        store_row<FAR, G, V, NV>(out, col, step, a.D, g);
     }
     // the workgroup's sums, wave by wave
     float* sums = a.sums + (size_t)blockIdx.x * 2 * a.D;
@@ -345,6 +347,10 @@ int by_shape(int D, int vec, F&& launch) {
     return pick(std::integral_constant<int, 1>());
 }
 
+// From 256 MB on, the size of the last cache, an output's reader finds it in memory in any case, and what the call reads
+// again stays (256 x 1000 x 1024, ragged: 206 us through the caches, 185 past them; the training step 606 and 592).
+inline bool is_far(const lstm_dyn_norm* h, int bytes) { return (long long)h->B * h->T * h->D * bytes >= 256LL << 20; }
+
 template <class E>
 int run_forward(lstm_dyn_norm* h, const NormParams& p) {
     const int vec = p.D % (16 / (int)sizeof(E)) == 0 ? 16 / (int)sizeof(E) : 1;
@@ -353,8 +359,9 @@ int run_forward(lstm_dyn_norm* h, const NormParams& p) {
         if constexpr (V == 1 || V == 16 / (int)sizeof(E)) {
             constexpr int PER = threads_of(W) / 64 / W;
             const long long groups = ((long long)p.rows + PER - 1) / PER, most = (long long)h->num_cus * (W > 4 ? 2 : 8);
-            hipLaunchKernelGGL((norm_kernel<E, V, NV, W>), dim3((unsigned)(groups < most ? groups : most)),
-                               dim3(threads_of(W)), 0, h->last_stream, p);
+            auto* k = is_far(h, (int)sizeof(E)) ? norm_kernel<E, V, NV, W, true> : norm_kernel<E, V, NV, W, false>;
+            hipLaunchKernelGGL(k, dim3((unsigned)(groups < most ? groups : most)), dim3(threads_of(W)), 0,
+                               h->last_stream, p);
         }
         return ops_launched(h);
     });
@@ -374,8 +381,8 @@ int run_backward(lstm_dyn_norm* h, const NormParams& p, float* d_weight, float* 
             if (most > MAX_GROUPS) most = MAX_GROUPS;
             const long long want = ((long long)p.rows + 4 * PER - 1) / (4 * PER);  // four rows and more each
             groups = (int)(want < most ? want : most);
-            hipLaunchKernelGGL((norm_back_kernel<E, G, V, NV, W>), dim3((unsigned)groups), dim3(threads_of(W)), 0,
-                               h->last_stream, p);
+            auto* k = is_far(h, (int)sizeof(G)) ? norm_back_kernel<E, G, V, NV, W, true> : norm_back_kernel<E, G, V, NV, W, false>;
+            hipLaunchKernelGGL(k, dim3((unsigned)groups), dim3(threads_of(W)), 0, h->last_stream, p);
         }
         return ops_launched(h);
     });

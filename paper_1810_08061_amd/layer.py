@@ -326,9 +326,17 @@ class GradClip(_Handle):
     def _grads(self, name, tensors, et):
         if len(tensors) != len(self.shapes):
             raise ValueError(f"{len(self.shapes)} of {name} are needed, got {len(tensors)}")
-        for t, s in zip(tensors, self.shapes):
+        addresses, device = [], self._device
+        for t, s in zip(tensors, self.shapes):      # (written out: lists are long, calls few microseconds)
+            try:
+                if t.dtype is et and t.shape == s and t.get_device() == device and t.is_contiguous():
+                    addresses.append(t.data_ptr())
+                    continue
+            except AttributeError:
+                pass
             self._check(name, t, et, s)
-        return self._pointers(*[t.data_ptr() for t in tensors])
+            addresses.append(t.data_ptr())
+        return self._pointers(*addresses)
 
     def _type(self, grads):
         torch = _t()
@@ -345,10 +353,13 @@ class GradClip(_Handle):
                 return self.norm(grads, grad_scale)
         grads = list(grads)
         et, code = self._type(grads)
-        g = self._grads("gradients", grads, et)
-        result = _t().empty((2,), dtype=_t().float32, device=grads[0].device)
+        return self._norm(self._grads("gradients", grads, et), code, grad_scale, grads[0].device)
+
+    def _norm(self, g, code, grad_scale, device):
+        torch = _t()
+        result = torch.empty((2,), dtype=torch.float32, device=device)
         _ok(ops._ready.lstm_dyn_clip_norm(self.handle, g, code, grad_scale, self.max_norm, result.data_ptr(),
-                                          _stream(result.device)), "lstm_dyn_clip_norm")
+                                          _stream(device)), "lstm_dyn_clip_norm")
         return result
 
     def clip(self, grads, grad_scale: float = 1.0, out=None, stream=None):
@@ -360,11 +371,10 @@ class GradClip(_Handle):
         et, code = self._type(grads)
         g = self._grads("gradients", grads, et)
         o = g if out is None else self._grads("out", list(out), et)
-        result = _t().empty((2,), dtype=_t().float32, device=grads[0].device)
-        stream = _stream(result.device)
-        _ok(ops._ready.lstm_dyn_clip_norm(self.handle, g, code, grad_scale, self.max_norm, result.data_ptr(), stream),
-            "lstm_dyn_clip_norm")
-        _ok(ops._ready.lstm_dyn_clip_apply(self.handle, g, code, result.data_ptr(), o, stream), "lstm_dyn_clip_apply")
+        device = grads[0].device
+        result = self._norm(g, code, grad_scale, device)
+        _ok(ops._ready.lstm_dyn_clip_apply(self.handle, g, code, result.data_ptr(), o, _stream(device)),
+            "lstm_dyn_clip_apply")
         return result
 
 

@@ -505,11 +505,13 @@ class AdamW(_Handle):
         for g, p in zip(grads, self.params):
             self._check("a gradient", g, et, p.shape)
         if clip is not None:
-            result = clip.norm(grads, grad_scale)
-            _ok(_ready.lstm_dyn_adamw_step_clipped(self.handle, self._pointers(*[g.data_ptr() for g in grads]),
-                                                   BF16 if et == torch.bfloat16 else F32, lr, self.betas[0],
-                                                   self.betas[1], self.eps, result.data_ptr(), self.steps_done + 1,
-                                                   _stream(grads[0].device)), "lstm_dyn_adamw_step_clipped")
+            if clip.shapes != [p.shape for p in self.params] or clip._device != self._device:
+                raise ValueError("clip must be over the parameters of this optimizer, on its device")
+            g, code, device = self._pointers(*[g.data_ptr() for g in grads]), BF16 if et == torch.bfloat16 else F32, grads[0].device
+            result = clip._norm(g, code, grad_scale, device)
+            _ok(_ready.lstm_dyn_adamw_step_clipped(self.handle, g, code, lr, self.betas[0], self.betas[1], self.eps,
+                                                   result.data_ptr(), self.steps_done + 1, _stream(device)),
+                "lstm_dyn_adamw_step_clipped")
             self.steps_done += 1
             return result
         _ok(_ready.lstm_dyn_adamw_step(self.handle, self._pointers(*[g.data_ptr() for g in grads]),
