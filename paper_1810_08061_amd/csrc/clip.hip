@@ -25,7 +25,7 @@ namespace {
 constexpr int CHUNK = 16384;  // elements per workgroup
 constexpr int GROUP = 256;    // tensors per launch
 constexpr int THREADS = 256;
-constexpr uint32_t FEW = 32;  // workgroups
+constexpr uint32_t FEW = THREADS;  // workgroups
 
 struct Piece {        // what a workgroup takes
     uint32_t tensor;
@@ -114,10 +114,10 @@ __global__ void __launch_bounds__(THREADS) clip_norm_kernel(ClipParams a, Reads 
         }
     }
     __syncthreads();
-    if (!last || threadIdx.x >= 64) return;
+    if (!last) return;
     double t = threadIdx.x < a.all
                    ? __hip_atomic_load(a.sums + threadIdx.x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
-    t = wave_sum(t);
+    t = group_sum<THREADS / 64>(t, lds);
     if (threadIdx.x == 0) {
         write_result(a, t);
         __hip_atomic_store(a.arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
