@@ -164,6 +164,8 @@ int lstm_dyn_check_sample_args(int N, int V, int dtype, const void* logits, cons
  *     d_out_S  [B][heads][Dk][Dv]             fp32, or NULL (zero)
  *     dz       as z                           dtype (written; zero at t >= L[b])
  *     dS0      [B][heads][Dk][Dv]             fp32 (written)
+ * Inside a chunk of 64 steps (32 with fp32 data) an infinity or a NaN in z or dy makes what comes before it in the
+ * chunk no number as well; with bf16 data a state beyond 3.39e38 makes y in its column no number.
  * No scale is put on q k: it belongs into the weights that q or k come from.
  * The backward needs no forward before it.  Sums go in an order that the sizes alone decide. */
 typedef struct lstm_dyn_attend lstm_dyn_attend_t;

@@ -226,6 +226,13 @@ struct Mask {
     }
 };
 
+// A tile under the mask: what it leaves out is zero even where the product was no finite number.
+__device__ inline f32x4_t masked(f32x4_t A, f32x4_t f) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) A[r] = f[r] != 0.0f ? A[r] * f[r] : 0.0f;
+    return A;
+}
+
 // --- bf16 ------------------------------------------------------------------
 
 // LDS holds the chunk's rows by steps, each in 16-byte pieces whose places are exchanged within the row: piece k
@@ -323,7 +330,7 @@ __device__ inline void give(LdsBf16<DP, false>& s, const Pass& a, const f32x4_t 
                 A[q][jt] = mfma(*reinterpret_cast<const bf16x8_t*>(at<COLS>(s.y, 16 * jt + l, 4 * kb, by_step)), b, A[q][jt]);
         }
 #pragma unroll
-        for (int jt = 0; jt < 4; ++jt) A[q][jt] *= mask.f[q][jt];
+        for (int jt = 0; jt < 4; ++jt) A[q][jt] = masked(A[q][jt], mask.f[q][jt]);
     }
     __builtin_amdgcn_sched_barrier(0);
     // through the state
@@ -537,7 +544,7 @@ __device__ inline void give(LdsF32<DP, false>& s, const Pass& a, const f32x4_t (
             }
         }
         A += A2;
-        A *= mask.f[pair / W][0];
+        A = masked(A, mask.f[pair / W][0]);
         *reinterpret_cast<f32x4_t*>(s.a + (16 * it + l) * 36 + 16 * jt + 4 * g) = A;
     }
     __syncthreads();
@@ -638,7 +645,9 @@ __global__ void __launch_bounds__(64 * Chunk<E>::waves(DP), Chunk<E>::per_unit(D
     const unsigned item = turn * 8u + blockIdx.x % 8u;
     if (item >= (unsigned)p.rows * (unsigned)p.shares) return;
     const Pass& a = p.pass[eight - turn * (unsigned)p.passes];
-    const int row = (int)scalar(item / (unsigned)p.shares), share = (int)(item - (unsigned)row * (unsigned)p.shares);
+    // (first shares first: of sequences of different lengths the later ones are empty, and a CU's groups, far
+    // apart in this order, are not all early ones)
+    const int share = (int)scalar(item / (unsigned)p.rows), row = (int)(item - (unsigned)share * (unsigned)p.rows);
     const int b = (int)scalar((unsigned)row / (unsigned)p.heads), head = row - b * p.heads;
     const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);

@@ -326,3 +326,21 @@ def test_replays_of_a_graph(dtype):
     del graph
     say(m.query(ld.ops.OPS_Q_WORKSPACE_BYTES))
     m.close(), other.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_products_under_the_mask_may_overflow(dtype):
+    """q of early steps and k of late ones, whose product no step forms, are far apart in size: it overflows, and
+    every result is finite."""
+    import torch
+    Dk, Dv, T = 16, 16, 60
+    r = np.random.default_rng(18)
+    s = _inputs(r, dtype, 1, T, 1, Dk, Dv)
+    s["z"][:, :30, :Dk] *= 1e20               # q
+    s["z"][:, 30:, Dk:2 * Dk] *= 1e20         # k
+    s["z"][:, 30:, :Dk] *= 1e-20
+    with ld.LinearAttention(1, 1, Dk, Dv, T, 0.9, dtype) as m:
+        y, S = m.forward(s["z"], None, s["S0"])
+        got = m.backward(s["z"], None, s["S0"], s["dy"], s["dS"])
+        torch.cuda.synchronize()
+        _compare(dict(got, y=y, S=S), s, [T], [0.9], Dk, Dv, dtype, tight=False)
