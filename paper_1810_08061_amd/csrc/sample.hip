@@ -44,7 +44,7 @@ struct RowLds {
     u64 segment[SEGMENTS];
     u64 part[16];
     float fpart[16];
-    u64 found, rest, total;
+    u64 found, rest;
     int range, count, first;
 };
 
@@ -120,38 +120,48 @@ struct Row {
     }
 };
 
-__device__ inline u64 wave_sum(u64 v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-    return v;
+// v of the lane that a row_shr or row_bcast names, zero where there is none.
+template <int CTRL, int ROWS>
+__device__ inline u64 moved(u64 v) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xf, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xf, false);
+    return (u64)hi << 32 | lo;
 }
 // The sum over the lanes up to this one.
 __device__ inline u64 wave_scan(u64 v) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const u64 w = __shfl_up(v, o);
-        if (lane >= o) v += w;
-    }
+    v += moved<0x111, 0xf>(v);   // row_shr 1, 2, 4, 8: within 16 lanes
+    v += moved<0x112, 0xf>(v);
+    v += moved<0x114, 0xf>(v);
+    v += moved<0x118, 0xf>(v);
+    v += moved<0x142, 0xa>(v);   // row_bcast 15 into rows 1 and 3, then 31 into rows 2 and 3
+    v += moved<0x143, 0xc>(v);
     return v;
 }
+__device__ inline u64 last_lane(u64 v) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, 63);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), 63);
+    return (u64)hi << 32 | lo;
+}
+__device__ inline u64 wave_sum(u64 v) { return last_lane(wave_scan(v)); }
 
-// The first of n sums (a power of two, at least the workgroup's threads) at which their running sum reaches `target`:
-// writes its index, what is left of the target before it and the sum of all.
-template <int THREADS, class G>
-__device__ inline void crossing(RowLds& s, int n, u64 target, G value) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, per = n / THREADS;
+// The first of n sums (a power of two, at least the workgroup's threads) at which their running sum reaches
+// aim(the sum of all): writes its index and what is left of the target before it.  Returns the sum of all.
+template <int THREADS, class A, class G>
+__device__ inline u64 crossing(RowLds& s, int n, A aim, G value) {
+    const int w = threadIdx.x >> 6, per = n / THREADS;
     u64 mine = 0;
     for (int i = 0; i < per; ++i) mine += value((int)threadIdx.x * per + i);
     const u64 up = wave_scan(mine);
-    if (lane == 63) s.part[w] = up;
+    if ((threadIdx.x & 63) == 63) s.part[w] = up;
     __syncthreads();
     u64 before = up - mine, all = 0;
+#pragma unroll
     for (int i = 0; i < THREADS / 64; ++i) {
-        if (i < w) before += s.part[i];
-        all += s.part[i];
+        const u64 p = s.part[i];
+        before += i < w ? p : 0;
+        all += p;
     }
-    if (threadIdx.x == 0) s.total = all;
+    const u64 target = aim(all);
     if (before < target && before + mine >= target) {
         for (int i = 0; i < per; ++i) {
             const u64 v = value((int)threadIdx.x * per + i);
@@ -164,6 +174,7 @@ __device__ inline void crossing(RowLds& s, int n, u64 target, G value) {
         }
     }
     __syncthreads();
+    return all;
 }
 
 // The shortest start, within `within` (ALL: it is all tokens), whose measure (the tokens' number, or with MASS
@@ -191,10 +202,9 @@ __device__ inline Start find_start(RowLds& s, const Row<E>& row, const Weigh& we
         }
     });
     __syncthreads();
-    crossing<THREADS>(s, BINS, 0, [&](int i) { return s.hist[i]; });  // the sum alone
-    const u64 all = s.total, target = aim(all);
+    u64 target = 0;
+    const u64 all = crossing<THREADS>(s, BINS, [&](u64 sum) { return target = aim(sum); }, [&](int i) { return s.hist[i]; });
     if (target >= all) return within;
-    crossing<THREADS>(s, BINS, target, [&](int i) { return s.hist[i]; });
     const int at = s.range;
     // f(x, key) of the range's tokens
     auto each = [&](auto f) {
@@ -263,7 +273,7 @@ __device__ inline Start find_start(RowLds& s, const Row<E>& row, const Weigh& we
             if (key >= lo && key <= hi) atomicAdd(&s.hist[(hi - key) >> shift], measure(x));
         });
         __syncthreads();
-        crossing<THREADS>(s, BINS, rest, [&](int i) { return s.hist[i]; });
+        crossing<THREADS>(s, BINS, [&](u64) { return rest; }, [&](int i) { return s.hist[i]; });
         rest = s.rest;
         const u64 top = hi - ((u64)s.range << shift), width = (1ull << shift) - 1;
         lo = top - lo > width ? top - width : lo;
@@ -290,9 +300,7 @@ __device__ inline void walk(RowLds& s, const Row<E>& row, W weight, A aim, F fou
         if (lane == 0) s.segment[g] = sum;
     }
     __syncthreads();
-    crossing<THREADS>(s, SEGMENTS, 0, [&](int i) { return s.segment[i]; });
-    const u64 all = s.total;
-    crossing<THREADS>(s, SEGMENTS, aim(all), [&](int i) { return s.segment[i]; });
+    const u64 all = crossing<THREADS>(s, SEGMENTS, aim, [&](int i) { return s.segment[i]; });
     if (wave != 0) return;
     u64 rest = s.rest;
     const int k0 = s.range * 64 * rounds;
@@ -320,7 +328,7 @@ __device__ inline void walk(RowLds& s, const Row<E>& row, W weight, A aim, F fou
                 before += w[j];
             }
         }
-        const u64 whole = __shfl(up, 63);
+        const u64 whole = last_lane(up);
         if (whole >= rest) break;
         rest -= whole;
     }

@@ -417,8 +417,7 @@ class TokenSample(_Handle):
                 setattr(f, name + "s", value.data_ptr())
             else:
                 setattr(f, name, value)
-        token = torch.empty((N,), dtype=torch.int32, device=logits.device)
-        logp = torch.empty((N,), dtype=torch.float32, device=logits.device)
+        token, logp = torch.empty_like(u, dtype=torch.int32), torch.empty_like(u)
         _ok(ops._ready.lstm_dyn_sample_step(self.handle, logits.data_ptr(), u.data_ptr(), self._filter_at,
                                             token.data_ptr(), logp.data_ptr(), _stream(logits.device)),
             "lstm_dyn_sample_step")
