@@ -654,8 +654,9 @@ __global__ void __launch_bounds__(64 * Chunk<E>::waves(DP), Chunk<E>::per_unit(D
     const int given = p.lengths[b * p.length_step], L = max(0, min(given, p.T));
     const int t0 = share * p.span, span = min(p.span, p.T - t0);
     const int len = max(0, min(L - t0, span));
+    const int used = max(1, (L + p.span - 1) / p.span);   // the row's shares; an empty row has its first
     // the last share has no successor going forward, the first none going back
-    if (STATE && (len == 0 || share == (a.back ? 0 : p.shares - 1))) return;
+    if (STATE && (share >= used || share == (a.back ? 0 : used - 1))) return;
 
     const float* powers = p.powers + head * TABLE;
     // (a chunk of n steps: rows that are not there are zeros, whatever they decay by)
@@ -673,8 +674,8 @@ __global__ void __launch_bounds__(64 * Chunk<E>::waves(DP), Chunk<E>::per_unit(D
 
     f32x4_t M[PT][RT];
     const int PR = a.P * a.R;
-    const float* start = p.shares > 1 ? a.share + ((long long)row * p.shares + share) * PR
-                                      : (a.start ? a.start + (long long)row * PR : nullptr);
+    const float* start = a.start ? a.start + (long long)row * PR : nullptr;   // of the share that is gone through first
+    if (share != (a.back ? used - 1 : 0)) start = share < used ? a.share + ((long long)row * p.shares + share) * PR : nullptr;
 #pragma unroll
     for (int pt = 0; pt < PT; ++pt)
 #pragma unroll
@@ -726,7 +727,7 @@ __global__ void __launch_bounds__(64 * Chunk<E>::waves(DP), Chunk<E>::per_unit(D
     }
 
     float* end = STATE ? a.share + ((long long)row * p.shares + share) * PR : a.end ? a.end + (long long)row * PR : nullptr;
-    if (!STATE && share != (a.back || L == 0 ? 0 : (L - 1) / p.span)) end = nullptr;
+    if (!STATE && share != (a.back ? 0 : used - 1)) end = nullptr;
     if (end) {
 #pragma unroll
         for (int pt = 0; pt < PT; ++pt)
@@ -748,31 +749,34 @@ __global__ void __launch_bounds__(64 * Chunk<E>::waves(DP), Chunk<E>::per_unit(D
     }
 }
 
-// The state every share starts from, in place of what it adds.
+// The states that a row's shares start from, but for the one that is gone through first: what share k adds
+// to the state lies in its place, and the start of the one that follows it takes its own.
 __global__ void __launch_bounds__(256) attend_join_kernel(AttendParams p) {
     const Pass& a = p.pass[blockIdx.z];
     const int row = blockIdx.y, PR = a.P * a.R, e = blockIdx.x * 256 + threadIdx.x;
     if (e >= PR) return;
     const int b = row / p.heads, head = row % p.heads;
     const int L = clamp_length(p.lengths[b * p.length_step], p.T, p.status, false);
+    const int used = (L + p.span - 1) / p.span;
+    if (used < 2) return;
     float* share = a.share + (long long)row * p.shares * PR + e;
     float state = a.start ? a.start[(long long)row * PR + e] : 0.0f;
+    // all shares are whole but for the last of the row
     const float whole = (float)power(p.log2a, head, p.span);
+    const float part = a.back ? (float)power(p.log2a, head, L - (used - 1) * p.span) : whole;
     constexpr int AT_ONCE = 8;   // fetched before the first is used
-    for (int i0 = 0; i0 < p.shares; i0 += AT_ONCE) {
-        float add[AT_ONCE];
+    auto place = [&](int i) { return share + (long long)(a.back ? used - 1 - i : i) * PR; };
+    float add = *place(0);
+    for (int i0 = 1; i0 < used; i0 += AT_ONCE) {
+        float next[AT_ONCE];   // (of the last share, whatever lies there: it is not used)
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) next[j] = *place(min(i0 + j, used - 1));
 #pragma unroll
         for (int j = 0; j < AT_ONCE; ++j) {
-            const int i = min(i0 + j, p.shares - 1), k = a.back ? p.shares - 1 - i : i;
-            add[j] = share[(long long)k * PR];
-        }
-#pragma unroll
-        for (int j = 0; j < AT_ONCE; ++j) {
-            const int i = i0 + j, k = a.back ? p.shares - 1 - i : i, len = max(0, min(L - k * p.span, p.span));
-            if (i >= p.shares) break;
-            share[(long long)k * PR] = state;
-            // (a share without steps has left nothing there, nor has the last one)
-            if (len) state = (len == p.span ? whole : (float)power(p.log2a, head, len)) * state + (i < p.shares - 1 ? add[j] : 0.0f);
+            if (i0 + j >= used) break;
+            state = (i0 + j == 1 ? part : whole) * state + add;
+            *place(i0 + j) = state;
+            add = next[j];
         }
     }
 }
