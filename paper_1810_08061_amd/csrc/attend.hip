@@ -256,7 +256,7 @@ struct LdsBf16 {
     __bf16 y[64 * DP];
     __bf16 z[64 * DP];
     __bf16 out[STATE ? 8 : 64 * DP];
-    float of_x[64], of_z[64];   // what a step's product with the state, and what it adds to the state, decay by
+    float of_x[64], of_z[64], of_state[4];   // what a step's product with the state, what it adds to the state, and the state decay by
 };
 
 template <int DP, bool STATE, int MODE>
@@ -442,12 +442,13 @@ __device__ inline void give(LdsBf16<DP, false>& s, const Pass& a, const f32x4_t 
 
 // The same chunk: the state after it.
 template <int DP, bool STATE>
-__device__ inline void carry(LdsBf16<DP, STATE>& s, const Pass& a, f32x4_t (&M)[DP / 16][DP / 16 / Chunk<__bf16>::waves(DP)], float keep) {
+__device__ inline void carry(LdsBf16<DP, STATE>& s, const Pass& a, f32x4_t (&M)[DP / 16][DP / 16 / Chunk<__bf16>::waves(DP)]) {
     constexpr int W = Chunk<__bf16>::waves(DP), RT = DP / 16 / W, PT = DP / 16, COLS = DP / 8;
     const int lane = here() & 63, l = lane & 15, g = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     Columns c;
     c.init<COLS>(l, g);
+    const float keep = s.of_state[0];
 #pragma unroll
     for (int pt = 0; pt < PT; ++pt)
 #pragma unroll
@@ -504,7 +505,7 @@ struct LdsF32 {
     float y[32 * LD];
     float z[32 * LD];
     float a[STATE ? 4 : 32 * 36];
-    float of_x[32], of_z[32];
+    float of_x[32], of_z[32], of_state[4];
 };
 
 template <int DP, bool STATE, int MODE>
@@ -594,7 +595,7 @@ __device__ inline void give(LdsF32<DP, false>& s, const Pass& a, const f32x4_t (
 }
 
 template <int DP, bool STATE>
-__device__ inline void carry(LdsF32<DP, STATE>& s, const Pass& a, f32x4_t (&M)[DP / 16][DP / 16 / Chunk<float>::waves(DP)], float keep) {
+__device__ inline void carry(LdsF32<DP, STATE>& s, const Pass& a, f32x4_t (&M)[DP / 16][DP / 16 / Chunk<float>::waves(DP)]) {
     constexpr int W = Chunk<float>::waves(DP), RT = DP / 16 / W, PT = DP / 16, LD = LdsF32<DP, STATE>::LD;
     const int lane = here() & 63, l = lane & 15, g = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -605,6 +606,7 @@ __device__ inline void carry(LdsF32<DP, STATE>& s, const Pass& a, f32x4_t (&M)[D
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
             for (int r = 0; r < 4; ++r) z[jt][rt][r] = s.z[(16 * jt + 4 * g + r) * LD + 16 * (w * RT + rt) + l];
+    const float keep = s.of_state[0];
 #pragma unroll
     for (int pt = 0; pt < PT; ++pt)
 #pragma unroll
@@ -665,6 +667,7 @@ __global__ void __launch_bounds__(64 * Chunk<E>::waves(DP), Chunk<E>::per_unit(D
             s.of_x[i] = powers[a.back ? max(n - 1 - i, 0) : i + 1];
             s.of_z[i] = powers[a.back ? i + 1 : max(n - 1 - i, 0)];
         }
+        if (threadIdx.x == 0) s.of_state[0] = powers[n];
     };
     const long long step0 = (long long)b * p.T + t0;
     const E* px = static_cast<const E*>(a.x) + step0 * a.ldx + head * a.P;
@@ -710,7 +713,6 @@ __global__ void __launch_bounds__(64 * Chunk<E>::waves(DP), Chunk<E>::per_unit(D
     if (chunks) fetch_chunk(0);
     Mask<E, DP> mask;
     if constexpr (!STATE) mask.init(powers, a.back, w, l, g);
-    const float keep = powers[C];
     decays(C);
     for (int c = 0; c < chunks; ++c) {
         const int k = chunk_of(c) * C;
@@ -722,7 +724,7 @@ __global__ void __launch_bounds__(64 * Chunk<E>::waves(DP), Chunk<E>::per_unit(D
         __syncthreads();
         if constexpr (!STATE) give<DP, MODE == PIECES>(s, a, M, mask, n, out + k * a.ldo);
         if (c + 1 < chunks) fetch_chunk(c + 1);   // (here, where few registers are in use)
-        carry<DP, STATE>(s, a, M, n == C ? keep : powers[n]);
+        carry<DP, STATE>(s, a, M);   // (and nothing else is fetched from memory: it would wait for all of the chunk)
         __syncthreads();
     }
 
