@@ -64,10 +64,10 @@ __device__ inline float clean(float x) { return fmaxf(x, -__builtin_inff()); }
 // exp((x - largest) / T): 1 / (T ln 2) is held in two parts, so its rounding does not
 // tilt the weights of tokens far from the largest.
 struct Weigh {
-    float largest, hi, lo, unit, none;
+    float largest, hi, lo, unit, none, per_range;
     // How far below the largest x is, in ranges of the histogram.  From `none` on there is no weight, nearer
     // p rounds to a multiple of 1 / unit that is not zero.  (-inf at an infinite T: the last range.)
-    __device__ float depth(float x) const { return fminf((x - largest) * hi * (-BINS / REACH), (float)(BINS - 1)); }
+    __device__ float depth(float x) const { return fminf((x - largest) * per_range, (float)(BINS - 1)); }
     __device__ float power(float x) const {
         const float d = x - largest, t = d * hi, e = __builtin_amdgcn_exp2f(t);
         return e + e * ((__builtin_fmaf(d, hi, -t) + d * lo) * 0.69314718f);
@@ -413,6 +413,7 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(SampleParams a) {
     weigh.hi = (float)per;
     weigh.lo = (float)(per - (double)weigh.hi);
     weigh.unit = __uint_as_float((uint32_t)(a.bits + 127) << 23);
+    weigh.per_range = weigh.hi * (-BINS / REACH);
     weigh.none = ((float)a.bits + 0.5f) * (BINS / REACH);
     auto token = [&](float x, int i, u64 all) {
         a.token[n] = i;
