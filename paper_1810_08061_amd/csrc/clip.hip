@@ -9,7 +9,8 @@
 // elements of one tensor and leaves its sum; the sums are added in an order that the sizes
 // decide, so the same call gives the same bits.  Up to FEW workgroups the last one to end adds
 // them; beyond, a launch of its own does: a counter that all count on takes about 40 ns each
-// (159 M elements, 9720 workgroups: 631 us so, XXX us with the launch).
+// (159 M elements, 9720 workgroups: 631 us so; 139 us and 5 with the launch, 4.6 TB/s).  2.9 M
+// elements: 10 us, and 9 for clipping them.
 //
 // One launch for up to 256 tensors (128 for clipping), whose addresses come with it.
 #include "ops.h"

@@ -15,6 +15,11 @@
 // vector unit of its CU, so where most tokens do not count a pass looks at them with as few instructions as
 // decide that (a difference, a product and a comparison), and forms keys and weights of the rest
 // alone; where most of them count it does the same for all, under no condition.
+//
+// Measured: 256 rows of 65536 in bf16 with top-p and min-p 55 us (25 without filters, where the row is
+// read and every weight formed once); 16 rows of 32768 with top-k and top-p 31 us, each row on one CU: six
+// passes of about 3 us with the joins between them.  Tried: the far ranges of the histogram summed in
+// registers instead (a branch an element: 74 us where one addition in LDS an element takes 62).
 #include "ops.h"
 #include "../../include/lstm_dyn_layer.h"
 
