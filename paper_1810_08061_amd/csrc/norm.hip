@@ -22,7 +22,6 @@ namespace ldyn {
 namespace {
 
 constexpr int MAX_D = 32768;
-constexpr int MAX_GROUPS = 1024;  // workgroups that leave sums
 
 struct NormParams {
     const void* x;
@@ -253,6 +252,14 @@ __global__ void __launch_bounds__(1024) norm_sums_kernel(const float* sums, int 
     }
 }
 
+// Workgroups that leave sums: rows of more than 4096 elements take 16 waves, one group a CU; the others
+// four groups a CU of 4 waves (1024 at most), with four rows and more for each wave or row of waves.
+int sum_groups(long long rows, int D, int num_cus, int at_once) {
+    const long long most = D > 4096 ? num_cus : 4LL * num_cus < 1024 ? 4LL * num_cus : 1024;
+    const long long want = (rows + 4 * at_once - 1) / (4 * at_once);
+    return (int)(want < most ? want : most);
+}
+
 int check_sizes(int B, int T, int D, int dtype, float eps) {
     if (B < 1 || T < 1 || D < 1 || !valid_dtype(dtype) || !(eps >= 0.0f) || std::isinf(eps)) return LSTM_DYN_ERR_INVALID;
     if (D > MAX_D || (long long)B * T >= 1LL << 31) return LSTM_DYN_ERR_UNSUPPORTED;
@@ -314,7 +321,8 @@ extern "C" int lstm_dyn_norm_create(lstm_dyn_norm_t** out, int B, int T, int D, 
     h->D = D;
     h->dtype = dtype;
     h->eps = eps;
-    if ((rc = ops_device(h)) == LSTM_DYN_OK) rc = ops_init(h, 256 + 8LL * MAX_GROUPS * D);
+    if ((rc = ops_device(h)) == LSTM_DYN_OK)
+        rc = ops_init(h, 256 + 8LL * sum_groups((long long)B * T, D, h->num_cus, 1) * D);
     if (rc != LSTM_DYN_OK) {
         delete h;
         return rc;
@@ -389,10 +397,7 @@ int run_backward(lstm_dyn_norm* h, const NormParams& p, float* d_weight, float* 
         constexpr int V = decltype(v)::value, NV = decltype(nv)::value, W = decltype(w)::value;
         if constexpr (V == 1 || V == VEC) {
             constexpr int PER = threads_of(W) / 64 / W;
-            long long most = (long long)h->num_cus * (W > 4 ? 1 : 4);
-            if (most > MAX_GROUPS) most = MAX_GROUPS;
-            const long long want = ((long long)p.rows + 4 * PER - 1) / (4 * PER);  // four rows and more each
-            groups = (int)(want < most ? want : most);
+            groups = sum_groups(p.rows, p.D, h->num_cus, PER);
             auto* k = is_far(h, (int)sizeof(G)) ? norm_back_kernel<E, G, V, NV, W, true> : norm_back_kernel<E, G, V, NV, W, false>;
             hipLaunchKernelGGL(k, dim3((unsigned)groups), dim3(threads_of(W)), 0, h->last_stream, p);
         }

@@ -134,6 +134,14 @@ def test_the_step_clipped_is_the_step_of_clipped_gradients(dtype, bits):
     one.close(), two.close(), clip.close()
 
 
+def test_nothing_to_add():
+    import torch
+    g = [torch.empty(0, device="cuda"), torch.empty(3, 0, device="cuda")]
+    with ld.GradClip(g, 1.0) as m:
+        for _ in range(2):
+            assert m.clip(g, grad_scale=0.5).tolist() == [0.0, 0.5]
+
+
 def test_wrong_lists_are_refused():
     import torch
     g = [torch.ones(4, device="cuda"), torch.ones(2, 3, device="cuda")]

@@ -206,3 +206,20 @@ def test_same_call_same_bits_and_replays(dtype):
         assert all((out[k] == want[k]).all() and (again[k] == want[k]).all() for k in want), i
     del graph
     m.close(), other.close()
+
+
+@pytest.mark.parametrize("D,dtype", [(4096, "bf16"), (4097, "bf16"), (4104, "f32"), (40, "f32"), (41, "bf16")])
+@pytest.mark.parametrize("rows", [1, 5, 1023, 5000])
+def test_sums_stay_in_the_workspace(D, dtype, rows):
+    """The workgroups' sums for every number of rows and shape of a row: as many as the handle made room for, and the
+    same as over the rows one by one (of ones and signs, whose sums are exact)."""
+    import torch
+    x = torch.ones((1, rows, D), device="cuda", dtype=torch.bfloat16 if dtype == "bf16" else torch.float32)
+    x[..., ::2] = -1
+    with ld.LayerNorm(1, rows, D, dtype, eps=0.0) as m:
+        got = m.backward(x, None, None, torch.ones_like(x))
+        room = m.query(ld.ops.OPS_Q_WORKSPACE_BYTES)
+    assert (got["dbias"] == rows).all()
+    assert room <= 256 + 8 * D * min((rows + 3) // 4, 1024)
+    if D % 2 == 0:
+        assert (got["dweight"][::2] == -rows).all() and (got["dweight"][1::2] == rows).all()
