@@ -186,7 +186,7 @@ class LinearAttention(_Handle):
         else:
             self._check("out_S", out_S, torch.float32, S0.shape)
         if out_y is None:
-            out_y = torch.empty((self.B, self.T, self._out), dtype=self._et, device=z.device)
+            out_y = z.new_empty((self.B, self.T, self._out))
         else:
             self._check("out_y", out_y, self._et, (self.B, self.T, self._out))
         _ok(ops._ready.lstm_dyn_attend_forward(self.handle, z.data_ptr(), L, S0.data_ptr(), out_S.data_ptr(),
@@ -235,7 +235,7 @@ class LinearAttention(_Handle):
         else:
             self._check("out_S", out_S, torch.float32, S.shape)
         if out_y is None:
-            out_y = torch.empty((R, self._out), dtype=self._et, device=z.device)
+            out_y = z.new_empty((R, self._out))
         else:
             self._check("out_y", out_y, self._et, (R, self._out))
         _ok(ops._ready.lstm_dyn_attend_step(self.handle, R, z.data_ptr(), S.data_ptr(), out_S.data_ptr(),
@@ -295,8 +295,8 @@ class LayerNorm(_Handle):
         code = BF16 if isinstance(dy, torch.Tensor) and dy.dtype == torch.bfloat16 else F32
         self._check("dy", dy, torch.bfloat16 if code == BF16 else torch.float32, x.shape)
         if out is None:
-            out = {"dx": torch.empty_like(dy), "dweight": torch.empty((self.D,), dtype=torch.float32, device=x.device),
-                   "dbias": torch.empty((self.D,), dtype=torch.float32, device=x.device)}
+            like = weight if weight is not None else x.new_empty((self.D,), dtype=torch.float32)
+            out = {"dx": torch.empty_like(dy), "dweight": torch.empty_like(like), "dbias": torch.empty_like(like)}
         else:
             if sorted(out) != ["dbias", "dweight", "dx"]:
                 raise ValueError("out must hold exactly ['dbias', 'dweight', 'dx']")
@@ -353,13 +353,12 @@ class GradClip(_Handle):
                 return self.norm(grads, grad_scale)
         grads = list(grads)
         et, code = self._type(grads)
-        return self._norm(self._grads("gradients", grads, et), code, grad_scale, grads[0].device)
+        return self._norm(self._grads("gradients", grads, et), code, grad_scale, grads[0])
 
-    def _norm(self, g, code, grad_scale, device):
-        torch = _t()
-        result = torch.empty((2,), dtype=torch.float32, device=device)
+    def _norm(self, g, code, grad_scale, like):
+        result = like.new_empty((2,), dtype=_t().float32)
         _ok(ops._ready.lstm_dyn_clip_norm(self.handle, g, code, grad_scale, self.max_norm, result.data_ptr(),
-                                          _stream(device)), "lstm_dyn_clip_norm")
+                                          _stream(like.device)), "lstm_dyn_clip_norm")
         return result
 
     def clip(self, grads, grad_scale: float = 1.0, out=None, stream=None):
@@ -371,9 +370,8 @@ class GradClip(_Handle):
         et, code = self._type(grads)
         g = self._grads("gradients", grads, et)
         o = g if out is None else self._grads("out", list(out), et)
-        device = grads[0].device
-        result = self._norm(g, code, grad_scale, device)
-        _ok(ops._ready.lstm_dyn_clip_apply(self.handle, g, code, result.data_ptr(), o, _stream(device)),
+        result = self._norm(g, code, grad_scale, grads[0])
+        _ok(ops._ready.lstm_dyn_clip_apply(self.handle, g, code, result.data_ptr(), o, _stream(result.device)),
             "lstm_dyn_clip_apply")
         return result
 

@@ -225,7 +225,12 @@ def _t():
 
 
 def _stream(device):
-    return _torch.cuda.current_stream(device).cuda_stream
+    """The address of the device's current stream.  torch's own short way to it takes 0.1 us, the public one,
+    which makes a Stream object, 2 us of calls that take 8."""
+    try:
+        return _torch._C._cuda_getCurrentRawStream(device.index)
+    except AttributeError:
+        return _torch.cuda.current_stream(device).cuda_stream
 
 
 def _dtype(dtype):
@@ -508,7 +513,7 @@ class AdamW(_Handle):
             if clip.shapes != [p.shape for p in self.params] or clip._device != self._device:
                 raise ValueError("clip must be over the parameters of this optimizer, on its device")
             g, code, device = self._pointers(*[g.data_ptr() for g in grads]), BF16 if et == torch.bfloat16 else F32, grads[0].device
-            result = clip._norm(g, code, grad_scale, device)
+            result = clip._norm(g, code, grad_scale, grads[0])
             _ok(_ready.lstm_dyn_adamw_step_clipped(self.handle, g, code, lr, self.betas[0], self.betas[1], self.eps,
                                                    result.data_ptr(), self.steps_done + 1, _stream(device)),
                 "lstm_dyn_adamw_step_clipped")
