@@ -685,16 +685,25 @@ __global__ void __launch_bounds__(64 * Chunk<E>::waves(DP), Chunk<E>::per_unit(D
     const E* pz = static_cast<const E*>(a.z) + step0 * a.ldz + head * a.R;
     E* out = STATE ? nullptr : static_cast<E*>(a.out) + step0 * a.ldo + head * a.R;
 
+    // All that comes before the first chunk is on its way before any of it is looked at: a share may be a chunk alone.
+    const int chunks = (len + C - 1) / C;
+    Stage<E, DP, STATE, MODE> stage;
+    auto chunk_of = [&](int c) { return a.back ? chunks - 1 - c : c; };
+    auto fetch_chunk = [&](int c) {
+        const int k = chunk_of(c) * C;
+        stage.get(px + k * a.ldx, py + k * a.ldy, pz + k * a.ldz, a, min(C, len - k));
+    };
+    if (chunks) fetch_chunk(0);
     f32x4_t M[PT][RT];
     const int PR = a.P * a.R;
     const float* start = a.start ? a.start + (long long)row * PR : nullptr;   // of the share that is gone through first
     if (share != (a.back ? used - 1 : 0)) start = share < used ? a.share + ((long long)row * p.shares + share) * PR : nullptr;
+    const int step_i = a.transposed ? 1 : p.Dv, step_c = a.transposed ? p.Dv : 1;
 #pragma unroll
     for (int pt = 0; pt < PT; ++pt)
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) M[pt][rt] = f32x4_t{0, 0, 0, 0};
-    const int step_i = a.transposed ? 1 : p.Dv, step_c = a.transposed ? p.Dv : 1;
-    if (!STATE && start) {   // (all fetched before the first is looked at, as in Stage)
+    if (!STATE && start) {
 #pragma unroll
         for (int pt = 0; pt < PT; ++pt)
 #pragma unroll
@@ -704,26 +713,20 @@ __global__ void __launch_bounds__(64 * Chunk<E>::waves(DP), Chunk<E>::per_unit(D
                     const int i = min(16 * pt + 4 * g + r, a.P - 1), c = min(16 * (w * RT + rt) + l, a.R - 1);
                     M[pt][rt][r] = start[i * step_i + c * step_c];
                 }
-#pragma unroll
-        for (int pt = 0; pt < PT; ++pt)
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (16 * pt + 4 * g + r >= a.P || 16 * (w * RT + rt) + l >= a.R) M[pt][rt][r] = 0.0f;
     }
-
-    const int chunks = (len + C - 1) / C;
-    Stage<E, DP, STATE, MODE> stage;
-    auto chunk_of = [&](int c) { return a.back ? chunks - 1 - c : c; };
-    auto fetch_chunk = [&](int c) {
-        const int k = chunk_of(c) * C;
-        stage.get(px + k * a.ldx, py + k * a.ldy, pz + k * a.ldz, a, min(C, len - k));
-    };
-    if (chunks) fetch_chunk(0);
     Mask<E, DP> mask;
     if constexpr (!STATE) mask.init(powers, a.back, w, l, g);
     decays(C);
+#pragma unroll
+    for (int pt = 0; pt < PT; ++pt)
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (16 * pt + 4 * g + r >= a.P || 16 * (w * RT + rt) + l >= a.R) M[pt][rt][r] = 0.0f;
+    float* end = STATE ? a.share + ((long long)row * p.shares + share) * PR : a.end ? a.end + (long long)row * PR : nullptr;
+    if (!STATE && share != (a.back ? 0 : used - 1)) end = nullptr;
+
     for (int c = 0; c < chunks; ++c) {
         const int k = chunk_of(c) * C;
         const int n = min(C, len - k);
@@ -734,12 +737,11 @@ __global__ void __launch_bounds__(64 * Chunk<E>::waves(DP), Chunk<E>::per_unit(D
         __syncthreads();
         if constexpr (!STATE) give<DP, MODE == PIECES>(s, a, M, mask, n, out + k * a.ldo);
         if (c + 1 < chunks) fetch_chunk(c + 1);   // (here, where few registers are in use)
-        carry<DP, STATE>(s, a, M);   // (and nothing else is fetched from memory: it would wait for all of the chunk)
+        if (c + 1 < chunks || end)   // a state that is neither read again nor kept is not formed
+            carry<DP, STATE>(s, a, M);   // (and nothing else is fetched from memory: it would wait for all of the chunk)
         __syncthreads();
     }
 
-    float* end = STATE ? a.share + ((long long)row * p.shares + share) * PR : a.end ? a.end + (long long)row * PR : nullptr;
-    if (!STATE && share != (a.back ? 0 : used - 1)) end = nullptr;
     if (end) {
 #pragma unroll
         for (int pt = 0; pt < PT; ++pt)
