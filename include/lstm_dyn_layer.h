@@ -114,8 +114,8 @@ int lstm_dyn_adamw_step_clipped(lstm_dyn_adamw_t* h, const void* const* grads, i
  * are all -inf has no token: -1, with logp -inf.  top_k <= 0 and top_p or min_p that are NaN are as if
  * not given, top_p <= 0 keeps the first token.
  * p are held as multiples of 2^-46 (of 2^-(62 - n) if V > 2^16, for the n with
- * 2^(n-1) < V <= 2^n): their sums are exact, so the order of summation changes nothing, and a token
- * whose p rounds to none of them is not chosen.
+ * 2^(n-1) < V <= 2^n), rounded down: their sums are exact, so the order of summation changes nothing, and a
+ * token whose p is below one of them is not chosen.
  *     logits  [N][V]  dtype, aligned to its elements
  *     u       [N]     fp32 in [0, 1) (clamped; NaN is 0)
  *     out_token int32 [N], out_logp fp32 [N]; they overlap nothing else */

@@ -31,7 +31,7 @@ namespace {
 typedef unsigned long long u64;
 
 constexpr int BINS = 2048, LIST = 512, SEGMENTS = 1024;
-constexpr float REACH = 48.0f;   // powers of two that the histogram spans: 2^-47 has no weight
+constexpr float REACH = 48.0f;   // powers of two that the histogram spans: below 2^-46 there is no weight
 constexpr int ROW_THREADS = 1024, SHORT_ROW_THREADS = 256, SHORT_ROW = 4096;
 
 struct SampleParams {
@@ -70,14 +70,19 @@ __device__ inline float clean(float x) { return fmaxf(x, -__builtin_inff()); }
 // tilt the weights of tokens far from the largest.
 struct Weigh {
     float largest, hi, lo, unit, none, per_range;
-    // How far below the largest x is, in ranges of the histogram.  From `none` on there is no weight, nearer
-    // p rounds to a multiple of 1 / unit that is not zero.  (-inf at an infinite T: the last range.)
+    // How far below the largest x is, in ranges of the histogram.  From `none` on there is no weight.  (-inf at an
+    // infinite T: the last range.)
     __device__ float depth(float x) const { return fminf((x - largest) * per_range, (float)(BINS - 1)); }
     __device__ float power(float x) const {
         const float d = x - largest, t = d * hi, e = __builtin_amdgcn_exp2f(t);
         return e + e * ((__builtin_fmaf(d, hi, -t) + d * lo) * 0.69314718f);
     }
-    __device__ u64 weight(float p) const { return (u64)rintf(p * unit); }
+    // p in multiples of 1 / (2^32 unit), rounded down.
+    __device__ u64 weight(float p) const {
+        const float x = p * unit;
+        const uint32_t high = (uint32_t)x;
+        return (u64)high << 32 | (uint32_t)((x - (float)high) * 0x1p32f);
+    }
 };
 
 // The tokens of the order's start: all of some weight whose keys are `key` or more.
@@ -210,12 +215,12 @@ __device__ inline Start find_start(RowLds& s, const Row<E>& row, const Weigh& we
     u64 target = 0;
     const u64 all = crossing<THREADS>(s, BINS, [&](u64 sum) { return target = aim(sum); }, [&](int i) { return s.hist[i]; });
     if (target >= all) return within;
-    const int at = s.range;
+    const float from = (float)s.range, upto = fminf(from + 1.0f, weigh.none);
     // f(x, key) of the range's tokens
     auto each = [&](auto f) {
         row.each(tid, row.pieces, THREADS, [&](float x, int i) {
             const float q = weigh.depth(x);
-            if ((int)q == at && q < weigh.none && (ALL || within.has(x, i))) f(x, key_of(x, i));
+            if (q >= from && q < upto && (ALL || within.has(x, i))) f(x, key_of(x, i));
         });
     };
     u64 rest = s.rest, lo = 0, hi = ~0ull;
@@ -417,9 +422,9 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(SampleParams a) {
     weigh.largest = mx;
     weigh.hi = (float)per;
     weigh.lo = (float)(per - (double)weigh.hi);
-    weigh.unit = __uint_as_float((uint32_t)(a.bits + 127) << 23);
+    weigh.unit = __uint_as_float((uint32_t)(a.bits - 32 + 127) << 23);
     weigh.per_range = weigh.hi * (-BINS / REACH);
-    weigh.none = ((float)a.bits + 0.5f) * (BINS / REACH);
+    weigh.none = (float)a.bits * (BINS / REACH);
     auto token = [&](float x, int i, u64 all) {
         a.token[n] = i;
         a.logp[n] = (float)(((double)x - (double)mx) / (double)T - log((double)all * exp2(-(double)a.bits)));
