@@ -114,18 +114,39 @@ struct Row {
         }
         return x;
     }
-    // f(x, index) of every element of pieces begin, begin + step, ... below end; the next two are on their way.
+    // f(x, index) of every element of pieces begin, begin + step, ... below end, in no order that counts. Whole pieces
+    // are read without a condition, so the next two are on their way while one is worked at; the row's first and last
+    // piece come by themselves where they are in part.
     template <class F>
     __device__ void each(int begin, int end, int step, F f) const {
-        if (begin >= end) return;
-        auto next = piece(begin), after = piece(min(begin + step, end - 1));
-#pragma unroll 1
-        for (int k = begin; k < end; k += step) {
-            const auto x = next;
-            next = after;
-            after = piece(min(k + 2 * step, end - 1));
+        using P = typename Vec<E, N>::type;
+        const int low = off ? 1 : 0, high = (V + off) / N;  // the whole pieces
+        const int stop = min(end, high);
+        int k = begin;
+        const auto work = [&](const P& x, int k) {
 #pragma unroll
             for (int j = 0; j < N; ++j) f(clean((float)x[j]), k * N - off + j);
+        };
+        bool part = k < low && k < end;
+        if (k < low) k += step;
+        if (k < stop) {
+            const P* from = reinterpret_cast<const P*>(p - off);
+            P next = from[k], after = from[min(k + step, stop - 1)];
+#pragma unroll 1
+            for (; k < stop; k += step) {
+                const P x = next;
+                next = after;
+                after = from[min(k + 2 * step, stop - 1)];
+                work(x, k);
+            }
+        }
+        // The last piece, if it is in part and this thread's, and the first.
+        const int last = pieces - 1;
+        const bool tail = last >= high && last >= low && last >= begin && last < end && (last - begin) % step == 0;
+#pragma unroll 1
+        for (int e = part ? 0 : 1; e < (tail ? 2 : 1); ++e) {
+            const int at = e ? last : 0;
+            work(piece(at), at);
         }
     }
 };
