@@ -40,6 +40,7 @@
 #include "../../include/lstm_dyn_layer.h"
 
 #include <cmath>
+#include <type_traits>
 #include <vector>
 
 namespace ldyn {
@@ -89,6 +90,9 @@ struct Chunk<float> {
 };
 
 __device__ inline double power(const double* log2a, int head, int n) { return n ? exp2(log2a[head] * n) : 1.0; }
+
+template <int N>
+using Part = std::integral_constant<int, N>;
 
 // The thread's number as one that the compiler does not know: what is formed from it inside the loop
 // over chunks is not kept in registers across it.
@@ -166,13 +170,15 @@ struct Stage {
             }
         }
     }
+    // PART of a chunk: 0 x, 1 y, 2 z.
+    template <int PART>
     __device__ void get(const E* px, const E* py, const E* pz, const Pass& a, int steps) {
         const unsigned id = here();
         const int c = (int)(id % COLS) * N, r0 = (int)(id / COLS) * ROWS;
         n = steps;
-        if constexpr (!STATE) fetch(x, px, a.ldx, r0, c, a.P);
-        fetch(y, py, a.ldy, r0, c, a.P);
-        fetch(z, pz, a.ldz, r0, c, a.R);
+        if constexpr (!STATE && PART == 0) fetch(x, px, a.ldx, r0, c, a.P);
+        if constexpr (PART == 1) fetch(y, py, a.ldy, r0, c, a.P);
+        if constexpr (PART == 2) fetch(z, pz, a.ldz, r0, c, a.R);
     }
     __device__ void settle(const Pass& a) {
         if constexpr (MODE == PIECES) return;
@@ -450,9 +456,9 @@ __device__ inline void give(LdsBf16<DP, false>& s, const Pass& a, const f32x4_t 
     }
 }
 
-// The same chunk: the state after it.
-template <int DP, bool STATE>
-__device__ inline void carry(LdsBf16<DP, STATE>& s, const Pass& a, f32x4_t (&M)[DP / 16][DP / 16 / Chunk<__bf16>::waves(DP)]) {
+// The same chunk: the state after it. fetch(Part): asks for an operand of the next chunk.
+template <int DP, bool STATE, class F>
+__device__ inline void carry(LdsBf16<DP, STATE>& s, const Pass& a, f32x4_t (&M)[DP / 16][DP / 16 / Chunk<__bf16>::waves(DP)], F fetch) {
     constexpr int W = Chunk<__bf16>::waves(DP), RT = DP / 16 / W, PT = DP / 16, COLS = DP / 8;
     const int lane = here() & 63, l = lane & 15, g = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -489,6 +495,12 @@ __device__ inline void carry(LdsBf16<DP, STATE>& s, const Pass& a, f32x4_t (&M)[
         }
         // the three parts one after another: a product waits for the one before in its sum
         bf16x8_t y[PT];
+        // the next chunk's operands are asked for in between: all at once they would fill the way to memory, and the
+        // wave would wait for room
+        __builtin_amdgcn_sched_barrier(0);
+        if (kb == 0) fetch(Part<0>());
+        else fetch(Part<2>());
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int pt = 0; pt < PT; ++pt) {
             y[pt] = columns<COLS>(s.y, c, pt, kb);
@@ -499,6 +511,11 @@ __device__ inline void carry(LdsBf16<DP, STATE>& s, const Pass& a, f32x4_t (&M)[
         for (int pt = 0; pt < PT; ++pt)
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) M[pt][rt] = mfma(y[pt], z2[rt], M[pt][rt]);
+        if (kb == 0) {
+            __builtin_amdgcn_sched_barrier(0);
+            fetch(Part<1>());
+            __builtin_amdgcn_sched_barrier(0);
+        }
 #pragma unroll
         for (int pt = 0; pt < PT; ++pt)
 #pragma unroll
@@ -689,11 +706,18 @@ __global__ void __launch_bounds__(64 * Chunk<E>::waves(DP), Chunk<E>::per_unit(D
     const int chunks = (len + C - 1) / C;
     Stage<E, DP, STATE, MODE> stage;
     auto chunk_of = [&](int c) { return a.back ? chunks - 1 - c : c; };
-    auto fetch_chunk = [&](int c) {
-        const int k = chunk_of(c) * C;
-        stage.get(px + k * a.ldx, py + k * a.ldy, pz + k * a.ldz, a, min(C, len - k));
+    auto fetch = [&](int c, auto part) {
+        // (behind the last chunk: through descriptors of no rows, otherwise the last one again)
+        const int k = chunk_of(min(c, chunks - 1)) * C;
+        stage.template get<decltype(part)::value>(px + k * a.ldx, py + k * a.ldy, pz + k * a.ldz, a,
+                                                  MODE == PIECES && c == chunks ? 0 : min(C, len - k));
     };
-    if (chunks) fetch_chunk(0);
+    auto fetch_all = [&](int c) {
+        fetch(c, Part<0>());
+        fetch(c, Part<1>());
+        fetch(c, Part<2>());
+    };
+    if (chunks) fetch_all(0);
     f32x4_t M[PT][RT];
     const int PR = a.P * a.R;
     const float* start = a.start ? a.start + (long long)row * PR : nullptr;   // of the share that is gone through first
@@ -735,10 +759,22 @@ __global__ void __launch_bounds__(64 * Chunk<E>::waves(DP), Chunk<E>::per_unit(D
         stage.settle(a);
         put_chunk(s, stage);
         __syncthreads();
-        if constexpr (!STATE) give<DP, MODE == PIECES>(s, a, M, mask, n, out + k * a.ldo);
-        if (c + 1 < chunks) fetch_chunk(c + 1);   // (here, where few registers are in use)
-        if (c + 1 < chunks || end)   // a state that is neither read again nor kept is not formed
-            carry<DP, STATE>(s, a, M);   // (and nothing else is fetched from memory: it would wait for all of the chunk)
+        // A state that is neither read again nor kept is not formed. (carry fetches nothing else from memory: it would
+        // wait for all of the next chunk.)
+        const bool carried = c + 1 < chunks || end;
+        if constexpr (C == 64) {
+            // (a wave at its outputs comes before one at its state; so they alternate better, 3 to 4%)
+            if constexpr (!STATE) {
+                __builtin_amdgcn_s_setprio(1);
+                give<DP, MODE == PIECES>(s, a, M, mask, n, out + k * a.ldo);
+                __builtin_amdgcn_s_setprio(0);
+            }
+            if (carried) carry<DP, STATE>(s, a, M, [&](auto part) { fetch(c + 1, part); });
+        } else {
+            if constexpr (!STATE) give<DP, MODE == PIECES>(s, a, M, mask, n, out + k * a.ldo);
+            if (c + 1 < chunks) fetch_all(c + 1);   // (here, where few registers are in use)
+            if (carried) carry<DP, STATE>(s, a, M);
+        }
         __syncthreads();
     }
 
