@@ -63,9 +63,6 @@ __device__ inline float logit_of(u64 key) {
     return __uint_as_float(b & 0x80000000u ? b & 0x7fffffffu : ~b);
 }
 
-// NaN as -inf.
-__device__ inline float clean(float x) { return fmaxf(x, -__builtin_inff()); }
-
 // exp((x - largest) / T): 1 / (T ln 2) is held in two parts, so its rounding does not
 // tilt the weights of tokens far from the largest.
 struct Weigh {
@@ -114,7 +111,8 @@ struct Row {
         }
         return x;
     }
-    // f(x, index) of every element of pieces begin, begin + step, ... below end, in no order that counts. Whole pieces
+    // f(x, index) of every element of pieces begin, begin + step, ... below end, in no order that counts (x may be NaN:
+    // every f leaves it out by a comparison). Whole pieces
     // are read without a condition, so the next two are on their way while one is worked at; the row's first and last
     // piece come by themselves where they are in part.
     template <class F>
@@ -125,7 +123,7 @@ struct Row {
         int k = begin;
         const auto work = [&](const P& x, int k) {
 #pragma unroll
-            for (int j = 0; j < N; ++j) f(clean((float)x[j]), k * N - off + j);
+            for (int j = 0; j < N; ++j) f((float)x[j], k * N - off + j);
         };
         bool part = k < low && k < end;
         if (k < low) k += step;
@@ -237,9 +235,14 @@ __device__ inline Start find_start(RowLds& s, const Row<E>& row, const Weigh& we
     const u64 all = crossing<THREADS>(s, BINS, [&](u64 sum) { return target = aim(sum); }, [&](int i) { return s.hist[i]; });
     if (target >= all) return within;
     const float from = (float)s.range, upto = fminf(from + 1.0f, weigh.none);
-    // f(x, key) of the range's tokens
+    // f(x, key) of the range's tokens: bounds that hold more than the range (by 2^-20, roundings are 2^-23; all, where no
+    // range has an end) leave most tokens out by two comparisons
+    const double far = (double)upto / weigh.per_range, near = (double)from / weigh.per_range;
+    const float low = (float)(weigh.largest + far - 0x1p-20 * (fabs(far) + fabs(weigh.largest)));
+    const float high = (float)(weigh.largest + near + 0x1p-20 * (fabs(near) + fabs(weigh.largest)));
     auto each = [&](auto f) {
         row.each(tid, row.pieces, THREADS, [&](float x, int i) {
+            if (x < low || x > high) return;
             const float q = weigh.depth(x);
             if (q >= from && q < upto && (ALL || within.has(x, i))) f(x, key_of(x, i));
         });
@@ -343,7 +346,7 @@ __device__ inline void walk(RowLds& s, const Row<E>& row, W weight, A aim, F fou
         if (k < row.pieces) {
             const auto raw = row.piece(k);
 #pragma unroll
-            for (int j = 0; j < M; ++j) x[j] = clean((float)raw[j]);
+            for (int j = 0; j < M; ++j) x[j] = (float)raw[j];
         }
 #pragma unroll
         for (int j = 0; j < M; ++j) {
