@@ -447,7 +447,7 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(SampleParams a) {
     weigh.hi = (float)per;
     weigh.lo = (float)(per - (double)weigh.hi);
     weigh.unit = __uint_as_float((uint32_t)(a.bits - 32 + 127) << 23);
-    weigh.per_range = weigh.hi * (-BINS / REACH);
+    weigh.per_range = fmaxf(weigh.hi * (-BINS / REACH), -3.4028235e38f);   // (finite: the largest is at depth zero at any T)
     weigh.none = (float)a.bits * (BINS / REACH);
     auto token = [&](float x, int i, u64 all) {
         a.token[n] = i;

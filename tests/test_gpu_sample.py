@@ -179,6 +179,54 @@ def test_far_apart_and_large_logits():
     assert (token == 77).all() and (logp == 0).all()
 
 
+@pytest.mark.parametrize("T", [1e-30, 1e-36, 1.9e-37, 1.7e-37, 1e-37, 1e-38, 5e-39])
+@pytest.mark.parametrize("filters", [{}, {"top_p": 0.9}, {"top_k": 6}, {"top_k": 9, "top_p": 0.8, "min_p": 0.01}])
+def test_temperatures_near_the_end_of_fp32(T, filters):
+    """Down to where 1 / T is no fp32 number, the differences of logits count in multiples of T. Weights are off by 2^-22
+    (an exponential and its correction), log p by twice as much and its own rounding (below 16: 2^-21)."""
+    r = np.random.default_rng(5)
+    N, V = 24, 200
+    x = np.full((N, V), -1.0)
+    x[:, ::9] = -T * r.integers(0, 40, (N, 23)) / 8
+    x = _dev(x)
+    u, t = np.float32(r.random(N)).astype(np.float64), float(np.float32(T))
+    token, logp = _sample(x, u, temperature=t, **filters)
+    xs, seen = x.double().cpu().numpy(), 0
+    f32 = lambda v: float(np.float32(v))
+    for n in range(N):
+        want, lp, near = layer_util.sample(xs[n], u[n], t, filters.get("top_k", 0), f32(filters.get("top_p", 1.0)),
+                                           f32(filters.get("min_p", 0.0)))
+        if near < 1e-6:
+            continue
+        seen += 1
+        assert token[n] == want and abs(logp[n] - lp) <= 2.0 ** -20, (n, token[n], want, logp[n], lp)
+    assert seen > N // 2
+
+
+def _nan_rows(V):
+    x = np.full((5, V), float("nan"))
+    x[0, V // 2] = 1.0
+    x[1, ::3] = np.arange(len(x[1, ::3])) % 5
+    x[2, :] = np.where(np.arange(V) % 2, x[2], -INF)
+    x[3, V - 1] = x[3, 0] = -3e38
+    x[4, :7] = 3e38
+    return x
+
+
+@pytest.mark.parametrize("V", [9, 1001, 5000])
+@pytest.mark.parametrize("filters", [{}, {"top_p": 0.7}, {"top_k": 3}, {"top_k": 8, "top_p": 0.6}, {"min_p": 0.1}])
+def test_no_numbers_are_never_taken(V, filters):
+    """Rows of NaN but for a few logits, among them the largest and smallest finite ones."""
+    x, u = _nan_rows(V), [0.3, 0.55, 0.3, 0.8, 0.45]
+    token, logp = _sample(x, u, **filters)
+    xs = np.float32(x).astype(np.float64)
+    for n in range(5):
+        want, lp, near = layer_util.sample(xs[n], float(np.float32(u[n])), 1.0, filters.get("top_k", 0),
+                                           float(np.float32(filters.get("top_p", 1.0))), float(np.float32(filters.get("min_p", 0.0))))
+        assert near > 1e-6 and token[n] == want, (n, token[n], want)
+        assert logp[n] == lp or abs(logp[n] - lp) < 2.0 ** -20 * max(1.0, abs(lp)), (n, logp[n], lp)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_rows_off_their_alignment(dtype):
     """Odd V: every row starts elsewhere; and a buffer that starts at any element."""
