@@ -10,15 +10,20 @@
 // in it; its few tokens are ranked by counting.  Where they are more than LIST
 // (many equal logits), the range is cut again by key until they are not.  Then the kept weights of each
 // segment of the row are summed, and one wave walks the segment that u falls into.
+// Where the first histogram shows that FEW tokens at most can be taken (a small k, or weights
+// that few tokens have), they are gathered once, and every cut and the running sum are formed by
+// comparing each with each, without more passes.
 //
-// A workgroup holds a row: its two to six passes come from the L2 after the first.  They are bound by the
+// A workgroup holds a row: its passes, three to six, come from the L2 after the first.  They are bound by the
 // vector unit of its CU, so where most tokens do not count a pass looks at them with as few instructions as
-// decide that (a difference, a product and a comparison), and forms keys and weights of the rest
+// decide that (two comparisons), and forms keys and weights of the rest
 // alone; where most of them count it does the same for all, under no condition.
 //
-// Measured: 256 rows of 65536 in bf16 with top-p and min-p 55 us (25 without filters, where the row is
-// read and every weight formed once); 16 rows of 32768 with top-k and top-p 31 us, each row on one CU: six
-// passes of about 3 us with the joins between them.  Tried: the far ranges of the histogram summed in
+// Measured, bf16: 256 rows of 65536 with top-p and min-p 51 us (21 without filters, where the row is
+// read and every weight formed once); 16 rows of 32768 with top-k to 1000 and top-p 30 us, each row on one CU:
+// passes of about 3 us with the joins between them.  With k 50 and p 0.9, few tokens: 16 rows of 32768
+// 12.9 us (23.9 with the passes), 256 of 65536 19 (38), in fp32 one of 131072 27 (66).  FEW: comparing 256 with each
+// other took 6 us and more, as much as it saves.  Tried: the far ranges of the histogram summed in
 // registers instead (a branch an element: 74 us where one addition in LDS an element takes 62).
 #include "ops.h"
 #include "../../include/lstm_dyn_layer.h"
@@ -30,7 +35,7 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr int BINS = 2048, LIST = 512, SEGMENTS = 1024;
+constexpr int BINS = 2048, LIST = 512, SEGMENTS = 1024, FEW = 128;
 constexpr float REACH = 48.0f;   // powers of two that the histogram spans: below 2^-46 there is no weight
 constexpr int ROW_THREADS = 1024, SHORT_ROW_THREADS = 256, SHORT_ROW = 4096;
 
@@ -86,6 +91,7 @@ struct Weigh {
 struct Start {
     u64 key = 0;
     float logit = -__builtin_inff();   // of `key`: a smaller one is out
+    bool done = false;                 // the row has its token
     __device__ bool has(float x, int i) const { return x > logit || (x == logit && key_of(x, i) >= key); }
 };
 
@@ -206,11 +212,90 @@ __device__ inline u64 crossing(RowLds& s, int n, A aim, G value) {
     return all;
 }
 
+// A logit that no token less deep than `upto` is below: 2^-20 of both terms further, where roundings are 2^-23.
+__device__ inline float below(const Weigh& weigh, float upto) {
+    const double far = (double)upto / weigh.per_range;   // (-inf where no range has an end)
+    return (float)(weigh.largest + far - 0x1p-20 * (fabs(far) + fabs(weigh.largest)));
+}
+
+// What is left of the row where few tokens can be taken: those less deep than `upto`, the start of the order.  Of them the
+// first k, of those the first whose weights reach goal(the sum of theirs), of those the ones that keep(x) leaves.  Each
+// token's place and the sums before it are formed by comparing it with every other one: no more passes over the row.
+// False, and nothing done, if they are more than FEW.
+template <int THREADS, class E, class G, class K, class A, class F>
+__device__ inline bool among_few(RowLds& s, const Row<E>& row, const Weigh& weigh, float upto, u64 k, G goal, K keep, A aim, F found) {
+    const int tid = threadIdx.x;
+    if (tid == 0) s.count = 0;
+    for (int i = tid; i < 3 * FEW; i += THREADS) s.segment[i] = 0;
+    __syncthreads();
+    const float low = below(weigh, upto);
+    row.each(tid, row.pieces, THREADS, [&](float x, int i) {
+        if (x < low || !(weigh.depth(x) < upto)) return;
+        const int to = atomicAdd(&s.count, 1);
+        if (to < FEW) {
+            s.key[to] = key_of(x, i);
+            s.weight[to] = weigh.weight(weigh.power(x));
+        }
+    });
+    __syncthreads();
+    const int n = s.count;
+    if (n > FEW) {
+        __syncthreads();   // all have read s.count
+        return false;
+    }
+    // several waves compare the same tokens, each with some of the others
+    const int wide = n > 64 ? 128 : 64, token = tid & (wide - 1), part = tid / wide, parts = THREADS / wide;
+    u64 *sums = s.segment, *places = sums + FEW, *sums_by_index = places + FEW;
+    {
+        const u64 key = s.key[token];
+        u64 before = 0, place = 0;
+#pragma unroll 4
+        for (int e = part; e < n; e += parts) {
+            const bool first = s.key[e] > key;
+            before += first ? s.weight[e] : 0ull;
+            place += first;
+        }
+        atomicAdd(sums + token, before);
+        atomicAdd(places + token, place);
+    }
+    __syncthreads();
+    // (a wave's tokens are a lane each: two waves)
+    u64 key = 0, kept = 0, before = 0;
+    if (tid < n) {
+        key = s.key[tid];
+        before = sums[tid];
+        kept = places[tid] < k ? s.weight[tid] : 0;
+    }
+    u64 all = wave_sum(kept);
+    if (tid < FEW && (tid & 63) == 0) s.part[tid >> 6] = all;
+    __syncthreads();
+    if (!(before < goal(s.part[0] + s.part[1])) || !keep(logit_of(key))) kept = 0;
+    if (tid < n) s.weight[tid] = kept;
+    all = wave_sum(kept);
+    if (tid < FEW && (tid & 63) == 0) s.part[2 + (tid >> 6)] = all;
+    __syncthreads();
+    {
+        const uint32_t index = ~(uint32_t)s.key[token];
+        u64 before = 0;
+#pragma unroll 4
+        for (int e = part; e < n; e += parts) before += ~(uint32_t)s.key[e] < index ? s.weight[e] : 0ull;
+        atomicAdd(sums_by_index + token, before);
+    }
+    __syncthreads();
+    if (!kept) return true;
+    before = sums_by_index[tid];
+    all = s.part[2] + s.part[3];
+    const u64 target = aim(all);
+    if (before < target && before + kept >= target) found(logit_of(key), (int)~(uint32_t)key, all);
+    return true;
+}
+
 // The shortest start, within `within` (ALL: it is all tokens), whose measure (the tokens' number, or with MASS
 // their weight) reaches the target.  aim(all): the target, given the sum of all measures; if it is no less than
-// all there is, `within` itself.
-template <int THREADS, bool MASS, bool ALL, class E, class A>
-__device__ inline Start find_start(RowLds& s, const Row<E>& row, const Weigh& weigh, const Start within, A aim) {
+// all there is, `within` itself.  few(upto, measure, all): told that tokens of this measure are less deep than upto, among them the
+// start's, may end the row.
+template <int THREADS, bool MASS, bool ALL, class E, class A, class W>
+__device__ inline Start find_start(RowLds& s, const Row<E>& row, const Weigh& weigh, const Start within, A aim, W few) {
     const int tid = threadIdx.x;
     auto clear = [&] {
         for (int i = tid; i < BINS; i += THREADS) s.hist[i] = 0;
@@ -233,12 +318,16 @@ __device__ inline Start find_start(RowLds& s, const Row<E>& row, const Weigh& we
     __syncthreads();
     u64 target = 0;
     const u64 all = crossing<THREADS>(s, BINS, [&](u64 sum) { return target = aim(sum); }, [&](int i) { return s.hist[i]; });
-    if (target >= all) return within;
+    Start done;
+    done.done = true;
+    if (target >= all) return few(weigh.none, all, all) ? done : within;
     const float from = (float)s.range, upto = fminf(from + 1.0f, weigh.none);
+    u64 rest = s.rest, lo = 0, hi = ~0ull;
+    if (few(upto, target - rest + s.hist[s.range], all)) return done;
     // f(x, key) of the range's tokens: bounds that hold more than the range (by 2^-20, roundings are 2^-23; all, where no
     // range has an end) leave most tokens out by two comparisons
-    const double far = (double)upto / weigh.per_range, near = (double)from / weigh.per_range;
-    const float low = (float)(weigh.largest + far - 0x1p-20 * (fabs(far) + fabs(weigh.largest)));
+    const double near = (double)from / weigh.per_range;
+    const float low = below(weigh, upto);
     const float high = (float)(weigh.largest + near + 0x1p-20 * (fabs(near) + fabs(weigh.largest)));
     auto each = [&](auto f) {
         row.each(tid, row.pieces, THREADS, [&](float x, int i) {
@@ -247,7 +336,6 @@ __device__ inline Start find_start(RowLds& s, const Row<E>& row, const Weigh& we
             if (q >= from && q < upto && (ALL || within.has(x, i))) f(x, key_of(x, i));
         });
     };
-    u64 rest = s.rest, lo = 0, hi = ~0ull;
     for (bool by_key = false;; by_key = true) {
         // the tokens of the range, if they are few
         if (tid == 0) s.count = 0;
@@ -454,13 +542,26 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(SampleParams a) {
         a.logp[n] = (float)(((double)x - (double)mx) / (double)T - log((double)all * exp2(-(double)a.bits)));
     };
     auto aim = [&](u64 all) { return above(u, all); };
+    auto goal = [&](u64 all) { return top_p < 1.0f ? top_p_of(top_p, all) : ~0ull; };
+    auto keep = [&](float x) { return !(least_p && weigh.power(x) < min_p); };
+    auto none = [](float, u64, u64) { return false; };
     Start start;
     if (top_k) {
-        start = find_start<THREADS, false, true>(s, row, weigh, start, [&](u64) { return (u64)top_k; });
+        start = find_start<THREADS, false, true>(s, row, weigh, start, [&](u64) { return (u64)top_k; }, [&](float upto, u64 tokens, u64) {
+            return tokens <= FEW && among_few<THREADS>(s, row, weigh, upto, (u64)top_k, goal, keep, aim, token);
+        });
+        if (start.done) return;
         if (top_p < 1.0f)
-            start = find_start<THREADS, true, false>(s, row, weigh, start, [&](u64 all) { return top_p_of(top_p, all); });
+            start = find_start<THREADS, true, false>(s, row, weigh, start, [&](u64 all) { return top_p_of(top_p, all); }, none);
     } else if (top_p < 1.0f) {
-        start = find_start<THREADS, true, true>(s, row, weigh, start, [&](u64 all) { return top_p_of(top_p, all); });
+        start = find_start<THREADS, true, true>(s, row, weigh, start, [&](u64 all) { return top_p_of(top_p, all); },
+                                                [&](float upto, u64 weights, u64 all) {
+            // each of them has this weight at least (the last of them a rounding less)
+            const float least = __builtin_amdgcn_exp2f((float)a.bits - upto * (REACH / BINS));
+            return (float)weights <= 0.98f * FEW * least &&
+                   among_few<THREADS>(s, row, weigh, upto, ~0ull, [&](u64) { return top_p_of(top_p, all); }, keep, aim, token);
+        });
+        if (start.done) return;
     } else if (!least_p) {
         walk<THREADS>(
             s, row,

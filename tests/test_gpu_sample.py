@@ -203,6 +203,30 @@ def test_temperatures_near_the_end_of_fp32(T, filters):
     assert seen > N // 2
 
 
+@pytest.mark.parametrize("top", [1, 2, 63, 64, 65, 127, 128, 129, 300, 513])
+@pytest.mark.parametrize("spread", [0.0, 0.01, 3.0])
+@pytest.mark.parametrize("V", [2000, 9001])
+def test_few_and_more_tokens_far_above_the_others(top, spread, V):
+    """As many as can be compared one by one, one more, and fewer, in one range of the histogram and in several,
+    with the cuts of every filter in them and behind. Tolerance of log p: that of the temperatures above."""
+    r = np.random.default_rng(top)
+    x = np.full((1, V), -30.0) - r.random((1, V))
+    x[0, r.permutation(V)[:top]] = 4 - spread * np.arange(top) / top
+    x = np.repeat(np.float32(x).astype(np.float64), 12, 0)
+    u = np.float32(r.random(12)).astype(np.float64)
+    f32, seen = lambda v: float(np.float32(v)), 0
+    for f in ({"top_k": top}, {"top_k": max(top - 1, 2)}, {"top_k": top + 1}, {"top_p": 0.61}, {"top_p": 0.999}, {"top_k": top + 9, "top_p": 0.53},
+              {"top_k": max(top // 2, 2), "top_p": 0.37, "min_p": 0.2}, {"top_p": 0.77, "min_p": 0.3}):
+        token, logp = _sample(x, u, **f)
+        for n in range(12):
+            want, lp, near = layer_util.sample(x[n], u[n], 1.0, f.get("top_k", 0), f32(f.get("top_p", 1.0)), f32(f.get("min_p", 0.0)))
+            if near < 1e-6:
+                continue
+            seen += 1
+            assert token[n] == want and abs(logp[n] - lp) <= 2.0 ** -20, (f, n, token[n], want, logp[n], lp)
+    assert seen > 48
+
+
 def _nan_rows(V):
     x = np.full((5, V), float("nan"))
     x[0, V // 2] = 1.0
