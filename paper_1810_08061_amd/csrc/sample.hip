@@ -7,8 +7,8 @@
 // that is all whose 64-bit key, the logit's bits in an order-preserving form above the
 // complement of the index, reaches a cut.  The cut for a count (top-k) or a sum of weights (top-p) is
 // found by a histogram over 2048 ranges of the exponent, which leaves one range with the cut
-// in it; its few tokens are ranked by counting.  Where they are more than LIST
-// (many equal logits), the range is cut again by key until they are not.  Then the kept weights of each
+// in it; its few tokens are listed, cut once more by key if they are many, and ranked by counting.  Where
+// they are more than LIST (many equal logits), the row is cut again by key until they are not.  Then the kept weights of each
 // segment of the row are summed, and one wave walks the segment that u falls into.
 // Where the first histogram shows that FEW tokens at most can be taken (a small k, or weights
 // that few tokens have), they are gathered once, and every cut and the running sum are formed by
@@ -19,7 +19,7 @@
 // decide that (two comparisons), and forms keys and weights of the rest
 // alone; where most of them count it does the same for all, under no condition.
 //
-// Measured, bf16: 256 rows of 65536 with top-p and min-p 51 us (21 without filters, where the row is
+// Measured, bf16: 256 rows of 65536 with top-p and min-p 46 us (21 without filters, where the row is
 // read and every weight formed once); 16 rows of 32768 with top-k to 1000 and top-p 30 us, each row on one CU:
 // passes of about 3 us with the joins between them.  With k 50 and p 0.9, few tokens: 16 rows of 32768
 // 12.9 us (23.9 with the passes), 256 of 65536 19 (38), in fp32 one of 131072 27 (66).  FEW: comparing 256 with each
@@ -28,6 +28,7 @@
 #include "ops.h"
 #include "../../include/lstm_dyn_layer.h"
 
+#include <cfloat>
 #include <cmath>
 
 namespace ldyn {
@@ -36,6 +37,7 @@ namespace {
 typedef unsigned long long u64;
 
 constexpr int BINS = 2048, LIST = 512, SEGMENTS = 1024, FEW = 128;
+static_assert(BINS == 1 << 11, "a key's range is found by a shift");
 constexpr float REACH = 48.0f;   // powers of two that the histogram spans: below 2^-46 there is no weight
 constexpr int ROW_THREADS = 1024, SHORT_ROW_THREADS = 256, SHORT_ROW = 4096;
 
@@ -214,8 +216,8 @@ __device__ inline u64 crossing(RowLds& s, int n, A aim, G value) {
 
 // A logit that no token less deep than `upto` is below: 2^-20 of both terms further, where roundings are 2^-23.
 __device__ inline float below(const Weigh& weigh, float upto) {
-    const double far = (double)upto / weigh.per_range;   // (-inf where no range has an end)
-    return (float)(weigh.largest + far - 0x1p-20 * (fabs(far) + fabs(weigh.largest)));
+    const float far = upto / weigh.per_range;   // (-inf where no range has an end)
+    return weigh.largest + far - 0x1p-20f * (fabsf(far) + fabsf(weigh.largest));
 }
 
 // What is left of the row where few tokens can be taken: those less deep than `upto`, the start of the order.  Of them the
@@ -301,6 +303,25 @@ __device__ inline Start find_start(RowLds& s, const Row<E>& row, const Weigh& we
         for (int i = tid; i < BINS; i += THREADS) s.hist[i] = 0;
         __syncthreads();
     };
+    // the least a and the largest b of all threads
+    auto ends = [&](u64& a, u64& b, u64* room) {
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+            const u64 a2 = __shfl_xor(a, o), b2 = __shfl_xor(b, o);
+            a = a2 < a ? a2 : a;
+            b = b2 > b ? b2 : b;
+        }
+        if ((tid & 63) == 0) {
+            s.part[tid >> 6] = a;
+            room[tid >> 6] = b;
+        }
+        __syncthreads();
+#pragma unroll 2   // (all at once they would take 64 registers)
+        for (int i = 0; i < THREADS / 64; ++i) {
+            a = s.part[i] < a ? s.part[i] : a;
+            b = room[i] > b ? room[i] : b;
+        }
+    };
     auto measure = [&](float x) { return MASS ? weigh.weight(weigh.power(x)) : 1ull; };
     clear();
     row.each(tid, row.pieces, THREADS, [&](float x, int i) {
@@ -326,9 +347,9 @@ __device__ inline Start find_start(RowLds& s, const Row<E>& row, const Weigh& we
     if (few(upto, target - rest + s.hist[s.range], all)) return done;
     // f(x, key) of the range's tokens: bounds that hold more than the range (by 2^-20, roundings are 2^-23; all, where no
     // range has an end) leave most tokens out by two comparisons
-    const double near = (double)from / weigh.per_range;
+    const float near = from / weigh.per_range;
     const float low = below(weigh, upto);
-    const float high = (float)(weigh.largest + near + 0x1p-20 * (fabs(near) + fabs(weigh.largest)));
+    const float high = weigh.largest + near + 0x1p-20f * (fabsf(near) + fabsf(weigh.largest));
     auto each = [&](auto f) {
         row.each(tid, row.pieces, THREADS, [&](float x, int i) {
             if (x < low || x > high) return;
@@ -351,12 +372,41 @@ __device__ inline Start find_start(RowLds& s, const Row<E>& row, const Weigh& we
         __syncthreads();
         const int n = s.count;
         if (n <= LIST) {
-            for (int e = tid; e < n; e += THREADS) {
-                const u64 key = s.key[e];
-                u64 before = 0;
+            // the token of the first `number` in which the target is, by comparing each with each
+            auto rank = [&](const u64* keys, const u64* weights, int number) {
+                for (int e = tid; e < number; e += THREADS) {
+                    const u64 key = keys[e];
+                    u64 before = 0;
 #pragma unroll 4
-                for (int f = 0; f < n; ++f) before += s.key[f] > key ? s.weight[f] : 0ull;
-                if (before < rest && before + s.weight[e] >= rest) s.found = key;
+                    for (int f = 0; f < number; ++f) before += keys[f] > key ? weights[f] : 0ull;
+                    if (before < rest && before + weights[e] >= rest) s.found = key;
+                }
+            };
+            if (n <= 64) {
+                rank(s.key, s.weight, n);
+            } else {
+                // cut by key among themselves: comparing each with each would take up to 6 us, this takes 2
+                u64 a = ~0ull, b = 0;
+                for (int e = tid; e < n; e += THREADS) {
+                    a = s.key[e] < a ? s.key[e] : a;
+                    b = s.key[e] > b ? s.key[e] : b;
+                }
+                ends(a, b, s.segment);
+                const int shift = max(53 - __builtin_clzll((b - a) | 1), 0);   // (of 2^11 ranges)
+                if (tid == 0) s.count = 0;
+                clear();
+                for (int e = tid; e < n; e += THREADS) atomicAdd(&s.hist[(b - s.key[e]) >> shift], s.weight[e]);
+                __syncthreads();
+                crossing<THREADS>(s, BINS, [&](u64) { return rest; }, [&](int i) { return s.hist[i]; });
+                rest = s.rest;
+                for (int e = tid; e < n; e += THREADS) {
+                    if ((int)((b - s.key[e]) >> shift) != s.range) continue;
+                    const int to = atomicAdd(&s.count, 1);
+                    s.segment[to] = s.key[e];
+                    s.segment[LIST + to] = s.weight[e];
+                }
+                __syncthreads();
+                rank(s.segment, s.segment + LIST, s.count);
             }
             __syncthreads();
             const u64 key = s.found;
@@ -369,27 +419,12 @@ __device__ inline Start find_start(RowLds& s, const Row<E>& row, const Weigh& we
                 a = key < a ? key : a;
                 b = key > b ? key : b;
             });
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1) {
-                const u64 a2 = __shfl_xor(a, o), b2 = __shfl_xor(b, o);
-                a = a2 < a ? a2 : a;
-                b = b2 > b ? b2 : b;
-            }
-            if ((tid & 63) == 0) {
-                s.part[tid >> 6] = a;
-                s.weight[tid >> 6] = b;
-            }
-            __syncthreads();
-            for (int i = 0; i < THREADS / 64; ++i) {
-                a = s.part[i] < a ? s.part[i] : a;
-                b = s.weight[i] > b ? s.weight[i] : b;
-            }
+            ends(a, b, s.weight);
             lo = a;
             hi = b;
             __syncthreads();
         }
-        int shift = 0;
-        while ((hi - lo) >> shift >= BINS) ++shift;
+        const int shift = max(53 - __builtin_clzll((hi - lo) | 1), 0);
         clear();
         each([&](float x, u64 key) {
             if (key >= lo && key <= hi) atomicAdd(&s.hist[(hi - key) >> shift], measure(x));
@@ -535,7 +570,7 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(SampleParams a) {
     weigh.hi = (float)per;
     weigh.lo = (float)(per - (double)weigh.hi);
     weigh.unit = __uint_as_float((uint32_t)(a.bits - 32 + 127) << 23);
-    weigh.per_range = fmaxf(weigh.hi * (-BINS / REACH), -3.4028235e38f);   // (finite: the largest is at depth zero at any T)
+    weigh.per_range = fmaxf(weigh.hi * (-BINS / REACH), -FLT_MAX);   // (finite: the largest is at depth zero at any T)
     weigh.none = (float)a.bits * (BINS / REACH);
     auto token = [&](float x, int i, u64 all) {
         a.token[n] = i;
@@ -544,6 +579,8 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(SampleParams a) {
     auto aim = [&](u64 all) { return above(u, all); };
     auto goal = [&](u64 all) { return top_p < 1.0f ? top_p_of(top_p, all) : ~0ull; };
     auto keep = [&](float x) { return !(least_p && weigh.power(x) < min_p); };
+    // depths from which on tokens are smaller than min_p
+    const float min_p_depth = least_p ? fminf((1e-3f - __builtin_amdgcn_logf(min_p)) * (BINS / REACH), weigh.none) : weigh.none;
     auto none = [](float, u64, u64) { return false; };
     Start start;
     if (top_k) {
@@ -557,17 +594,21 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(SampleParams a) {
         start = find_start<THREADS, true, true>(s, row, weigh, start, [&](u64 all) { return top_p_of(top_p, all); },
                                                 [&](float upto, u64 weights, u64 all) {
             // each of them has this weight at least (the last of them a rounding less)
+            upto = fminf(upto, min_p_depth);
             const float least = __builtin_amdgcn_exp2f((float)a.bits - upto * (REACH / BINS));
             return (float)weights <= 0.98f * FEW * least &&
                    among_few<THREADS>(s, row, weigh, upto, ~0ull, [&](u64) { return top_p_of(top_p, all); }, keep, aim, token);
         });
         if (start.done) return;
-    } else if (!least_p) {
+    }
+    // the least logit that may be left: for most tokens the only test
+    const float least = fmaxf(fmaxf(below(weigh, min_p_depth), -FLT_MAX), start.logit);
+    if (!top_k && !(top_p < 1.0f) && !least_p) {
         walk<THREADS>(
             s, row,
             [&](float x, int) {
                 const u64 w = weigh.weight(weigh.power(x));
-                return weigh.depth(x) < weigh.none ? w : 0ull;
+                return x >= least ? w : 0;
             },
             aim, token);
         return;
@@ -575,7 +616,7 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(SampleParams a) {
     walk<THREADS>(
         s, row,
         [&](float x, int i) -> u64 {
-            if (!(x >= start.logit && weigh.depth(x) < weigh.none && start.has(x, i))) return 0;
+            if (!(x >= least && start.has(x, i))) return 0;
             const float p = weigh.power(x);
             return least_p && p < min_p ? 0 : weigh.weight(p);
         },
