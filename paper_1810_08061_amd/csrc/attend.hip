@@ -27,15 +27,16 @@
 // a launch forms what each share adds to the state, one joins them in their order, and
 // the pass's shares start from the joined states.
 //
-// Measured, bf16, heads of 128: 1 x 32768 x 16, forward, 75 us for the shares' states, 15 to join them, 157 for the pass
-// (3.4 TB/s of z and y; 241 us together, 2.2 TB/s of what the call cannot do without); 8 x 4096 x 16, ragged, forward
-// and backward 572 us, the three passes back 319.  What bounds a pass: for 64 steps a wave issues 208
+// Measured, bf16, heads of 128: 1 x 32768 x 16, forward, 74 us for the shares' states (3.6 TB/s), 16 to join them, 144 for
+// the pass (3.7 TB/s; 223 us together, 2.4 TB/s of what the call cannot do without); 8 x 4096 x 16, ragged, forward
+// and backward 540 to 560 us, the three passes back 264.  What bounds a pass: for 64 steps a wave issues 208
 // products for the matrix unit (3300 clocks), 870 vector instructions (3500: splitting into parts, decays,
-// addresses) and LDS reads, in phases between barriers; two workgroups a CU, which its registers allow, overlap
-// them by about half.  Tried and not kept: eight waves of 16 columns (199 us: spills, and every wave reads all rows); operands fetched a phase
-// ahead by scheduling barriers (no gain); vector and matrix instructions interleaved by scheduling groups (no
-// gain); more shares (327 us with twice as many).
-// A step of 16 x 8 heads of 64: 3.9 us, 4.3 TB/s of states.
+// addresses) and LDS reads, in phases between barriers; two workgroups a CU, which its registers allow, take 14800
+// clocks for a chunk each.  Tried and not kept: eight waves of 16 columns (199 us: spills, and every wave reads all rows);
+// operands fetched from LDS a phase ahead by scheduling barriers (no gain); vector and matrix instructions interleaved by
+// scheduling groups (no gain); workgroups of half the columns for the states (no gain: they wait for memory);
+// workgroups that are behind issued first (no gain over outputs first).
+// A step of 16 x 8 heads of 64: 4.0 us, 4.2 TB/s of states.
 #include "ops.h"
 #include "../../include/lstm_dyn_layer.h"
 

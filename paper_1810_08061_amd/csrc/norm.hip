@@ -10,9 +10,9 @@
 // rows, with weight, bias and the two gradients' sums of its columns in registers;
 // each workgroup leaves its sums in the workspace, and a second launch adds them in their order.
 //
-// Measured: 256 x 1000 x 1024 in bf16, ragged (half of the rows), with fp32 gradients: forward 187 us (4.2 TB/s),
-// backward 386 us (4.7) and 6 for the sums; a 2 GiB copy reaches 4.9.  21 x 45 x 333 in fp32, element by element: 3.8
-// and 10.3 us, a chain of loads and reductions for four rows a wave.
+// Measured: 256 x 1000 x 1024 in bf16, ragged (half of the rows), with fp32 gradients: forward 199 us (3.9 TB/s),
+// backward 382 us (4.7) and 5 for the sums; a 2 GiB copy reaches 4.9.  21 x 45 x 333 in fp32, element by element: 3.8
+// and 10.4 us, a chain of loads and reductions for four rows a wave.
 #include "ops.h"
 #include "../../include/lstm_dyn_layer.h"
 
