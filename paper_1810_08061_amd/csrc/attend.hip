@@ -950,10 +950,11 @@ static int attend_make(lstm_dyn_attend* h, const float* decay) {
     // As many shares as bring the workgroups that the device holds at once (bf16: two a CU of 128 columns, four of
     // 64; fp32: one), since a share costs a second reading of two operands and its states.  From 256
     // rows and heads on, which fill the device by themselves, a share has to be 16 chunks: below, the
-    // states cost more than the even load gains.  us, these rules and another number: 1 x 32768 x 16 heads of 128,
-    // forward, 307 and 353 with 256, 327 with 1024; 16 x 4096 x 16 heads of 64, forward, 152 and 215 with 512; training
-    // steps of 32 x 512 x 8 heads of 64, 77 and 130 without the last rule; of 5 x 301 x 3 heads in fp32, 61 and
-    // 116 with four chunks and more a share; of 4 x 1024 x 8 heads of 128 in fp32, 212 and 238 with 512.
+    // states cost more than the even load gains.  us, calls back to back, these rules and another number: 1 x 32768 x 16
+    // heads of 128, forward, 278 and 306 with 256, 295 with 1024; 8 x 4096 x 16, ragged, training steps, 535, 604 and 569;
+    // 16 x 4096 x 16 heads of 64, forward, 142 and 177 with 512; training steps of 32 x 512 x 8 heads of 64, 72 and 132
+    // without the last rule; of 5 x 301 x 3 heads in fp32, 55 and 112 with four chunks and more a share; of 4 x 1024 x 8
+    // heads of 128 in fp32, 194 and 217 with 512.
     const int C = h->dtype == LSTM_DYN_BF16 ? Chunk<__bf16>::C : Chunk<float>::C;
     const int groups = h->dtype != LSTM_DYN_BF16 ? 256 : h->Dk > 64 || h->Dv > 64 ? 512 : 1024;
     const int rows = h->B * h->heads, chunks = (h->T + C - 1) / C;
