@@ -41,7 +41,6 @@ static_assert(BINS == 1 << 11, "a key's range is found by a shift");
 constexpr int BITS = 46;         // of the largest weight
 constexpr float REACH = 48.0f;   // powers of two that the histogram spans: below 2^-46 there is no weight
 static_assert(BITS * (BINS / REACH) <= BINS - 64, "a range each for lanes whose tokens have no weight");
-constexpr int ROW_THREADS = 1024, SHORT_ROW_THREADS = 256, SHORT_ROW = 4096;
 
 struct SampleParams {
     const void* logits;
@@ -694,11 +693,18 @@ extern "C" int lstm_dyn_sample_step(lstm_dyn_sample_t* h, const void* logits, co
     if (rc != LSTM_DYN_OK || (rc = ops_begin(h, stream)) != LSTM_DYN_OK) return rc;
     const lstm_dyn_sample_filter_t none{1.0f, 1.0f, 0.0f, 0, nullptr, nullptr, nullptr, nullptr};
     const SampleParams p{logits, u, filter ? *filter : none, out_token, out_logp, h->V, h->bits};
-    const bool small = h->V <= SHORT_ROW;
-    auto* k = h->dtype == LSTM_DYN_BF16
-                  ? (small ? sample_kernel<__bf16, SHORT_ROW_THREADS> : sample_kernel<__bf16, ROW_THREADS>)
-                  : (small ? sample_kernel<float, SHORT_ROW_THREADS> : sample_kernel<float, ROW_THREADS>);
-    hipLaunchKernelGGL(k, dim3((unsigned)h->N), dim3(small ? SHORT_ROW_THREADS : ROW_THREADS), 0, h->last_stream, p);
+    // A workgroup is a row.  Where a CU has one, 512 threads hold a short row's waits at joins down and 1024 take a long one's
+    // work (us, k 200 and p 0.9, bf16: 64 rows of 4000 14.1 and 16.0 with 1024, 16 of 32768 26.4 and 30.2 with 512).  Where
+    // a CU has two, 512 let both be there; where it has more, 256 let four be, which fill each other's waits
+    // (1024 of 2000: 19.4, with 512 27.7, with 1024 52.3; 1500 of 8000: 51.8, 54.0, 87.2), but for rows so long that few such
+    // workgroups end last (1100 of 32768 in fp32, p 0.9: 147 and 130 with 512).
+    const int threads = h->N > 2 * h->num_cus && h->V <= 16384 ? 256 : h->N <= h->num_cus && h->V > 8192 ? 1024 : 512;
+    auto launch = [&](auto of_bf16, auto of_f32) {
+        hipLaunchKernelGGL(h->dtype == LSTM_DYN_BF16 ? of_bf16 : of_f32, dim3((unsigned)h->N), dim3(threads), 0, h->last_stream, p);
+    };
+    if (threads == 256) launch(sample_kernel<__bf16, 256>, sample_kernel<float, 256>);
+    else if (threads == 512) launch(sample_kernel<__bf16, 512>, sample_kernel<float, 512>);
+    else launch(sample_kernel<__bf16, 1024>, sample_kernel<float, 1024>);
     return ops_launched(h);
 }
 

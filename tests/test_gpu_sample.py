@@ -251,6 +251,29 @@ def test_no_numbers_are_never_taken(V, filters):
         assert logp[n] == lp or abs(logp[n] - lp) < 2.0 ** -20 * max(1.0, abs(lp)), (n, logp[n], lp)
 
 
+@pytest.mark.parametrize("V", [700, 9000, 17001])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("k,p,m", FILTERS)
+def test_a_row_gives_the_same_in_any_batch(dtype, V, k, p, m):
+    """Workgroups differ with the number of rows; sums are of whole numbers, so tokens and log p do not."""
+    import torch
+    r = np.random.default_rng(V + 4 * k + 2 * p + m)
+    N = 700
+    x, u = _dev(r.standard_normal((N, V)) * 3, dtype), _dev(r.random(N))
+    f = {"temperature": _dev(r.uniform(0.3, 1.2, N))}
+    if k:
+        f["top_k"] = _dev(r.integers(0, 600, N).astype(np.int32))
+    if p:
+        f["top_p"] = _dev(r.uniform(0.2, 1.0, N))
+    if m:
+        f["min_p"] = _dev(r.uniform(0.0, 0.2, N))
+    token, logp = _sample(x, u, **f)
+    for n in (300, 9):
+        at = torch.arange(n, device="cuda") * (N // n)
+        some = _sample(x[at], u[at], **{name: v[at] for name, v in f.items()})
+        assert (some[0] == token[at.cpu().numpy()]).all() and (some[1] == logp[at.cpu().numpy()]).all(), n
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_rows_off_their_alignment(dtype):
     """Odd V: every row starts elsewhere; and a buffer that starts at any element."""
