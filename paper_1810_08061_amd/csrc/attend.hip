@@ -39,6 +39,7 @@
 // A step of 16 x 8 heads of 64: 4.0 us, 4.2 TB/s of states.
 #include "ops.h"
 #include "../../include/lstm_dyn_layer.h"
+#include "attend_shares.h"
 
 #include <cmath>
 #include <type_traits>
@@ -684,9 +685,8 @@ __global__ void __launch_bounds__(64 * Chunk<E>::waves(DP), Chunk<E>::per_unit(D
     const int given = p.lengths[b * p.length_step], L = max(0, min(given, p.T));
     const int t0 = share * p.span, span = min(p.span, p.T - t0);
     const int len = max(0, min(L - t0, span));
-    const int used = max(1, (L + p.span - 1) / p.span);   // the row's shares; an empty row has its first
-    // the last share has no successor going forward, the first none going back
-    if (STATE && (share >= used || share == (a.back ? 0 : used - 1))) return;
+    const int used = shares_used(L, p.span);
+    if (STATE && !adds(share, used, a.back)) return;
 
     const float* powers = p.powers + head * TABLE;
     // (a chunk of n steps: rows that are not there are zeros, whatever they decay by)
@@ -721,8 +721,10 @@ __global__ void __launch_bounds__(64 * Chunk<E>::waves(DP), Chunk<E>::per_unit(D
     if (chunks) fetch_all(0);
     f32x4_t M[PT][RT];
     const int PR = a.P * a.R;
-    const float* start = a.start ? a.start + (long long)row * PR : nullptr;   // of the share that is gone through first
-    if (share != (a.back ? used - 1 : 0)) start = share < used ? a.share + ((long long)row * p.shares + share) * PR : nullptr;
+    const Start from = start_of(share, used);
+    const float* start = from == Start::SLOT            ? a.share + ((long long)row * p.shares + share) * PR
+                         : from == Start::GIVEN && a.start ? a.start + (long long)row * PR
+                                                           : nullptr;
     const int step_i = a.transposed ? 1 : p.Dv, step_c = a.transposed ? p.Dv : 1;
 #pragma unroll
     for (int pt = 0; pt < PT; ++pt)
@@ -750,7 +752,7 @@ __global__ void __launch_bounds__(64 * Chunk<E>::waves(DP), Chunk<E>::per_unit(D
             for (int r = 0; r < 4; ++r)
                 if (16 * pt + 4 * g + r >= a.P || 16 * (w * RT + rt) + l >= a.R) M[pt][rt][r] = 0.0f;
     float* end = STATE ? a.share + ((long long)row * p.shares + share) * PR : a.end ? a.end + (long long)row * PR : nullptr;
-    if (!STATE && share != (a.back ? 0 : used - 1)) end = nullptr;
+    if (!STATE && !ends_row(share, used, a.back)) end = nullptr;
 
     for (int c = 0; c < chunks; ++c) {
         const int k = chunk_of(c) * C;
@@ -800,15 +802,15 @@ __global__ void __launch_bounds__(64 * Chunk<E>::waves(DP), Chunk<E>::per_unit(D
     }
 }
 
-// The states that a row's shares start from, but for the one that is gone through first: what share k adds
-// to the state lies in its place, and the start of the one that follows it takes its own.
+// The states that a row's shares start from: what share k adds to the state lies in its slot until it has been read, and
+// its start takes that place.
 __global__ void __launch_bounds__(256) attend_join_kernel(AttendParams p) {
     const Pass& a = p.pass[blockIdx.z];
     const int row = blockIdx.y, PR = a.P * a.R, e = blockIdx.x * 256 + threadIdx.x;
     if (e >= PR) return;
     const int b = row / p.heads, head = row % p.heads;
     const int L = clamp_length(p.lengths[b * p.length_step], p.T, p.status, false);
-    const int used = (L + p.span - 1) / p.span;
+    const int used = shares_used(L, p.span);
     if (used < 2) return;
     float* share = a.share + (long long)row * p.shares * PR + e;
     float state = a.start ? a.start[(long long)row * PR + e] : 0.0f;
@@ -818,6 +820,7 @@ __global__ void __launch_bounds__(256) attend_join_kernel(AttendParams p) {
     constexpr int AT_ONCE = 8;   // fetched before the first is used
     auto place = [&](int i) { return share + (long long)(a.back ? used - 1 - i : i) * PR; };
     float add = *place(0);
+    *place(0) = state;
     for (int i0 = 1; i0 < used; i0 += AT_ONCE) {
         float next[AT_ONCE];   // (of the last share, whatever lies there: it is not used)
 #pragma unroll
