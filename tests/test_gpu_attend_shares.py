@@ -1,11 +1,11 @@
-"""Linear attention where a row of the time axis is cut into shares: the state in place, beside other work on the device."""
+"""Linear attention where a row of the time axis is cut into shares of several chunks; the state in place, beside other work."""
 import numpy as np
 import pytest
 
 import paper_1810_08061_amd as ld
 import workloads
 from tests.gpu_util import say, to_device
-from tests.test_gpu_attend import _inputs, _lengths
+from tests.test_gpu_attend import _compare, _inputs, _lengths
 
 pytestmark = pytest.mark.gpu
 
@@ -55,3 +55,27 @@ def test_in_place_gives_the_same_bits_beside_other_work(dtype, B, heads, Dk, Dv,
             assert (h == alone[0]).all() and (c == alone[1]).all()
         assert m.status() == ld.OK and loop.query(ld.Q_LAST_STATUS) == ld.OK
     loop.close()
+
+
+# Shares of several chunks each: states carried from chunk to chunk behind a row's first share, additions that several
+# chunks form, decays over whole shares of several chunks; lengths inside, at and just past a share of `span` steps.
+SEVERAL = [("f32", 20, 5, 16, 16, 300, 128), ("f32", 7, 16, 24, 9, 300, 128), ("f32", 2, 16, 128, 128, 700, 96),
+           ("bf16", 10, 30, 16, 16, 2500, 1024), ("bf16", 2, 16, 128, 128, 1100, 128), ("bf16", 2, 16, 128, 100, 1100, 128),
+           ("bf16", 5, 30, 20, 33, 1400, 256)]
+
+
+@pytest.mark.parametrize("dtype,B,heads,Dk,Dv,T,span", SEVERAL)
+def test_shares_of_several_chunks(dtype, B, heads, Dk, Dv, T, span):
+    say("several", dtype, B, heads, Dk, Dv, T)
+    r = np.random.default_rng(T + B)
+    last = (T - 1) // span * span
+    L = [T, last + 1, span, span + 1, 0, last, span - 1, 1, 2 * span, T - 1, *(int(x) for x in r.integers(0, T + 1, 10))][:B]
+    decay = [0.9, 1.0, 0.0, 0.999, 0.99, 0.5] * 5
+    s = _inputs(r, dtype, B, T, heads, Dk, Dv)
+    with ld.LinearAttention(B, heads, Dk, Dv, T, decay[:heads], dtype) as m:
+        assert _shares(m) == (T - 1) // span + 1 > 1          # and a share is several chunks of 32 or 64 steps
+        assert span > (64 if dtype == "bf16" else 32)
+        y, S = m.forward(s["z"], _lengths(L), s["S0"])
+        got = m.backward(s["z"], _lengths(L), s["S0"], s["dy"], s["dS"])
+        _compare(dict(got, y=y, S=S), s, L, decay[:heads], Dk, Dv, dtype)
+        assert m.status() == ld.OK
