@@ -73,17 +73,25 @@ __device__ inline float logit_of(u64 key) {
 
 // exp((x - largest) / T): 1 / (T ln 2) is held in two parts, so its rounding does not
 // tilt the weights of tokens far from the largest.
+// A token's weight is formed once for a sum and again where the token in which that sum's target lies is looked for. A
+// target that no token reached would leave a cut or the row's token unwritten, so every compiled copy of these functions has to give
+// the same bits: each rounding is written out, and no product is joined with a sum at the compiler's choice.
 struct Weigh {
     float largest, hi, lo, unit, none, per_range;
     // How far below the largest x is, in ranges of the histogram.  From `none` on there is no weight.  (-inf at an
     // infinite T: the last range.)
-    __device__ float depth(float x) const { return fminf((x - largest) * per_range, (float)(BINS - 1)); }
+    __device__ float depth(float x) const {
+#pragma clang fp contract(off)
+        return fminf((x - largest) * per_range, (float)(BINS - 1));
+    }
     __device__ float power(float x) const {
+#pragma clang fp contract(off)
         const float d = x - largest, t = d * hi, e = __builtin_amdgcn_exp2f(t);
-        return e + e * ((__builtin_fmaf(d, hi, -t) + d * lo) * 0.69314718f);
+        return __builtin_fmaf(e, __builtin_fmaf(d, lo, __builtin_fmaf(d, hi, -t)) * 0.69314718f, e);
     }
     // p in multiples of 1 / (2^32 unit), rounded down.
     __device__ u64 weight(float p) const {
+#pragma clang fp contract(off)
         const float x = p * unit;
         const uint32_t high = (uint32_t)x;
         return (u64)high << 32 | (uint32_t)((x - (float)high) * 0x1p32f);
