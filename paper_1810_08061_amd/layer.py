@@ -10,6 +10,7 @@ library's HIP kernels, a handle has one call in flight, a call runs on the curre
 from __future__ import annotations
 
 import ctypes
+import operator
 
 from . import BF16, F32, _on, ops
 from .ops import _call, _create, _dtype, _Handle, _ok, _query, _t
@@ -413,6 +414,8 @@ class TokenSample(_Handle):
             if isinstance(value, torch.Tensor):
                 self._check(name, value, torch.int32 if name == "top_k" else torch.float32, (N,))
                 setattr(f, name + "s", value.data_ptr())
+            elif name == "top_k":       # (a number that the structure's 32 bits do not hold would be cut to its low ones)
+                f.top_k = max(0, min(operator.index(value), self.V))
             else:
                 setattr(f, name, value)
         token, logp = torch.empty_like(u, dtype=torch.int32), torch.empty_like(u)
