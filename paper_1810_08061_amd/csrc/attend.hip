@@ -192,11 +192,11 @@ struct Stage {
     }
 };
 
-// out's rows 16 it + l from tiles whose lanes hold four columns of a row, from column c on.  WHOLE: through a
-// descriptor, as Stage fetches.
+// out's rows 16 it + l from tiles whose lanes hold four columns of a row, from column c on.  WHOLE (fp32; bf16 has its own
+// way through LDS): through a descriptor, as Stage fetches.
 template <class E, int TI, int RT, bool WHOLE>
 __device__ inline void put_rows(E* out, const Pass& a, int n, int c, int l, const f32x4_t (&O)[TI][RT]) {
-    typedef typename Vec<E, 4>::type four_t;
+    static_assert(!WHOLE || sizeof(E) == 4, "a tile's four columns are the 16 bytes of a store");
     const uint32_t row = (uint32_t)a.ldo * (uint32_t)sizeof(E);
     const auto rows = __builtin_amdgcn_make_buffer_rsrc(out, 0, (int)(n * row), 0x00027000);
 #pragma unroll
@@ -206,11 +206,7 @@ __device__ inline void put_rows(E* out, const Pass& a, int n, int c, int l, cons
 #pragma unroll
         for (int it = 0; it < TI; ++it) {
             if constexpr (WHOLE) {
-                const four_t e = __builtin_convertvector(O[it][rt], four_t);
-                if constexpr (sizeof(E) == 2)
-                    __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2_t, e), rows, to + it * 16 * row, 0, 0);
-                else
-                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, e), rows, to + it * 16 * row, 0, 0);
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, O[it][rt]), rows, to + it * 16 * row, 0, 0);
             } else if (16 * it + l < n) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
