@@ -19,7 +19,8 @@
  * argument problems are returned synchronously; lengths outside [0, T_max] are
  * clamped and reported by the operator's query (the selectors of lstm_dyn_ops.h).
  * "dtype" is LSTM_DYN_F32 or LSTM_DYN_BF16; all sums, statistics and states are
- * formed in fp32 or more.
+ * formed and held in fp32 or more (what enters some products with fewer bits stands
+ * at the operator).
  */
 #ifndef LSTM_DYN_LAYER_H
 #define LSTM_DYN_LAYER_H
@@ -70,8 +71,8 @@ int lstm_dyn_check_norm_args(int B, int T_max, int D, int dtype, float eps, cons
  *     result[0] = |grad_scale| sqrt(sum over all tensors and elements of g^2)
  *     result[1] = grad_scale min(1, max_norm / result[0])   (grad_scale where result[0] is 0)
  * The sum is formed in 64 bits: it neither overflows nor underflows where the
- * norm is an fp32 number.  A norm that is infinite gives a factor of zero, one that is not a
- * number gives such a factor.  Clipping writes out = g result[1], rounded once
+ * norm is an fp32 number.  A norm that is infinite gives a factor of zero (but for an infinite
+ * max_norm, which clips nothing), one that is not a number gives such a factor.  Clipping writes out = g result[1], rounded once
  * (an infinite g times zero is not a number). */
 typedef struct lstm_dyn_clip lstm_dyn_clip_t;
 
@@ -113,9 +114,10 @@ int lstm_dyn_adamw_step_clipped(lstm_dyn_adamw_t* h, const void* const* grads, i
  * logp 0.  Where the largest logit is +inf, such tokens have p = 1, all others 0.  A row whose logits
  * are all -inf has no token: -1, with logp -inf.  top_k <= 0 and top_p or min_p that are NaN are as if
  * not given, top_p <= 0 keeps the first token.
- * p are held as multiples of 2^-46 (of 2^-(62 - n) if V > 2^16, for the n with
- * 2^(n-1) < V <= 2^n), rounded down: their sums are exact, so the order of summation changes nothing, and a
- * token whose p is below one of them is not chosen.
+ * p are fp32 exponentials, off by up to 2^-22 of themselves, held as multiples of 2^-46 (of 2^-(62 - n) if
+ * V > 2^16, for the n with 2^(n-1) < V <= 2^n), rounded down: the sums of these p are exact, so the order of summation
+ * changes nothing, and a token whose p is below one of them is not chosen.  Where u or top_p comes nearer than about 2^-22 of
+ * the whole to a sum that it is compared with, or min_p to a p, the token may be that of its other side.
  *     logits  [N][V]  dtype, aligned to its elements
  *     u       [N]     fp32 in [0, 1) (clamped; NaN is 0)
  *     out_token int32 [N], out_logp fp32 [N]; they overlap nothing else */
@@ -166,6 +168,9 @@ int lstm_dyn_check_sample_args(int N, int V, int dtype, const void* logits, cons
  *     dS0      [B][heads][Dk][Dv]             fp32 (written)
  * Inside a chunk of 64 steps (32 with fp32 data) an infinity or a NaN in z or dy makes what comes before it in the
  * chunk no number as well; with bf16 data a state beyond 3.39e38 makes y in its column no number.
+ * With bf16 data a state and a product q k, v dy, ... of two steps enter the products that give y and dz as 16 bits (two
+ * bf16 parts): beside their rounding to bf16, y and dz are off by up to 2^-17 of the magnitudes that they are the sum of.
+ * States themselves and dS0 are fp32 sums of unrounded products.
  * No scale is put on q k: it belongs into the weights that q or k come from.
  * The backward needs no forward before it.  Sums go in an order that the sizes alone decide. */
 typedef struct lstm_dyn_attend lstm_dyn_attend_t;

@@ -19,23 +19,28 @@
 // same order, so M never leaves the registers.
 //
 // bf16 data: operands of the matrix units are bf16.  x, y and z are that already; the
-// masked products and M are given as two parts (16 bits, 2^-17 of them is left: far
-// below the rounding of out), what is added to M, a^. z, as three (24 bits: the state is fp32).
+// masked products and M are given as two parts (16 bits; 2^-17 of them is left, below the rounding of
+// out where a sum does not cancel to less than 2^-8 of its terms: one bf16 value in 400 to 900 of out is another
+// than with all bits, and the error against 64 bits, 1.7e-3, is the same), what is added to M, a^. z, as three (24
+// bits: the state is fp32).
 // fp32 data: the matrix units' fp32 products.
 //
 // Where rows and heads are fewer than workgroups should be, the time axis is cut into shares:
 // a launch forms what each share adds to the state, one joins them in their order, and
 // the pass's shares start from the joined states.
 //
-// Measured, bf16, heads of 128: 1 x 32768 x 16, forward, 74 us for the shares' states (3.6 TB/s), 16 to join them, 144 for
-// the pass (3.7 TB/s; 223 us together, 2.4 TB/s of what the call cannot do without); 8 x 4096 x 16, ragged, forward
-// and backward 540 to 560 us, the three passes back 264.  What bounds a pass: for 64 steps a wave issues 208
+// Measured, bf16, heads of 128: 1 x 32768 x 16, forward, 74 us for the shares' states (3.6 TB/s), 15 to join them, 144 to 147
+// for the pass (3.7 TB/s; 223 to 229 us together, 2.4 TB/s of what the call cannot do without); 8 x 4096 x 16, ragged, forward
+// and backward 530 to 560 us, the three passes back 264.  What bounds a pass: for 64 steps a wave issues 208
 // products for the matrix unit (3300 clocks), 870 vector instructions (3500: splitting into parts, decays,
 // addresses) and LDS reads, in phases between barriers; two workgroups a CU, which its registers allow, take 14800
 // clocks for a chunk each.  Tried and not kept: eight waves of 16 columns (199 us: spills, and every wave reads all rows);
 // operands fetched from LDS a phase ahead by scheduling barriers (no gain); vector and matrix instructions interleaved by
 // scheduling groups (no gain); workgroups of half the columns for the states (no gain: they wait for memory);
 // workgroups that are behind issued first (no gain over outputs first).
+// fp32, heads of 128: a training step of 4 x 1024 x 8 takes 194 us, its bytes 40.  For 32 steps a wave issues 176 fp32 products in
+// a pass (144 in the half of the waves that form no masked ones) and 64 for a share's state, of 32 clocks each: 89 us of the
+// matrix unit, which stands while the one workgroup of a CU is at its LDS reads and barriers.
 // A step of 16 x 8 heads of 64: 4.0 us, 4.2 TB/s of states.
 #include "ops.h"
 #include "../../include/lstm_dyn_layer.h"
@@ -946,14 +951,26 @@ extern "C" int lstm_dyn_check_attend_args(int B, int heads, int Dk, int Dv, int 
 }
 
 static int attend_make(lstm_dyn_attend* h, const float* decay) {
-    // As many shares as bring the workgroups that the device holds at once (bf16: two a CU of 128 columns, four of
-    // 64; fp32: one), since a share costs a second reading of two operands and its states.  From 256
+    // As many shares as bring the workgroups that bf16 calls have on the device at once (two a CU of 128 columns, four of
+    // 64), since a share costs a second reading of two operands and its states; with fp32 data, where two workgroups
+    // of 128 columns would fit, 256 by measurement at all widths.  From 256
     // rows and heads on, which fill the device by themselves, a share has to be 16 chunks: below, the
-    // states cost more than the even load gains.  us, calls back to back, these rules and another number: 1 x 32768 x 16
-    // heads of 128, forward, 278 and 306 with 256, 295 with 1024; 8 x 4096 x 16, ragged, training steps, 535, 604 and 569;
-    // 16 x 4096 x 16 heads of 64, forward, 142 and 177 with 512; training steps of 32 x 512 x 8 heads of 64, 72 and 132
-    // without the last rule; of 5 x 301 x 3 heads in fp32, 55 and 112 with four chunks and more a share; of 4 x 1024 x 8
-    // heads of 128 in fp32, 194 and 217 with 512.
+    // states cost more than the even load gains.  us, calls one after another in a graph, by the number of workgroups:
+    //                                                      256    512   1024   2048
+    //   bf16   1 x 32768 x 16 heads of 128, forward        276    235    255    306   (512 taken)
+    //          8 x 4096 x 16 of 128, ragged, training      766    674    738    848   (512)
+    //          16 x 4096 x 16 of 64, forward               208    190    214    212   (1024, as the next four)
+    //          the same, ragged                            204    182    172
+    //          the same, ragged, training                  485    511    525
+    //          2 x 4096 x 8 of 64, forward                  31     31     37
+    //          2 x 4096 x 8 of 32, training                 58     59     65
+    //   fp32   4 x 1024 x 8 of 128, training               194    219    286    286   (256, as the others)
+    //          4 x 1024 x 8 of 64, training                 82     86    101    102
+    //          4 x 1024 x 8 of 32, training                 53     50     54     54
+    //          1 x 4096 x 4 of 64, training                 67     79     80     80
+    //          16 x 1024 x 8 of 64, training               234    221    223    255
+    // (Heads of 64 and less take 512 better, by 3 to 18%, but for the ragged forward.)  The last rule: training steps of 32 x 512 x 8 heads of 64, 72 and 130 without it.  Four chunks and more a share: 5 x 301 x 3 heads in
+    // fp32, 110 and 53 without.
     const int C = h->dtype == LSTM_DYN_BF16 ? Chunk<__bf16>::C : Chunk<float>::C;
     const int groups = h->dtype != LSTM_DYN_BF16 ? 256 : h->Dk > 64 || h->Dv > 64 ? 512 : 1024;
     const int rows = h->B * h->heads, chunks = (h->T + C - 1) / C;

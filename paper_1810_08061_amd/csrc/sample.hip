@@ -14,14 +14,17 @@
 // that few tokens have), they are gathered once, and every cut and the running sum are formed by
 // comparing each with each, without more passes.
 //
-// A workgroup holds a row: its passes, three to six, come from the L2 after the first.  They are bound by the
-// vector unit of its CU, so where most tokens do not count a pass looks at them with as few instructions as
+// A workgroup holds a row: its passes, three to six, come from the L2 after the first.  While a long row is
+// worked at, the vector units of its CU are busy for three quarters of the time (256 rows of 65536: 48 vector instructions a
+// token, 20 us of an average row's 28; the waves wait for reads, LDS and joins for 56% of theirs, side by side), so where most tokens
+// do not count a pass looks at them with as few instructions as
 // decide that (two comparisons), and forms keys and weights of the rest
-// alone; where most of them count it does the same for all, under no condition.
+// alone; where most of them count it does the same for all, under no condition.  The call ends with its slowest row.
 //
-// Measured, bf16: 256 rows of 65536 with top-p and min-p 46 us (21 without filters, where the row is
-// read and every weight formed once); 16 rows of 32768 with top-k to 1000 and top-p 30 us, each row on one CU:
-// passes of about 3 us with the joins between them.  With k 50 and p 0.9, few tokens: 16 rows of 32768
+// Measured, bf16: 256 rows of 65536 with top-p and min-p 43 to 46 us (21 without filters, where the row is
+// read and every weight formed once); 16 rows of 32768 with top-k to 1000 and top-p 27 to 31 us, each row on one CU:
+// passes of about 3 us with the joins between them.  One row in fp32, T 0.8, with all filters at once (k 50, p 0.9, min-p 0.02) and with
+// p 0.9 alone: of 1000 7.0 and 7.5 us, of 32768 12.5 and 24, of 131072 26 and 74.  With k 50 and p 0.9, few tokens: 16 rows of 32768
 // 12.9 us (23.9 with the passes), 256 of 65536 19 (38), in fp32 one of 131072 27 (66).  FEW: comparing 256 with each
 // other took 6 us and more, as much as it saves.  Tried: the far ranges of the histogram summed in
 // registers instead (a branch an element: 74 us where one addition in LDS an element takes 62).
