@@ -79,3 +79,32 @@ def test_shares_of_several_chunks(dtype, B, heads, Dk, Dv, T, span):
         got = m.backward(s["z"], _lengths(L), s["S0"], s["dy"], s["dS"])
         _compare(dict(got, y=y, S=S), s, L, decay[:heads], Dk, Dv, dtype)
         assert m.status() == ld.OK
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_state_that_replays_carry_on(dtype):
+    """A captured call whose result lies in its given state, over several shares: every replay goes on from the one before, with
+    eager calls of the same handle between."""
+    import torch
+    B, heads, Dk, Dv, T = 3, 2, 48, 64, 900
+    r = np.random.default_rng(3)
+    s = _inputs(r, dtype, B, T, heads, Dk, Dv)
+    L = _lengths([900, 70, 0])
+    with ld.LinearAttention(B, heads, Dk, Dv, T, [0.99, 1.0], dtype) as m:
+        assert _shares(m) > 1
+        state = s["S0"].clone()
+        y = torch.empty((B, T, heads * Dv), dtype=s["z"].dtype, device="cuda")
+        m.forward(s["z"], L, s["S0"])
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            m.forward(s["z"], L, state, out_S=state, out_y=y)
+        want = s["S0"]
+        for i in range(4):
+            s["z"].mul_(-0.75)
+            want_y, want = m.forward(s["z"], L, want)
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert (state == want).all() and (y == want_y).all(), i
+        del graph
